@@ -348,88 +348,104 @@ def _plain_rotary(s):
     return [qo.to(t), ko.to(t), dq.to(t), dk.to(t), dwq, dwk]
 
 
-def _grouped(x, Hkv):
-    """[n][Hq][D] -> [Hkv][G n][D], the heads of a group one after another."""
-    n, H, D = x.shape
-    return x.float().permute(1, 0, 2).reshape(Hkv, H // Hkv * n, D).contiguous()
+SCORES = 1 << 28  # held at once
 
 
-def _ungrouped(x, n):
-    """The inverse of _grouped."""
-    Hkv, Gn, D = x.shape
-    return x.reshape(Hkv * (Gn // n), n, D).permute(1, 0, 2)
+def _batches(lens, heads):
+    """Sequences of like length together, by their numbers."""
+    out = []
+    for i in sorted(range(len(lens)), key=lambda i: -lens[i]):
+        most = lens[out[-1][0]] if out else 0
+        if out and 2 * lens[i] >= most and (len(out[-1]) + 1) * heads * most * most <= SCORES:
+            out[-1].append(i)
+        else:
+            out.append([i])
+    return out
 
 
-ROWS = 1 << 28  # scores held at once
+def _padded(x, at):
+    """Rows `at` [B][n] of [T][heads][D] in 32 bits: [B][heads][n][D]."""
+    return x[at].float().transpose(1, 2).contiguous()
 
 
-def _plain_attn_one(q, k, v, scale, causal, do=None):
-    """Attention of one sequence, [n][heads][D] each: output, log of the sum
-    of exponentials, and with `do` the gradients, in pieces of the queries.
-    Causal: the last query sees every key."""
-    n, Hq, D = q.shape
-    m, Hkv = k.shape[:2]
-    k, v = _grouped(k, Hkv), _grouped(v, Hkv)
-    kt, vt = k.transpose(1, 2).contiguous(), v.transpose(1, 2).contiguous()
-    o = torch.empty((n, Hq, D), device=q.device)
-    lse = torch.empty((n, Hq), device=q.device)
+def _plain_attn_batch(q, k, v, nq, nk, scale, causal, do=None):
+    """Attention of B sequences padded to one length: q [B][Hq][n][D], k and v
+    [B][Hkv][m][D], nq and nk their lengths [B]; output, log of the sum of
+    exponentials, and with `do` (zero in the padding) the gradients, in pieces
+    of the queries.  Causal: a sequence's last query sees every key."""
+    B, Hq, n, D = q.shape
+    Hkv, m = k.shape[1:3]
+    dev = q.device
+    kt, vt = k.transpose(2, 3).contiguous(), v.transpose(2, 3).contiguous()
+    o, lse = torch.empty_like(q), torch.empty((B, Hq, n), device=dev)
     if do is not None:
-        dq, dk, dv = torch.empty_like(o), torch.zeros_like(k), torch.zeros_like(v)
-    piece = max(1, min(n, ROWS // max(1, Hq * m)))
+        dq, dk, dv = torch.empty_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    j = torch.arange(m, device=dev)
+    last = nk.view(B, 1, 1) - 1
+    piece = max(1, min(n, SCORES // max(1, B * Hq * m)))
     for a in range(0, n, piece):
         b = min(n, a + piece)
-        qs = _grouped(q[a:b], Hkv)
+        group = lambda t: t[:, :, a:b].reshape(B, Hkv, -1, D)  # noqa: E731
+        whole = lambda t: t.reshape(B, Hq, b - a, -1)  # noqa: E731
+        qs = group(q)
         x = torch.matmul(qs, kt) * scale
+        see = last.expand(B, b - a, 1)
         if causal:
-            i = torch.arange(a, b, device=q.device)[:, None] + (m - n)
-            hide = torch.arange(m, device=q.device)[None] > i
-            x = x.view(Hq, b - a, m).masked_fill_(hide, float("-inf")).view(Hkv, -1, m)
+            i = torch.arange(a, b, device=dev).view(1, -1, 1)
+            see = torch.minimum(last, i + last + 1 - nq.view(B, 1, 1))
+        x = whole(x).masked_fill_((j > see).unsqueeze(1), float("-inf")).view(B, Hkv, -1, m)
         top = x.amax(-1, keepdim=True)
         p = torch.exp(x - top)
         z = p.sum(-1, keepdim=True)
         p = p / z
         os = torch.matmul(p, v)
-        o[a:b] = _ungrouped(os, b - a)
-        lse[a:b] = _ungrouped(top + z.log(), b - a)[..., 0]
+        o[:, :, a:b] = whole(os)
+        lse[:, :, a:b] = whole(top + z.log())[..., 0]
         if do is not None:
-            g = _grouped(do[a:b], Hkv)
-            dv += torch.matmul(p.transpose(1, 2), g)
+            g = group(do)
+            dv += torch.matmul(p.transpose(2, 3), g)
             ds = p * (torch.matmul(g, vt) - (g * os).sum(-1, keepdim=True)) * scale
-            dq[a:b] = _ungrouped(torch.matmul(ds, k), b - a)
-            dk += torch.matmul(ds.transpose(1, 2), qs)
-    if do is None:
-        return o, lse
-    return o, lse, dq, _ungrouped(dk, m), _ungrouped(dv, m)
+            dq[:, :, a:b] = whole(torch.matmul(ds, k))
+            dk += torch.matmul(ds.transpose(2, 3), qs)
+    return (o, lse) if do is None else (o, lse, dq, dk, dv)
 
 
 def _plain_attn(s):
     c = s["case"]
     q, k, v = _split(s["qkv"], c)
-    scale = 1.0 / math.sqrt(c["D"])
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(q.shape[:2], device=q.device)
-    if c["bwd"]:
-        dqkv = torch.empty_like(s["qkv"])
-        dq, dk, dv = _split(dqkv, c)
-    a = 0
-    for n in s["lens"]:
-        b = a + n
-        r = _plain_attn_one(q[a:b], k[a:b], v[a:b], scale, c["causal"],
-                            s["do"][a:b] if c["bwd"] else None)
-        o[a:b], lse[a:b] = r[0], r[1]
+    T = q.shape[0]
+    # one row more, which takes the padding's results
+    o, lse = q.new_empty((T + 1,) + q.shape[1:]), torch.empty((T + 1, c["Hq"]), device=q.device)
+    d = q.new_empty((T + 1,) + s["qkv"].shape[1:]) if c["bwd"] else None
+    n_all = (s["start"][1:] - s["start"][:-1]).long()
+    for which in _batches(s["lens"], c["Hq"]):
+        L = max(s["lens"][i] for i in which)
+        ids = torch.tensor(which, device=q.device)
+        n, i = n_all[ids], torch.arange(L, device=q.device)
+        at = s["start"].long()[ids][:, None] + i
+        here = i < n[:, None]
+        at, to = at.clamp(max=T - 1), torch.where(here, at, T)
+        do = _padded(s["do"], at) * here[:, None, :, None] if c["bwd"] else None
+        r = _plain_attn_batch(_padded(q, at), _padded(k, at), _padded(v, at), n, n,
+                              1.0 / math.sqrt(c["D"]), c["causal"], do)
+        o[to] = r[0].transpose(1, 2).to(o.dtype)
+        lse[to] = r[1].transpose(1, 2)
         if c["bwd"]:
-            dq[a:b], dk[a:b], dv[a:b] = r[2], r[3], r[4]
-        a = b
-    return [o, dqkv] if c["bwd"] else [o, lse]
+            d[to] = torch.cat(r[2:], 1).transpose(1, 2).to(o.dtype)
+    return [o[:T], d[:T]] if c["bwd"] else [o[:T], lse[:T]]
 
 
 def _plain_step(s):
     c = s["case"]
-    o = torch.empty_like(s["q"])
-    for i, n in enumerate(s["lens"]):
-        a = i * s["cap"]
-        o[i] = _plain_attn_one(s["q"][i], s["kc"][a:a + n], s["vc"][a:a + n],
-                               1.0 / math.sqrt(c["D"]), True)[0]
+    q, o = s["q"], torch.empty_like(s["q"])
+    for which in _batches(s["lens"], c["Hq"]):
+        L = max(s["lens"][i] for i in which)
+        ids = torch.tensor(which, device=q.device)
+        at = s["start"].long()[ids][:, None] + torch.arange(L, device=q.device)
+        r = _plain_attn_batch(q[ids].float().transpose(1, 2).contiguous(), _padded(s["kc"], at),
+                              _padded(s["vc"], at), torch.full_like(ids, c["n"]),
+                              s["len"].long()[ids], 1.0 / math.sqrt(c["D"]), True)
+        o[ids] = r[0].transpose(1, 2).to(o.dtype)
     return [o]
 
 

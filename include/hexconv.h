@@ -296,6 +296,144 @@ int hexpool3d_bwd(const void *dy, const uint16_t *argmax, const void *relu_y, vo
                   int C, int D, int H, int W, int k, int kz, int stride, int stride_z,
                   hex_pool_mode mode, hex_dtype dt, void *stream);
 
+/*
+ * Attention over hexagonal pixels.  The lit pixels of a camera event are a
+ * sequence of tokens, each with a position (the pixel's place on the grid,
+ * and its time where the camera is time-resolved, Sec. 2.4); events differ
+ * in length, so a batch is PACKED: the tokens of all events one after
+ * another, with int32 offsets on the device.  These are the parts of an
+ * attention layer over such sequences; the paper has no counterpart.
+ *
+ * Conventions, beside those above:
+ *  - a tensor of tokens is [tokens][heads][D]: heads dense, tokens a stride
+ *    `ld` apart (in elements), so that queries, keys and values may be parts
+ *    of one tensor.  ld >= heads * D, and a row of tokens must start at a
+ *    16-byte boundary (ld a multiple of 4 in float32, 8 in bf16).
+ *  - D, the head size, is a multiple of 8 up to HEX_ATTN_MAX_DIM.  Hq query
+ *    heads share Hkv key heads, Hq / Hkv in a row each.
+ *  - Offsets into tensors are 64 bits wide: a cache may be larger than 2^31
+ *    elements.
+ *  - Offsets and lengths on the device are not checked on the host; the
+ *    kernels bring them into the tensors' bounds, so wrong ones give wrong
+ *    results and no access outside.
+ *  - Outputs of rows that belong to no sequence are left as they are.
+ *  - Products take bf16 operands as they are and add in float32.
+ *    Probabilities and their gradients are rounded to bf16 for their second
+ *    product (bf16 calls); sums, maxima and logarithms are float32.
+ *  - Outputs must not overlap inputs.
+ */
+#define HEX_ATTN_MAX_DIM 128
+#define HEX_ROTARY_MAX_AXES 8
+enum { HEX_ATTN_CAUSAL = 1 };
+enum { HEX_ROTARY_NORM = 1 };
+
+/*
+ * Norm and rotation of query and key heads.  For every token t and head:
+ *   y = x / sqrt(mean(x^2) + eps) * w      (HEX_ROTARY_NORM; else y = x)
+ *   out_j         = y_j cos a_j - y_(j + D/2) sin a_j
+ *   out_(j + D/2) = y_j sin a_j + y_(j + D/2) cos a_j,   j < D/2,
+ *   a_j = pos[t][axis[j]] * freq[j]
+ * pos is float32 [T][A], freq float32 [D/2] (radians a unit; 0 leaves a pair
+ * as it is), axis int32 [D/2]; a pair whose axis is not in 0 .. A-1 is left
+ * as it is.  Angles are reduced from the exact product; up to 2^20 radians
+ * their error is below 1e-6.  wq and wk [D], in dtype dt, may be NULL (ones).
+ *
+ * With `slot` (int32 [T]) the keys of token t go to row slot[t] of ko, and
+ * with v and vo the values, unchanged, to row slot[t] of vo: the caches of
+ * hexattn_step, n_slots rows each.  A slot outside 0 .. n_slots-1 stores
+ * neither.  No two tokens of a call may share a slot.  Without slot, row t.
+ * v and vo may be NULL (both).
+ */
+int hexrotary_fwd(const void *q, const void *k, const void *v, const float *pos,
+                  const float *freq, const int32_t *axis, const void *wq, const void *wk, void *qo,
+                  void *ko, void *vo, const int32_t *slot, int T, int Hq, int Hkv, int D, int A,
+                  int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, int64_t ldko, int64_t ldvo,
+                  int n_slots, float eps, int flags, hex_dtype dt, void *stream);
+
+/* Bytes of device workspace hexrotary_bwd needs (0 for invalid arguments). */
+size_t hexrotary_bwd_workspace(int T, int Hq, int Hkv, int D, hex_dtype dt);
+
+/*
+ * Gradients of hexrotary_fwd (without slots): dq and dk from dqo and dko,
+ * and the weights' dwq and dwk, float32 [D], each nullable.  q and k are the
+ * forward's inputs; without HEX_ROTARY_NORM they are not read and may be
+ * NULL, and dwq, dwk and ws must be NULL.  ws: at least
+ * hexrotary_bwd_workspace(...) bytes.  Deterministic.
+ */
+int hexrotary_bwd(const void *q, const void *k, const float *pos, const float *freq,
+                  const int32_t *axis, const void *wq, const void *wk, const void *dqo,
+                  const void *dko, void *dq, void *dk, float *dwq, float *dwk, void *ws,
+                  size_t ws_bytes, int T, int Hq, int Hkv, int D, int A, int64_t ldq, int64_t ldk,
+                  int64_t lddqo, int64_t lddko, int64_t lddq, int64_t lddk, float eps, int flags,
+                  hex_dtype dt, void *stream);
+
+/*
+ * Softmax attention over S packed sequences.  Sequence s has the queries
+ * q_start[s] .. q_start[s+1]-1 of the Tq tokens of q (int32 [S+1],
+ * ascending) and its keys in the Tk tokens of k and v: k_start[s] ..
+ * k_start[s+1]-1 (int32 [S+1]), or, where k_len (int32 [S]) is not NULL,
+ * k_len[s] of them from k_start[s] (int32 [S]) on, as in a cache.
+ *   x_ij = scale q_i . k_j,  lse_i = log sum_j exp(x_ij),
+ *   o_i = sum_j exp(x_ij - lse_i) v_j,  scale >= 0
+ * HEX_ATTN_CAUSAL: with n queries and m keys, query i sees the keys j <=
+ * i + m - n (the last query sees them all).  A row that sees no key gives
+ * o = 0 and lse = -inf.  Whatever lies in k and v outside a sequence's keys,
+ * NaN included, changes nothing.  lse is float32 [Tq][Hq] and may be NULL.
+ */
+int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse,
+                const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, int S,
+                int Tq, int Tk, int Hq, int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv,
+                int64_t ldo, float scale, int flags, hex_dtype dt, void *stream);
+
+/* Bytes of device workspace hexattn_bwd needs (0 for invalid arguments). */
+size_t hexattn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, hex_dtype dt);
+
+/*
+ * Gradients of hexattn_fwd (k_start as offsets [S+1], no k_len): dq, dk and
+ * dv, strides lddq, lddk and lddv, from dout and the forward's o and lse.  A
+ * key head's gradients are the sums over the query heads that share it.
+ * Rows that see no key, and keys that no row sees, get zeros.  ws: at least
+ * hexattn_bwd_workspace(...) bytes.  Deterministic.
+ */
+int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
+                const void *dout, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes,
+                const int32_t *q_start, const int32_t *k_start, int S, int Tq, int Tk, int Hq,
+                int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, int64_t lddout,
+                int64_t lddq, int64_t lddk, int64_t lddv, float scale, int flags, hex_dtype dt,
+                void *stream);
+
+/* Bytes of device workspace hexattn_step needs (may be 0; 0 for invalid
+ * arguments). */
+size_t hexattn_step_workspace(int S, int n, int Hq, int Hkv, int D, int max_len, hex_dtype dt);
+
+/*
+ * Attention of n new tokens of each of S sequences over their caches: q and
+ * o are dense [S][n][Hq][D]; sequence s has the k_len[s] tokens from
+ * k_start[s] on of the Tk tokens of k and v (int32 [S] each), the last n of
+ * them the new tokens themselves, and new token t sees the keys up to its
+ * own.  A row that sees no key gives zeros.  max_len: a bound on the lengths
+ * (longer ones are cut to it), by which the work is split over the keys.
+ * ws: at least hexattn_step_workspace(...) bytes, NULL where that is 0.
+ * Deterministic.
+ */
+int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws, size_t ws_bytes,
+                 const int32_t *k_start, const int32_t *k_len, int S, int n, int Hq, int Hkv,
+                 int D, int Tk, int max_len, int64_t ldk, int64_t ldv, float scale, hex_dtype dt,
+                 void *stream);
+
+/*
+ * Dropout and residual of n elements: y_e = res_e + (kept_e ? x_e / (1 - p)
+ * : 0), 0 <= p < 1; res may be NULL (zeros).  kept_e = bits_e >= floor(p *
+ * 2^32), with bits_e word e % 4 of Philox 4x32-10 (Salmon et al., SC 2011)
+ * for the key rng[0] and the counter (e / 4, rng[1] + call), both 64 bits,
+ * low words first.  rng (device, two 64-bit words: seed and call number) is
+ * read when the kernel runs, so a captured graph draws new masks when the
+ * caller changes it between replays.  The gradient is the same call on dy
+ * without res; no mask is stored.
+ */
+int hexdropout(const void *x, const void *res, void *y, int64_t n, double p, const uint64_t *rng,
+               uint64_t call, hex_dtype dt, void *stream);
+
 /* Static description of a hex_status value. */
 const char *hex_status_string(int status);
 

@@ -1,0 +1,348 @@
+// attn.h -- what the attention kernels share: matrix-core operands of either
+// type, the LDS layout of a staged tile, the walk over packed sequences.
+//
+// All products are 32 x 32 (x 16 in bfloat16, x 2 in float32).  An operand
+// ("fragment") is 8 contraction elements of one row per lane: row = lane % 32,
+// half h = lane / 32.  Result register r of a lane holds row
+// (r % 4) + 8 (r / 4) + 4 h of column lane % 32.
+//
+// The scores are computed with the sequence axis that is contracted next as
+// the result's rows.  A lane's registers 8 s .. 8 s + 7 are then, without any
+// exchange between lanes, the operand of the next product, whose contraction
+// index is the row 16 s + 8 (i / 4) + 4 h + i % 4 for element i; the other
+// operand is read from LDS with rows in the same order (read_rows).
+#pragma once
+
+#include "hexdev.h"
+#include "kernels.h"
+
+namespace hexk {
+namespace attn {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
+
+// log2(e) and ln(2) as a float and what it leaves
+constexpr float kLog2e = 1.4426950408889634f, kLog2eLo = 1.4426950408889634 - kLog2e;
+constexpr float kLn2 = 0.6931471805599453f, kLn2Lo = 0.6931471805599453 - kLn2;
+
+struct FragF32 {
+    float v[8];
+};
+
+template <typename E> struct Elem;
+template <> struct Elem<bf16raw> {
+    using Frag = bf16x8;
+    static constexpr int VEC = 8; // elements of a 16-byte vector
+};
+template <> struct Elem<float> {
+    using Frag = FragF32;
+    static constexpr int VEC = 4;
+};
+
+__device__ __forceinline__ floatx16 mma(bf16x8 a, bf16x8 b, floatx16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mma(const FragF32 &a, const FragF32 &b, floatx16 c)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], c, 0, 0, 0);
+    return c;
+}
+
+// The next 16 elements of a sum over the head dimension.  float32: the
+// matrix core adds them from zero and the vector unit adds that to the sum, so
+// that a score of D = 128 is 8 roundings of its own size and not 64 (scores of
+// 100, whose exponentials carry 100 times a score's relative error: a third
+// of it; the additions run beside the next products).
+__device__ __forceinline__ floatx16 add_product(bf16x8 a, bf16x8 b, floatx16 c)
+{
+    return mma(a, b, c);
+}
+__device__ __forceinline__ floatx16 add_product(const FragF32 &a, const FragF32 &b, floatx16 c)
+{
+    return c + mma(a, b, floatx16{});
+}
+
+// A number of powers of two as hi + lo, and 2^(x scale log2(e) - ref).  At
+// scores of 100 the rounding of the factor and of the reference alone would
+// put float32 probabilities off by 1e-5; so there both are kept in two parts.
+struct Ref {
+    float hi, lo;
+};
+__device__ __forceinline__ Ref ref_of_lse(float lse)
+{
+    const float hi = lse * kLog2e;
+    return Ref{hi, fmaf(lse, kLog2eLo, fmaf(lse, kLog2e, -hi))};
+}
+template <typename E>
+__device__ __forceinline__ float prob(float x, const AttnArgs &a, float hi, float lo)
+{
+    float e = fmaf(x, a.c, -hi);
+    if constexpr (sizeof(E) == 4)
+        e += fmaf(x, a.c_lo, -lo);
+    return __builtin_amdgcn_exp2f(e);
+}
+// log of a sum l of 2^(.. - m), in units of e, with one rounding of its size
+__device__ __forceinline__ float log_sum(float m, float l)
+{
+    return fmaf(m, kLn2, fmaf(m, kLn2Lo, __builtin_amdgcn_logf(l) * kLn2));
+}
+
+// Registers 8 s .. 8 s + 7 of a result as an operand; bfloat16 rounds to
+// nearest even (probabilities lie in [0, 1], their sum is kept in float32
+// from the unrounded values).
+template <typename E> __device__ __forceinline__ typename Elem<E>::Frag to_frag(const floatx16 &x, int s)
+{
+    if constexpr (sizeof(E) == 2) {
+        bf16x8 f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = static_cast<__bf16>(x[8 * s + i]);
+        return f;
+    } else {
+        FragF32 f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f.v[i] = x[8 * s + i];
+        return f;
+    }
+}
+
+// ---- tiles in LDS: rows of DC head elements (a multiple of 32, padded with
+// zeros), 16-byte chunks permuted within the row by its number, so that both
+// reads below spread over all 64 banks: sixteen rows of one chunk
+// (read_cols), and runs of 64 or 128 bytes of four to eight rows (read_rows).
+template <typename E, int DC> struct Tile {
+    static constexpr int PITCH = (DC == 96 ? 128 : DC) * static_cast<int>(sizeof(E)); // bytes a row
+    static constexpr int CPR = DC * static_cast<int>(sizeof(E)) / 16; // chunks in use
+    static constexpr int bytes(int rows) { return rows * PITCH; }
+
+    __device__ __forceinline__ static int swz(int row)
+    {
+        if constexpr (sizeof(E) == 2) {
+            if constexpr (PITCH == 256)
+                return ((row >> 2) & 3) | (row & 3) << 2;
+            else if constexpr (PITCH == 128)
+                return ((row >> 2) & 3) | (row & 2) << 1;
+            else
+                return (row >> 2) & 3;
+        } else {
+            if constexpr (PITCH >= 256)
+                return (row & 3) | (row & 4) << 1 | (row & 8) >> 1;
+            else
+                return (row >> 1) & 7;
+        }
+    }
+    __device__ __forceinline__ static int chunk_at(int row, int chunk)
+    {
+        return row * PITCH + ((chunk ^ swz(row)) << 4);
+    }
+
+    // operand with the head dimension as contraction: row `row` (per lane),
+    // elements 16 s + 8 h ..
+    __device__ __forceinline__ static typename Elem<E>::Frag read_cols(const unsigned char *t,
+                                                                       int row, int s, int h)
+    {
+        if constexpr (sizeof(E) == 2) {
+            return *reinterpret_cast<const bf16x8 *>(t + chunk_at(row, 2 * s + h));
+        } else {
+            FragF32 f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4 u =
+                    *reinterpret_cast<const float4 *>(t + chunk_at(row, 4 * s + 2 * h + j));
+                f.v[4 * j] = u.x, f.v[4 * j + 1] = u.y, f.v[4 * j + 2] = u.z, f.v[4 * j + 3] = u.w;
+            }
+            return f;
+        }
+    }
+
+    // operand with rows as contraction, in the order of a result's registers:
+    // element i is row row0 + 8 (i / 4) + 4 h + i % 4, column 32 d + lane % 32.
+    // bfloat16: the transposing read (16 lanes read four rows of 16 columns,
+    // lane i of them receives column i of the four rows).
+    __device__ __forceinline__ static typename Elem<E>::Frag read_rows(unsigned char *t, int row0,
+                                                                       int d, int lane)
+    {
+        const int h = lane >> 5;
+        if constexpr (sizeof(E) == 2) {
+            using lp = __attribute__((address_space(3))) shortx4 *;
+            const int r = row0 + 4 * h + ((lane & 15) >> 2);
+            const int c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            const int o = 8 * (lane & 1);
+            const shortx4 lo =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(t + chunk_at(r, c) + o));
+            const shortx4 hi =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(t + chunk_at(r + 8, c) + o));
+            return __builtin_bit_cast(bf16x8,
+                                      __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            FragF32 f;
+            const int e = 32 * d + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = row0 + 8 * (i >> 2) + 4 * h + (i & 3);
+                f.v[i] = *reinterpret_cast<const float *>(t + chunk_at(r, e >> 2) + 4 * (e & 3));
+            }
+            return f;
+        }
+    }
+};
+
+// the sum, and the maximum, of a lane's value and lane ^ 32's: the swap gives
+// both lanes the lower half's value and the upper half's
+struct Halves {
+    float lower, upper;
+};
+__device__ __forceinline__ Halves halves(float v)
+{
+    const int i = __builtin_bit_cast(int, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    const uint32_t a = r[0], b = r[1]; // a bit cast of r[1] itself reads r[0]
+    return Halves{__uint_as_float(a), __uint_as_float(b)};
+}
+__device__ __forceinline__ float both_sum(float v)
+{
+    const Halves x = halves(v);
+    return x.lower + x.upper;
+}
+__device__ __forceinline__ float both_max(float v)
+{
+    const Halves x = halves(v);
+    return fmaxf(x.lower, x.upper);
+}
+
+// One operand of 8 head elements from global memory, zeros past D; `p` is the
+// row's start (16-byte aligned), c the first element (a multiple of 8, as D).
+template <typename E>
+__device__ __forceinline__ typename Elem<E>::Frag load_frag(const E *p, int c, int D)
+{
+    if constexpr (sizeof(E) == 2) {
+        uint4 u{0, 0, 0, 0};
+        if (c < D)
+            u = *reinterpret_cast<const uint4 *>(p + c);
+        return __builtin_bit_cast(bf16x8, u);
+    } else {
+        FragF32 f;
+        float4 u{0, 0, 0, 0}, w{0, 0, 0, 0};
+        if (c < D) {
+            u = *reinterpret_cast<const float4 *>(p + c);
+            w = *reinterpret_cast<const float4 *>(p + c + 4);
+        }
+        f.v[0] = u.x, f.v[1] = u.y, f.v[2] = u.z, f.v[3] = u.w;
+        f.v[4] = w.x, f.v[5] = w.y, f.v[6] = w.z, f.v[7] = w.w;
+        return f;
+    }
+}
+
+__device__ __forceinline__ float dot8(const FragF32 &a, const FragF32 &b)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        s = fmaf(a.v[i], b.v[i], s);
+    return s;
+}
+__device__ __forceinline__ float dot8(bf16x8 a, bf16x8 b)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        s = fmaf(static_cast<float>(a[i]), static_cast<float>(b[i]), s);
+    return s;
+}
+
+// ---- packed sequences ----------------------------------------------------
+// The rows of one (sequence, key head) are its query tokens times the G query
+// heads that share the key head, heads fastest.  Work is handed out in tiles
+// of TR rows.  Sequence s owns tile slots start[s] G / TR + s up to the next
+// sequence's first, which is as many as it needs or one more; so the slots
+// are known without the lengths on the host, rows G / TR + S in all.
+
+// token of row r: r / G by the reciprocal, which gives it or one less
+__device__ __forceinline__ int row_token(Group g, int r)
+{
+    const uint32_t t = __umulhi(static_cast<uint32_t>(r), g.inv);
+    return static_cast<int>(t + (static_cast<uint32_t>(r) - t * g.G >= static_cast<uint32_t>(g.G)));
+}
+
+inline int attn_slots(int T, int G, int TR, int S)
+{
+    return static_cast<int>(static_cast<int64_t>(T) * G / TR) + S;
+}
+
+// keys of sequence s: its k_len from k_start on, or up to the next start
+__device__ __forceinline__ void key_span(const AttnArgs &a, int s, int &begin, int &n)
+{
+    begin = min(max(a.k_start[s], 0), a.Tk);
+    const int end = a.k_len != nullptr ? a.k_len[s] : a.k_start[s + 1] - begin;
+    n = min(min(max(end, 0), a.max_len), a.Tk - begin);
+}
+
+// four results in a row of an output (8- or 16-byte aligned)
+__device__ __forceinline__ void store4(float *p, float x, float y, float z, float w)
+{
+    *reinterpret_cast<float4 *>(p) = float4{x, y, z, w};
+}
+__device__ __forceinline__ void store4(bf16raw *p, float x, float y, float z, float w)
+{
+    *reinterpret_cast<ushort4 *>(p) =
+        ushort4{from_f<bf16raw>(x), from_f<bf16raw>(y), from_f<bf16raw>(z), from_f<bf16raw>(w)};
+}
+
+// one lane's results of a column: registers 4 i .. 4 i + 3 are elements
+// c0 + 8 i .. of the row at p, those below D are stored, times f
+template <typename E>
+__device__ __forceinline__ void store_col(E *p, const floatx16 &x, int c0, int D, float f)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c0 + 8 * i < D)
+            store4(p + c0 + 8 * i, x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f,
+                   x[4 * i + 3] * f);
+}
+
+__device__ __forceinline__ int clamp_start(const int *start, int i, int T)
+{
+    return min(max(start[i], 0), T);
+}
+
+struct Span {
+    int seq;      // sequence
+    int begin, n; // its tokens
+    int tile;     // which of its tiles
+};
+
+// Sequence that owns tile slot w: 64 probes at once, log_64(S) rounds.
+template <int TR>
+__device__ __forceinline__ Span find_span(const int *start, int S, int T, int G, int w)
+{
+    const int lane = threadIdx.x & 63;
+    auto first = [&](int i) {
+        return static_cast<int>(static_cast<int64_t>(clamp_start(start, i, T)) * G / TR) + i;
+    };
+    int lo = 0, n = S;
+    while (n > 1) {
+        const int step = (n + 63) >> 6;
+        const int off = lane * step;
+        const bool ok = off < n && first(lo + off) <= w;
+        const int c = max(1, __popcll(__ballot(ok)));
+        lo += (c - 1) * step;
+        n = min(step, n - (c - 1) * step);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    Span s;
+    s.seq = lo;
+    s.begin = clamp_start(start, lo, T);
+    s.n = max(0, clamp_start(start, lo + 1, T) - s.begin);
+    s.tile = w - first(lo);
+    return s;
+}
+
+} // namespace attn
+} // namespace hexk

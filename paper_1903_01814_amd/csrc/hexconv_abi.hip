@@ -2,6 +2,7 @@
 // argument validation (host only, before anything is enqueued), choice of
 // kernel per shape regime, and launch-status mapping.
 #include <atomic>
+#include <float.h>
 #include <math.h>
 #include <mutex>
 #include <stdint.h>
@@ -419,6 +420,78 @@ void *scratch_ptr()
         g_scratch_dev[dev] = p;
     }
     return g_scratch_dev[dev];
+}
+
+// ---- attention over packed sequences
+
+constexpr int64_t kMaxRows = (INT64_C(1) << 31) - 4096; // row numbers, and the tile past them, are 32 bits
+constexpr int kMaxKeys = 1 << 30;                       // of a cache
+constexpr int64_t kMaxBlocks = (INT64_C(1) << 24) - 1;  // 256 threads each, 2^32 of them in all
+
+int64_t vec(int dt) { return dt == HEX_F32 ? 4 : 8; } // elements of 16 bytes
+
+// heads and head size
+int check_heads(int Hq, int Hkv, int D, int dt)
+{
+    if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || D < 1 || !dtype_ok(dt))
+        return HEX_ERR_INVALID_ARG;
+    if (D % 8 != 0 || D > HEX_ATTN_MAX_DIM || Hq > 65535)
+        return HEX_ERR_UNSUPPORTED;
+    return HEX_OK;
+}
+
+// a token stride: room for the heads, rows at 16-byte boundaries
+bool stride_ok(int64_t ld, int heads, int D, int dt)
+{
+    return ld >= static_cast<int64_t>(heads) * D && ld % vec(dt) == 0;
+}
+
+int check_attn(int S, int Tq, int Tk, int Hq, int Hkv, int D, int dt)
+{
+    if (S < 0 || Tq < 0 || Tk < 0)
+        return HEX_ERR_INVALID_ARG;
+    const int rc = check_heads(Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    // a row is (token, query head); a block takes 128 of them, or of the keys
+    const int64_t qrows = static_cast<int64_t>(Tq) * Hq, krows = static_cast<int64_t>(Tk) * Hkv;
+    const int64_t most = qrows > krows ? qrows : krows;
+    if (most > kMaxRows || most / 128 + static_cast<int64_t>(S) * Hkv > kMaxBlocks)
+        return HEX_ERR_UNSUPPORTED;
+    return HEX_OK;
+}
+
+hexk::AttnArgs attn_args(const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, int S,
+                   int Tq, int Tk, int Hq, int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv,
+                   int64_t ldo, float scale, bool causal)
+{
+    hexk::AttnArgs a;
+    a.q_start = q_start;
+    a.k_start = k_start;
+    a.k_len = k_len;
+    a.S = S;
+    a.Tq = Tq;
+    a.Tk = Tk;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.D = D;
+    a.group = hexk::make_group(Hq / Hkv);
+    a.ldq = ldq;
+    a.ldk = ldk;
+    a.ldv = ldv;
+    a.ldo = ldo;
+    a.scale = scale;
+    // log2(e) times the scale in two parts, both above 0, so that a masked
+    // score of -inf stays one
+    const double c = fmax(static_cast<double>(scale) * 1.4426950408889634, FLT_MIN);
+    a.c = static_cast<float>(c);
+    if (a.c > c)
+        a.c = nextafterf(a.c, 0.f);
+    a.c_lo = fmaxf(static_cast<float>(c - a.c), FLT_MIN);
+    a.causal = causal;
+    a.slots = 0;
+    a.max_len = Tk;
+    return a;
 }
 
 } // namespace
@@ -884,6 +957,203 @@ int hexpool3d_bwd(const void *dy, const uint16_t *argmax, const void *relu_y, vo
     if (!force_generic() && hexk::pool_any_ok(sh, d, true, true, mode))
         return launched(hexk::pool_any_bwd(dy, argmax, relu_y, dx, sh, mode, d, true, st));
     return launched(hexk::pool_bwd_generic(dy, argmax, relu_y, dx, sh, mode, d, true, st));
+}
+
+int hexrotary_fwd(const void *q, const void *k, const void *v, const float *pos,
+                  const float *freq, const int32_t *axis, const void *wq, const void *wk, void *qo,
+                  void *ko, void *vo, const int32_t *slot, int T, int Hq, int Hkv, int D, int A,
+                  int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, int64_t ldko, int64_t ldvo,
+                  int n_slots, float eps, int flags, hex_dtype dt, void *stream)
+{
+    if (T < 0 || A < 1 || n_slots < 0 || !(eps >= 0.f) || !isfinite(eps) ||
+        (flags & ~HEX_ROTARY_NORM) != 0 || (v == nullptr) != (vo == nullptr))
+        return HEX_ERR_INVALID_ARG;
+    int rc = check_heads(Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (A > HEX_ROTARY_MAX_AXES || T / 8 > kMaxBlocks - 1)
+        return HEX_ERR_UNSUPPORTED;
+    if (!stride_ok(ldq, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt) ||
+        !stride_ok(ldqo, Hq, D, dt) || !stride_ok(ldko, Hkv, D, dt) ||
+        (v != nullptr && (!stride_ok(ldv, Hkv, D, dt) || !stride_ok(ldvo, Hkv, D, dt))))
+        return HEX_ERR_INVALID_ARG;
+    if (T == 0)
+        return HEX_OK;
+    if ((rc = ptrs_ok({q, k, pos, freq, axis, qo, ko}, {wq, wk, v, vo, slot})) != HEX_OK)
+        return rc;
+    const hexk::RotaryArgs a{pos, freq, axis, T,  ldq, ldk, ldv,     ldqo, ldko,
+                             ldvo, 0,   0,    Hq, Hkv, D,   A,       n_slots, eps,
+                             (flags & HEX_ROTARY_NORM) != 0};
+    return launched(hexk::rotary_fwd(q, k, v, wq, wk, qo, ko, vo, slot, a, static_cast<Dtype>(dt),
+                                     static_cast<hipStream_t>(stream)));
+}
+
+size_t hexrotary_bwd_workspace(int T, int Hq, int Hkv, int D, hex_dtype dt)
+{
+    if (T < 1 || check_heads(Hq, Hkv, D, dt) != HEX_OK)
+        return 0;
+    return static_cast<size_t>(hexk::rotary_bwd_blocks(T)) * 2 * D * sizeof(float);
+}
+
+int hexrotary_bwd(const void *q, const void *k, const float *pos, const float *freq,
+                  const int32_t *axis, const void *wq, const void *wk, const void *dqo,
+                  const void *dko, void *dq, void *dk, float *dwq, float *dwk, void *ws,
+                  size_t ws_bytes, int T, int Hq, int Hkv, int D, int A, int64_t ldq, int64_t ldk,
+                  int64_t lddqo, int64_t lddko, int64_t lddq, int64_t lddk, float eps, int flags,
+                  hex_dtype dt, void *stream)
+{
+    const bool norm = (flags & HEX_ROTARY_NORM) != 0;
+    if (T < 0 || A < 1 || !(eps >= 0.f) || !isfinite(eps) || (flags & ~HEX_ROTARY_NORM) != 0)
+        return HEX_ERR_INVALID_ARG;
+    int rc = check_heads(Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (A > HEX_ROTARY_MAX_AXES || T / 8 > kMaxBlocks - 1)
+        return HEX_ERR_UNSUPPORTED;
+    if (!stride_ok(lddqo, Hq, D, dt) || !stride_ok(lddko, Hkv, D, dt) ||
+        !stride_ok(lddq, Hq, D, dt) || !stride_ok(lddk, Hkv, D, dt) ||
+        (norm && (!stride_ok(ldq, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt))))
+        return HEX_ERR_INVALID_ARG;
+    if (!norm && (dwq != nullptr || dwk != nullptr))
+        return HEX_ERR_INVALID_ARG;
+    if ((rc = ptrs_ok({}, {q, k, wq, wk, dwq, dwk, ws})) != HEX_OK)
+        return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (T == 0) // no token: the weights' gradients are zero
+        return launched(hexk::rotary_zero(dwq, dwk, D, st));
+    if ((rc = ptrs_ok({pos, freq, axis, dqo, dko, dq, dk}, {})) != HEX_OK)
+        return rc;
+    if (norm && (q == nullptr || k == nullptr || ws == nullptr ||
+                 ws_bytes < hexrotary_bwd_workspace(T, Hq, Hkv, D, dt)))
+        return HEX_ERR_INVALID_ARG;
+    const hexk::RotaryArgs a{pos, freq, axis, T,  ldq, ldk, 0, lddqo, lddko,
+                             0,   lddq, lddk, Hq, Hkv, D,   A, 0,     eps,
+                             norm};
+    return launched(hexk::rotary_bwd(q, k, wq, wk, dqo, dko, dq, dk, dwq, dwk,
+                                     static_cast<float *>(ws), a, static_cast<Dtype>(dt), st));
+}
+
+int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse,
+                const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, int S,
+                int Tq, int Tk, int Hq, int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv,
+                int64_t ldo, float scale, int flags, hex_dtype dt, void *stream)
+{
+    int rc = check_attn(S, Tq, Tk, Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 || !stride_ok(ldq, Hq, D, dt) ||
+        !stride_ok(ldo, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt))
+        return HEX_ERR_INVALID_ARG;
+    if (S == 0 || Tq == 0)
+        return HEX_OK;
+    if ((rc = ptrs_ok({q, o}, {k, v, lse})) != HEX_OK)
+        return rc;
+    if (q_start == nullptr || k_start == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
+        return HEX_ERR_INVALID_ARG;
+    const hexk::AttnArgs a = attn_args(q_start, k_start, k_len, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo,
+                                 scale, (flags & HEX_ATTN_CAUSAL) != 0);
+    return launched(hexk::attn_fwd(q, k, v, o, lse, a, static_cast<Dtype>(dt),
+                                   static_cast<hipStream_t>(stream)));
+}
+
+size_t hexattn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, hex_dtype dt)
+{
+    if (check_attn(S, Tq, Tk, Hq, Hkv, D, dt) != HEX_OK)
+        return 0;
+    return static_cast<size_t>(Tq) * Hq * sizeof(float);
+}
+
+int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
+                const void *dout, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes,
+                const int32_t *q_start, const int32_t *k_start, int S, int Tq, int Tk, int Hq,
+                int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, int64_t lddout,
+                int64_t lddq, int64_t lddk, int64_t lddv, float scale, int flags, hex_dtype dt,
+                void *stream)
+{
+    int rc = check_attn(S, Tq, Tk, Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 || !stride_ok(ldq, Hq, D, dt) ||
+        !stride_ok(ldo, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt) ||
+        !stride_ok(lddout, Hq, D, dt) || !stride_ok(lddq, Hq, D, dt) ||
+        !stride_ok(lddk, Hkv, D, dt) || !stride_ok(lddv, Hkv, D, dt))
+        return HEX_ERR_INVALID_ARG;
+    if (S == 0 || (Tq == 0 && Tk == 0))
+        return HEX_OK;
+    if ((rc = ptrs_ok({}, {q, k, v, o, lse, dout, dq, dk, dv, ws})) != HEX_OK)
+        return rc;
+    if (q_start == nullptr || k_start == nullptr)
+        return HEX_ERR_INVALID_ARG;
+    if (Tq > 0 && (q == nullptr || o == nullptr || lse == nullptr || dout == nullptr ||
+                   dq == nullptr || ws == nullptr ||
+                   ws_bytes < hexattn_bwd_workspace(Tq, Tk, S, Hq, Hkv, D, dt)))
+        return HEX_ERR_INVALID_ARG;
+    if (Tk > 0 && (k == nullptr || v == nullptr || dk == nullptr || dv == nullptr))
+        return HEX_ERR_INVALID_ARG;
+    const hexk::AttnArgs a = attn_args(q_start, k_start, nullptr, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv,
+                                 ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0);
+    return launched(hexk::attn_bwd(q, k, v, o, lse, dout, dq, dk, dv, static_cast<float *>(ws), a,
+                                   hexk::AttnGrads{lddout, lddq, lddk, lddv},
+                                   static_cast<Dtype>(dt), static_cast<hipStream_t>(stream)));
+}
+
+size_t hexattn_step_workspace(int S, int n, int Hq, int Hkv, int D, int max_len, hex_dtype dt)
+{
+    if (S < 1 || n < 1 || max_len < 0 || check_heads(Hq, Hkv, D, dt) != HEX_OK)
+        return 0;
+    return hexk::step_workspace(hexk::step_plan(S, n, Hq, Hkv, max_len), D);
+}
+
+int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws, size_t ws_bytes,
+                 const int32_t *k_start, const int32_t *k_len, int S, int n, int Hq, int Hkv,
+                 int D, int Tk, int max_len, int64_t ldk, int64_t ldv, float scale, hex_dtype dt,
+                 void *stream)
+{
+    if (S < 0 || n < 1 || Tk < 0 || max_len < 0 || !(scale >= 0.f) || !isfinite(scale))
+        return HEX_ERR_INVALID_ARG;
+    int rc = check_heads(Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt))
+        return HEX_ERR_INVALID_ARG;
+    if (S == 0)
+        return HEX_OK;
+    if ((rc = ptrs_ok({q, o}, {k, v, ws})) != HEX_OK)
+        return rc;
+    if (k_start == nullptr || k_len == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
+        return HEX_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(S) * n > kMaxRows / Hq || Tk > kMaxKeys || max_len > kMaxKeys)
+        return HEX_ERR_UNSUPPORTED;
+    const hexk::StepPlan p = hexk::step_plan(S, n, Hq, Hkv, max_len);
+    if (static_cast<int64_t>(S) * Hkv * p.row_tiles > kMaxBlocks / p.splits ||
+        p.rows * (D / 4) / 256 > kMaxBlocks)
+        return HEX_ERR_UNSUPPORTED;
+    const size_t need = hexk::step_workspace(p, D);
+    if (ws_bytes < need || (need > 0 && ws == nullptr))
+        return HEX_ERR_INVALID_ARG;
+    hexk::AttnArgs a = attn_args(nullptr, k_start, k_len, S, 0, Tk, Hq, Hkv, D, 0, ldk, ldv, 0, scale,
+                           true);
+    a.max_len = max_len;
+    return launched(hexk::attn_step(q, k, v, o, ws, a, p, static_cast<Dtype>(dt),
+                                    static_cast<hipStream_t>(stream)));
+}
+
+int hexdropout(const void *x, const void *res, void *y, int64_t n, double p, const uint64_t *rng,
+               uint64_t call, hex_dtype dt, void *stream)
+{
+    if (n < 0 || !(p >= 0.0 && p < 1.0) || !dtype_ok(dt))
+        return HEX_ERR_INVALID_ARG;
+    if (n == 0)
+        return HEX_OK;
+    if (n / 2048 > kMaxBlocks - 1)
+        return HEX_ERR_UNSUPPORTED;
+    const int rc = ptrs_ok({x, y}, {res});
+    if (rc != HEX_OK)
+        return rc;
+    if (rng == nullptr || (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
+        return HEX_ERR_INVALID_ARG;
+    return launched(hexk::dropout(x, res, y, n, p, rng, call, static_cast<Dtype>(dt),
+                                  static_cast<hipStream_t>(stream)));
 }
 
 int hexconv_timing_begin(void)

@@ -1,0 +1,134 @@
+// k_dropout.hip -- dropout with bits from a counter-based generator, and a
+// residual added.
+//
+//   y_e = res_e + (bits_e >= floor(p 2^32) ? x_e / (1 - p) : 0)
+//
+// bits_e is word e mod 4 of Philox 4x32 with ten rounds (Salmon, Moraes, Dror
+// and Shaw, SC 2011) for the counter (e / 4, call) and the seed as key: the
+// mask is a function of the element's number, so the backward makes it again
+// and nothing is stored.  Bound by memory: a thread takes eight elements, one
+// or two 16-byte loads an input; two generator calls (40 32 x 32 -> 64 bit
+// products) take less than their loads.
+#include "hexdev.h"
+#include "kernels.h"
+
+namespace hexk {
+namespace {
+
+struct Words {
+    uint32_t w[4];
+};
+
+__device__ __forceinline__ Words philox(uint64_t block, uint64_t call, uint64_t seed)
+{
+    uint32_t x0 = static_cast<uint32_t>(block), x1 = static_cast<uint32_t>(block >> 32);
+    uint32_t x2 = static_cast<uint32_t>(call), x3 = static_cast<uint32_t>(call >> 32);
+    uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = static_cast<uint64_t>(x0) * 0xD2511F53u;
+        const uint64_t b = static_cast<uint64_t>(x2) * 0xCD9E8D57u;
+        const uint32_t y0 = static_cast<uint32_t>(b >> 32) ^ x1 ^ k0;
+        const uint32_t y2 = static_cast<uint32_t>(a >> 32) ^ x3 ^ k1;
+        x1 = static_cast<uint32_t>(b);
+        x3 = static_cast<uint32_t>(a);
+        x0 = y0;
+        x2 = y2;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return Words{{x0, x1, x2, x3}};
+}
+
+template <typename E> __device__ __forceinline__ void load8(const E *p, float (&x)[8])
+{
+    if constexpr (sizeof(E) == 2) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 u = reinterpret_cast<const float4 *>(p)[i];
+            x[4 * i] = u.x, x[4 * i + 1] = u.y, x[4 * i + 2] = u.z, x[4 * i + 3] = u.w;
+        }
+    }
+}
+template <typename E> __device__ __forceinline__ void save8(E *p, const float (&x)[8])
+{
+    if constexpr (sizeof(E) == 2) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = from_f<bf16raw>(x[2 * i]) |
+                   static_cast<uint32_t>(from_f<bf16raw>(x[2 * i + 1])) << 16;
+        *reinterpret_cast<uint4 *>(p) = uint4{w[0], w[1], w[2], w[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            reinterpret_cast<float4 *>(p)[i] =
+                float4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void dropout_k(const E *x, const E *res, E *y, int64_t n,
+                                                 uint32_t least, float f, const uint64_t *rng,
+                                                 uint64_t call)
+{
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    if (at >= n)
+        return;
+    const bool whole = at + 8 <= n;
+    float v[8] = {}, s[8] = {};
+    if (whole) {
+        load8(x + at, v);
+        if (res != nullptr)
+            load8(res + at, s);
+    } else {
+        for (int i = 0; i < static_cast<int>(n - at); ++i) {
+            v[i] = to_f(x[at + i]);
+            if (res != nullptr)
+                s[i] = to_f(res[at + i]);
+        }
+    }
+    const uint64_t seed = rng[0], c = rng[1] + call;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const Words w = philox(static_cast<uint64_t>(at / 4 + b), c, seed);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float kept = w.w[i] >= least ? v[4 * b + i] * f : 0.f;
+            v[4 * b + i] = res != nullptr ? kept + s[4 * b + i] : kept;
+        }
+    }
+    if (whole)
+        save8(y + at, v);
+    else
+        for (int i = 0; i < static_cast<int>(n - at); ++i)
+            y[at + i] = from_f<E>(v[i]);
+}
+
+} // namespace
+
+hipError_t dropout(const void *x, const void *res, void *y, int64_t n, double p,
+                   const uint64_t *rng, uint64_t call, Dtype dt, hipStream_t st)
+{
+    const uint32_t least = static_cast<uint32_t>(p * 4294967296.0);
+    const float f = static_cast<float>(1.0 / (1.0 - p));
+    const dim3 grid(static_cast<uint32_t>((n + 2047) / 2048));
+    if (dt == F32)
+        HEX_LAUNCH((dropout_k<float>), grid, dim3(256), 0, st, static_cast<const float *>(x),
+                   static_cast<const float *>(res), static_cast<float *>(y), n, least, f, rng, call);
+    else
+        HEX_LAUNCH((dropout_k<bf16raw>), grid, dim3(256), 0, st, static_cast<const bf16raw *>(x),
+                   static_cast<const bf16raw *>(res), static_cast<bf16raw *>(y), n, least, f, rng,
+                   call);
+    return hipGetLastError();
+}
+
+} // namespace hexk

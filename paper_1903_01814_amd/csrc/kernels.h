@@ -243,4 +243,82 @@ bool wgrad_any_plan(const ConvShape &sh, Dtype d, WAnyPlan &pl);
 hipError_t wgrad_any(const void *x, const void *dy, float *dw, float *db, void *ws,
                      const ConvShape &sh, Dtype d, const WAnyPlan &pl, hipStream_t st);
 
+// ---- attention over packed sequences ------------------------------------
+
+// Query heads that share a key head, and the reciprocal that divides by their
+// number: floor(2^32 / G) (2^32 - 1 for G = 1) times r, shifted down, is r / G
+// or one less for every r < 2^31.
+struct Group {
+    int G;
+    uint32_t inv;
+};
+inline Group make_group(int G)
+{
+    return {G, G == 1 ? 0xffffffffu : static_cast<uint32_t>((1ull << 32) / G)};
+}
+
+// One call: token strides in elements, scale log2(e) = c + c_lo.
+struct AttnArgs {
+    const int32_t *q_start, *k_start, *k_len;
+    int S, Tq, Tk, Hq, Hkv, D;
+    Group group;
+    int64_t ldq, ldk, ldv, ldo;
+    float scale, c, c_lo;
+    bool causal;
+    int slots;   // tiles of rows handed out per key head (set by the launcher)
+    int max_len; // longest sequence of keys taken
+};
+
+// strides of the gradients
+struct AttnGrads {
+    int64_t lddo, lddq, lddk, lddv;
+};
+
+hipError_t attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse,
+                    const AttnArgs &a, Dtype dt, hipStream_t st);
+
+// delta: a float per query row [Tq][Hq], written by the first kernel and read
+// by the second; k_len is not used (a key belongs to one sequence)
+hipError_t attn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
+                    const void *dout, void *dq, void *dk, void *dv, float *delta,
+                    const AttnArgs &a, const AttnGrads &gr, Dtype dt, hipStream_t st);
+
+// New tokens over a cache: runs of `chunk` keys, `splits` of them at most,
+// row_tiles tiles of 32 rows; rows = S n Hq in all.
+struct StepPlan {
+    int n, row_tiles, splits, chunk;
+    int64_t rows;
+};
+StepPlan step_plan(int S, int n, int Hq, int Hkv, int max_len);
+size_t step_workspace(const StepPlan &p, int D);
+hipError_t attn_step(const void *q, const void *k, const void *v, void *o, void *ws,
+                     const AttnArgs &a, const StepPlan &pl, Dtype dt, hipStream_t st);
+
+// ---- norm and rotation of heads -----------------------------------------
+// Token strides in elements; in the backward ldqo and ldko are those of the
+// outputs' gradients.
+struct RotaryArgs {
+    const float *pos, *freq;
+    const int32_t *axis;
+    int64_t T, ldq, ldk, ldv, ldqo, ldko, ldvo, lddq, lddk;
+    int Hq, Hkv, D, A, n_slots;
+    float eps;
+    bool norm;
+};
+hipError_t rotary_fwd(const void *q, const void *k, const void *v, const void *wq, const void *wk,
+                      void *qo, void *ko, void *vo, const int32_t *slot, const RotaryArgs &a,
+                      Dtype dt, hipStream_t st);
+// part: rotary_bwd_blocks(T) * 2 * D floats
+int rotary_bwd_blocks(int64_t T);
+hipError_t rotary_bwd(const void *q, const void *k, const void *wq, const void *wk,
+                      const void *dqo, const void *dko, void *dq, void *dk, float *dwq, float *dwk,
+                      float *part, const RotaryArgs &a, Dtype dt, hipStream_t st);
+
+// dwq and dwk (where not null) := 0
+hipError_t rotary_zero(float *dwq, float *dwk, int D, hipStream_t st);
+
+// ---- dropout --------------------------------------------------------------
+hipError_t dropout(const void *x, const void *res, void *y, int64_t n, double p,
+                   const uint64_t *rng, uint64_t call, Dtype dt, hipStream_t st);
+
 } // namespace hexk

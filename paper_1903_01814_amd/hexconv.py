@@ -27,12 +27,18 @@ HEX_FLAG_RELU = 1
 HEX_MAX_K = 8
 HEX_MAX_STRIDE = 8
 HEX_MAX_KZ = 4
+HEX_ATTN_CAUSAL = 1
+HEX_ROTARY_NORM = 1
+HEX_ATTN_MAX_DIM = 128
+HEX_ROTARY_MAX_AXES = 8
 
 # (name, argtypes, restype) of every exported symbol
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _IP = ctypes.POINTER(ctypes.c_int)
 _S = ctypes.c_size_t
+_L = ctypes.c_int64
+_F = ctypes.c_float
 SIGNATURES = {
     "hex_num_taps": ([_I], _I),
     "hex_out_shape": ([_I, _I, _I, _I, _IP, _IP], _I),
@@ -58,6 +64,15 @@ SIGNATURES = {
     "hexconv3d_bwd_weight": ([_P, _P, _P, _P, _P, _S] + [_I] * 11 + [_P], _I),
     "hexpool3d_fwd": ([_P, _P, _P] + [_I] * 11 + [_P], _I),
     "hexpool3d_bwd": ([_P, _P, _P, _P] + [_I] * 11 + [_P], _I),
+    "hexrotary_fwd": ([_P] * 12 + [_I] * 5 + [_L] * 6 + [_I, _F, _I, _I, _P], _I),
+    "hexrotary_bwd_workspace": ([_I] * 5, _S),
+    "hexrotary_bwd": ([_P] * 14 + [_S] + [_I] * 5 + [_L] * 6 + [_F, _I, _I, _P], _I),
+    "hexattn_fwd": ([_P] * 8 + [_I] * 6 + [_L] * 4 + [_F, _I, _I, _P], _I),
+    "hexattn_bwd_workspace": ([_I] * 7, _S),
+    "hexattn_bwd": ([_P] * 10 + [_S] + [_P] * 2 + [_I] * 6 + [_L] * 8 + [_F, _I, _I, _P], _I),
+    "hexattn_step_workspace": ([_I] * 7, _S),
+    "hexattn_step": ([_P] * 5 + [_S] + [_P] * 2 + [_I] * 7 + [_L] * 2 + [_F, _I, _P], _I),
+    "hexdropout": ([_P] * 3 + [_L, ctypes.c_double, _P, ctypes.c_uint64, _I, _P], _I),
     "hexconv_timing_begin": ([], _I),
     "hexconv_timing_end": ([_I, ctypes.c_char_p, _IP, ctypes.POINTER(ctypes.c_double), _IP],
                            _I),
@@ -446,3 +461,174 @@ def hexpool3d_bwd(dy, argmax, relu_y, dx, k: int, kz: int, stride: int, stride_z
         N, C, D, H, W, k, kz, stride, stride_z, mode, dt, _stream(stream))
     _ok("hexpool3d_bwd", rc)
     return dx
+
+
+# --------------------------------------- attention over packed sequences
+
+def _tokens(t, name, dt, heads=None, D=None, n=None):
+    """Pointer and token stride of [tokens][heads][D] with dense heads."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("hexconv: %s must be a device tensor" % name)
+    if _dtype_code(t) != dt:
+        raise TypeError("hexconv: %s has dtype %s" % (name, t.dtype))
+    want = (n, heads, D)
+    if t.dim() != 3 or any(w is not None and w != g for w, g in zip(want, t.shape)):
+        raise ValueError("hexconv: %s has shape %s, expected [%s][%s][%s]"
+                         % ((name, tuple(t.shape)) + tuple("n" if w is None else w for w in want)))
+    h, d = t.shape[1:]
+    if t.numel() and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+        raise ValueError("hexconv: the heads of %s must be dense" % name)
+    # one token, or none: any stride does
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else h * d
+
+
+def _ints(t, name, shape):
+    """Pointer of an int32 device tensor; None passes through."""
+    if t is not None and t.dtype != _torch().int32:
+        raise TypeError("hexconv: %s must be int32" % name)
+    return _dev(t, name, None, shape)
+
+
+def _f32(t, name, shape):
+    if t is not None and t.dtype != _torch().float32:
+        raise TypeError("hexconv: %s must be float32" % name)
+    return _dev(t, name, None, shape)
+
+
+def _ws(ws):
+    return _dev(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def hexrotary_fwd(q, k, pos, freq, axis, wq, wk, qo, ko, eps: float = 1e-6, norm: bool = True,
+                  v=None, vo=None, slot=None, stream=None):
+    """qo, ko <- norm and rotation of the heads of q [T][Hq][D] and k
+    [T][Hkv][D] by positions pos [T][A]; with slot (int32 [T]) the keys, and
+    with v and vo the values, go to those rows of ko and vo."""
+    T, Hq, D = q.shape
+    Hkv, A = k.shape[1], pos.shape[1]
+    dt = _dtype_code(q)
+    n = T if slot is None else ko.shape[0]
+    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt), _tokens(k, "k", dt, Hkv, D, T)
+    (pv, ldv), (pvo, ldvo) = _tokens(v, "v", dt, Hkv, D, T), _tokens(vo, "vo", dt, Hkv, D, n)
+    (pqo, ldqo), (pko, ldko) = _tokens(qo, "qo", dt, Hq, D, T), _tokens(ko, "ko", dt, Hkv, D, n)
+    rc = load().hexrotary_fwd(
+        pq, pk, pv, _f32(pos, "pos", (T, A)), _f32(freq, "freq", (D // 2,)),
+        _ints(axis, "axis", (D // 2,)), _dev(wq, "wq", dt, (D,)), _dev(wk, "wk", dt, (D,)), pqo,
+        pko, pvo, _ints(slot, "slot", (T,)), T, Hq, Hkv, D, A, ldq, ldk, ldv, ldqo, ldko, ldvo, n,
+        eps, HEX_ROTARY_NORM if norm else 0, dt, _stream(stream))
+    _ok("hexrotary_fwd", rc)
+    return qo, ko
+
+
+def hexrotary_bwd_workspace(T, Hq, Hkv, D, dt):
+    return load().hexrotary_bwd_workspace(T, Hq, Hkv, D, dt)
+
+
+def hexrotary_bwd(q, k, pos, freq, axis, wq, wk, dqo, dko, dq, dk, dwq, dwk, ws,
+                  eps: float = 1e-6, norm: bool = True, stream=None):
+    """dq, dk and the float32 dwq, dwk (each may be None) <- gradients of
+    hexrotary_fwd.  Without the norm q and k may be None."""
+    T, Hq, D = dqo.shape
+    Hkv, A = dko.shape[1], pos.shape[1]
+    dt = _dtype_code(dqo)
+    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt, Hq, D, T), _tokens(k, "k", dt, Hkv, D, T)
+    (pgq, ldgq), (pgk, ldgk) = _tokens(dqo, "dqo", dt), _tokens(dko, "dko", dt, Hkv, D, T)
+    (pdq, lddq), (pdk, lddk) = _tokens(dq, "dq", dt, Hq, D, T), _tokens(dk, "dk", dt, Hkv, D, T)
+    rc = load().hexrotary_bwd(
+        pq, pk, _f32(pos, "pos", (T, A)), _f32(freq, "freq", (D // 2,)),
+        _ints(axis, "axis", (D // 2,)), _dev(wq, "wq", dt, (D,)), _dev(wk, "wk", dt, (D,)), pgq,
+        pgk, pdq, pdk, _f32(dwq, "dwq", (D,)), _f32(dwk, "dwk", (D,)), *_ws(ws), T, Hq, Hkv, D, A,
+        ldq, ldk, ldgq, ldgk, lddq, lddk, eps, HEX_ROTARY_NORM if norm else 0, dt,
+        _stream(stream))
+    _ok("hexrotary_bwd", rc)
+    return dq, dk, dwq, dwk
+
+
+def _scale(scale, D):
+    return D ** -0.5 if scale is None else scale
+
+
+def hexattn_fwd(q, k, v, o, lse, q_start, k_start=None, k_len=None, scale=None,
+                causal: bool = False, stream=None):
+    """o, lse (float32 [Tq][Hq], may be None) <- attention of the packed
+    queries q [Tq][Hq][D] over k and v [Tk][Hkv][D].  q_start: int32 [S+1];
+    k_start: the same for the keys (None: q_start), or int32 [S] with k_len.
+    scale: 1 / sqrt(D) by default."""
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[:2]
+    dt = _dtype_code(q)
+    S = q_start.shape[0] - 1
+    if k_start is None:
+        if k_len is not None:
+            raise ValueError("hexconv: k_len needs k_start")
+        k_start = q_start
+    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt), _tokens(k, "k", dt, Hkv, D)
+    (pv, ldv), (po, ldo) = _tokens(v, "v", dt, Hkv, D, Tk), _tokens(o, "o", dt, Hq, D, Tq)
+    rc = load().hexattn_fwd(
+        pq, pk, pv, po, _f32(lse, "lse", (Tq, Hq)), _ints(q_start, "q_start", (S + 1,)),
+        _ints(k_start, "k_start", (S + 1,) if k_len is None else (S,)),
+        _ints(k_len, "k_len", (S,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, _scale(scale, D),
+        HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
+    _ok("hexattn_fwd", rc)
+    return o, lse
+
+
+def hexattn_bwd_workspace(Tq, Tk, S, Hq, Hkv, D, dt):
+    return load().hexattn_bwd_workspace(Tq, Tk, S, Hq, Hkv, D, dt)
+
+
+def hexattn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, q_start, k_start=None, scale=None,
+                causal: bool = False, stream=None):
+    """dq, dk, dv <- gradients of hexattn_fwd from dout, o and lse."""
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[:2]
+    dt = _dtype_code(q)
+    S = q_start.shape[0] - 1
+    if k_start is None:
+        k_start = q_start
+    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt), _tokens(k, "k", dt, Hkv, D)
+    (pv, ldv), (po, ldo) = _tokens(v, "v", dt, Hkv, D, Tk), _tokens(o, "o", dt, Hq, D, Tq)
+    (pg, ldg), (pdq, lddq) = _tokens(dout, "dout", dt, Hq, D, Tq), _tokens(dq, "dq", dt, Hq, D, Tq)
+    (pdk, lddk), (pdv, lddv) = _tokens(dk, "dk", dt, Hkv, D, Tk), _tokens(dv, "dv", dt, Hkv, D, Tk)
+    rc = load().hexattn_bwd(
+        pq, pk, pv, po, _f32(lse, "lse", (Tq, Hq)), pg, pdq, pdk, pdv, *_ws(ws),
+        _ints(q_start, "q_start", (S + 1,)), _ints(k_start, "k_start", (S + 1,)), S, Tq, Tk, Hq,
+        Hkv, D, ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv, _scale(scale, D),
+        HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
+    _ok("hexattn_bwd", rc)
+    return dq, dk, dv
+
+
+def hexattn_step_workspace(S, n, Hq, Hkv, D, max_len, dt):
+    return load().hexattn_step_workspace(S, n, Hq, Hkv, D, max_len, dt)
+
+
+def hexattn_step(q, k, v, o, ws, k_start, k_len, max_len: int, scale=None, stream=None):
+    """o <- attention of n new tokens of every sequence, q [S][n][Hq][D],
+    over the k_len[s] cached tokens from k_start[s] on of k and v
+    [Tk][Hkv][D], at most max_len each."""
+    S, n, Hq, D = q.shape
+    Tk, Hkv = k.shape[:2]
+    dt = _dtype_code(q)
+    (pk, ldk), (pv, ldv) = _tokens(k, "k", dt, Hkv, D), _tokens(v, "v", dt, Hkv, D, Tk)
+    rc = load().hexattn_step(
+        _dev(q, "q", dt), pk, pv, _dev(o, "o", dt, (S, n, Hq, D)), *_ws(ws),
+        _ints(k_start, "k_start", (S,)), _ints(k_len, "k_len", (S,)), S, n, Hq, Hkv, D, Tk,
+        max_len, ldk, ldv, _scale(scale, D), dt, _stream(stream))
+    _ok("hexattn_step", rc)
+    return o
+
+
+def hexdropout(x, res, y, p: float, rng, call: int = 0, stream=None):
+    """y <- res (may be None) + dropout of x with probability p; rng: int64
+    device tensor [seed, call number]."""
+    dt = _dtype_code(x)
+    if rng.dtype != _torch().int64:
+        raise TypeError("hexconv: rng must be int64")
+    rc = load().hexdropout(_dev(x, "x", dt), _dev(res, "res", dt, x.shape),
+                           _dev(y, "y", dt, x.shape), x.numel(), p, _dev(rng, "rng", None, (2,)),
+                           call, dt, _stream(stream))
+    _ok("hexdropout", rc)
+    return y

@@ -1,0 +1,579 @@
+"""Attention over packed sequences, steps over a cache, norm and rotation, and
+dropout against float64, at the sizes and masks where they can go wrong:
+sequences of no and of one token, ragged tiles, several head layouts and
+sizes, rows that see no key, strided parts of one tensor, caches with NaN
+outside their tokens, offsets past 2^31 elements, other streams and graphs.
+
+Tolerances, in units of the sum of an element's terms' magnitudes: bfloat16
+rounds a probability (or its gradient) to 2^-9 of itself, o to 2^-9 before the
+gradients use it, and the result to 2^-9: 1e-2 holds all of it.  float32 adds
+up to 128 products of a score (128 2^-24 = 7.6e-6 if every rounding went one
+way) and 1e-6 for exponents up to 16: 1e-5."""
+import math
+
+import numpy as np
+import pytest
+
+import attn_ref as ref
+from gpu_helpers import tdtype, torch_mod
+from paper_1903_01814_amd import hexconv as hx
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TOL = {"f32": 1e-5, "bf16": 1e-2}
+
+
+def normal(g, *shape, dt="f32", std=1.0, mean=0.0):
+    """float64 values exact in dt, and the device tensor of them."""
+    t = (torch.randn(shape, generator=g) * std + mean).to(tdtype(dt))
+    return t.double(), t.cuda()
+
+
+def nan(*shape, dt="f32"):
+    return torch.full(shape, float("nan"), dtype=tdtype(dt), device="cuda")
+
+
+def ints(a):
+    return torch.tensor(a, dtype=torch.int32, device="cuda")
+
+
+def starts(lens):
+    return [0] + np.cumsum(lens).tolist()
+
+
+def near(got, want, mag, tol, what):
+    got = got.double().cpu()
+    assert torch.isfinite(got).all(), what + ": not finite"
+    err, lim = (got - want).abs(), tol * mag
+    bad = err > lim
+    assert not bad.any(), "%s: %d of %d off, worst %.3g of its limit" % (
+        what, int(bad.sum()), got.numel(), float((err / lim.clamp_min(1e-300)).max()))
+
+
+def near_lse(got, want, dt, what):
+    """-inf where no key is seen; else the scores' own error."""
+    got = got.double().cpu()
+    none = want == -math.inf
+    assert torch.equal(got == -math.inf, none), what + ": rows without keys"
+    err = (got - want)[~none].abs()
+    assert (err <= 1e-5 * (1 + want[~none].abs())).all(), "%s: lse off by %.3g" % (
+        what, float(err.max()))
+
+
+def run_attention(lq, lk, Hq, Hkv, D, dt, causal, seed, scale=None, apart=False):
+    """Forward and backward; queries, keys and values parts of one tensor where
+    lk is None, else of two.  apart: the parts' heads differ in size from the
+    tensor's token stride even more."""
+    g = torch.Generator().manual_seed(seed)
+    Tq, Tk = sum(lq), sum(lq if lk is None else lk)
+    pad = 2 if apart else 0
+    if lk is None:
+        qkv64, qkv = normal(g, Tq, Hq + 2 * Hkv + pad, D, dt=dt)
+        cut = lambda t: (t[:, :Hq], t[:, Hq:Hq + Hkv], t[:, Hq + Hkv:Hq + 2 * Hkv])
+        (q64, k64, v64), (q, k, v) = cut(qkv64), cut(qkv)
+        grads = nan(Tq, Hq + 2 * Hkv + pad, D, dt=dt)
+        dq, dk, dv = cut(grads)
+    else:
+        q64, q = normal(g, Tq, Hq, D, dt=dt)
+        kv64, kv = normal(g, Tk, 2 * Hkv, D, dt=dt)
+        k64, v64, k, v = kv64[:, :Hkv], kv64[:, Hkv:], kv[:, :Hkv], kv[:, Hkv:]
+        dq, grads = nan(Tq, Hq, D, dt=dt), nan(Tk, 2 * Hkv, D, dt=dt)
+        dk, dv = grads[:, :Hkv], grads[:, Hkv:]
+    do64, do = normal(g, Tq, Hq, D, dt=dt)
+    qs, ks = starts(lq), starts(lq if lk is None else lk)
+    spans = [(qs[i], lq[i], ks[i], ks[i + 1] - ks[i]) for i in range(len(lq))]
+    want = ref.attention(q64, k64, v64, spans, D ** -0.5 if scale is None else scale, causal, do64)
+    o, lse = nan(Tq, Hq, D, dt=dt), nan(Tq, Hq)
+    qd, kd = ints(qs), None if lk is None else ints(ks)
+    hx.hexattn_fwd(q, k, v, o, lse, qd, kd, scale=scale, causal=causal)
+    nb = hx.hexattn_bwd_workspace(Tq, Tk, len(lq), Hq, Hkv, D, hx._dtype_code(q))
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda") if nb else None
+    hx.hexattn_bwd(q, k, v, o, lse, do, dq, dk, dv, ws, qd, kd, scale=scale, causal=causal)
+    torch.cuda.synchronize()
+    got = {"o": o, "dq": dq, "dk": dk, "dv": dv}
+    near_lse(lse, want["lse"], dt, "lse")
+    for n in got:
+        near(got[n], want[n], want[n + "_mag"], TOL[dt], n)
+    if pad and lk is None:
+        assert torch.isnan(grads[:, Hq + 2 * Hkv:]).all(), "wrote between the parts"
+    return got
+
+
+LENS = [
+    [1], [2, 1, 0, 3], [31, 32, 33], [64, 0, 0, 65, 63], [127, 128, 129, 1], [300, 5, 0, 77],
+]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [(4, 4, 32), (6, 2, 40), (4, 1, 64), (2, 2, 80), (8, 2, 96),
+                                   (5, 1, 128), (3, 3, 8)])
+@pytest.mark.parametrize("lens", LENS, ids=lambda l: "-".join(map(str, l)))
+def test_attention_packed(lens, heads, dt, causal):
+    torch_mod()
+    run_attention(lens, None, *heads, dt, causal, 11 + sum(lens) + sum(heads), apart=True)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("lq,lk", [
+    ([5, 40, 3], [70, 0, 200]),       # a sequence without keys
+    ([50, 7, 130], [20, 7, 64]),      # causal: rows that see no key
+    ([0, 9], [33, 9]),                # keys that no row sees
+    ([1, 1, 1], [1, 129, 257]),
+])
+def test_attention_of_other_lengths(lq, lk, dt, causal):
+    torch_mod()
+    run_attention(lq, lk, 4, 2, 64, dt, causal, 5)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_attention_long(dt, D):
+    """Many tiles, many sequences of one token among long ones; every head
+    layout's rows and keys cross tile borders."""
+    torch_mod()
+    run_attention([700, 1, 1, 1, 515], None, 6, 2, D, dt, True, 3)
+    run_attention([1] * 70 + [640], None, 2, 1, D, dt, False, 4)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0.0, 0.01, 3.0])
+def test_attention_scales(dt, scale):
+    """Scores all equal, nearly equal, and so large that one key takes all."""
+    torch_mod()
+    run_attention([90, 33], None, 4, 2, 64, dt, True, 8, scale=scale)
+
+
+def test_attention_rising_scores():
+    """Scores that rise by hundreds from key to key: the running maximum
+    moves in every tile and old sums vanish."""
+    torch_mod()
+    g = torch.Generator().manual_seed(1)
+    n, D = 400, 32
+    q64 = torch.ones(n, 1, D, dtype=torch.float64)
+    k64 = (torch.arange(n, dtype=torch.float64) * 2)[:, None, None].expand(n, 1, D).contiguous()
+    v64, v = normal(g, n, 1, D)
+    want = ref.attention(q64, k64, v64, [(0, n, 0, n)], 1.0, True)
+    o, lse = nan(n, 1, D), nan(n, 1)
+    hx.hexattn_fwd(q64.float().cuda(), k64.float().cuda(), v, o, lse, ints([0, n]), scale=1.0,
+                   causal=True)
+    near(o, want["o"], want["o_mag"], 1e-5, "o")
+    near_lse(lse, want["lse"], "f32", "lse")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_gradients_against_differences(dt):
+    """<gradient, u> against the central difference of the float64 loss along
+    u, for the three inputs.  Its step's error is (1e-4)^2 of the loss's third
+    derivative; the limit is the elements' own, added up."""
+    torch_mod()
+    lens, Hq, Hkv, D = [37, 70], 4, 2, 32
+    g = torch.Generator().manual_seed(21)
+    T = sum(lens)
+    q64, q = normal(g, T, Hq, D, dt=dt)
+    k64, k = normal(g, T, Hkv, D, dt=dt)
+    v64, v = normal(g, T, Hkv, D, dt=dt)
+    do64, do = normal(g, T, Hq, D, dt=dt)
+    s = starts(lens)
+    spans = [(s[i], lens[i], s[i], lens[i]) for i in range(2)]
+    o, lse = nan(T, Hq, D, dt=dt), nan(T, Hq)
+    grads = [nan(*t.shape, dt=dt) for t in (q, k, v)]
+    ws = torch.empty(hx.hexattn_bwd_workspace(T, T, 2, Hq, Hkv, D, hx._dtype_code(q)),
+                     dtype=torch.uint8, device="cuda")
+    hx.hexattn_fwd(q, k, v, o, lse, ints(s), causal=True)
+    hx.hexattn_bwd(q, k, v, o, lse, do, *grads, ws, ints(s), causal=True)
+    full = ref.attention(q64, k64, v64, spans, D ** -0.5, True, do64)
+    for at, name in enumerate(("dq", "dk", "dv")):
+        ins = [q64, k64, v64]
+        u = torch.randn(ins[at].shape, generator=g, dtype=torch.float64)
+        loss = []
+        for e in (1e-4, -1e-4):
+            moved = list(ins)
+            moved[at] = ins[at] + e * u
+            loss.append(float((ref.attention(*moved, spans, D ** -0.5, True)["o"] * do64).sum()))
+        got = float((grads[at].double().cpu() * u).sum())
+        lim = TOL[dt] * float((full[name + "_mag"] * u.abs()).sum()) + 1e-6
+        assert abs(got - (loss[0] - loss[1]) / 2e-4) <= lim, name
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attention_repeats_itself(dt):
+    """The same bits from every run: no sum depends on the order of blocks."""
+    torch_mod()
+    a, b = (run_attention([333, 90, 1], None, 8, 2, 64, dt, True, 77) for _ in range(2))
+    for n in a:
+        assert torch.equal(a[n], b[n]), n
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_over_cache(dt, causal):
+    """Keys in a cache of slots (k_start, k_len), NaN everywhere else, empty
+    and full slots, chunks of a prompt; rows outside the sequences stay."""
+    torch_mod()
+    g = torch.Generator().manual_seed(2)
+    Hq, Hkv, D, cap = 6, 2, 64, 150
+    ln, lk = [20, 1, 0, 64], [130, 150, 70, 0]
+    T = sum(ln)
+    q64, q = normal(g, T + 5, Hq, D, dt=dt)
+    kc64, kc = normal(g, 4 * cap, Hkv, D, dt=dt)
+    vc64, vc = normal(g, 4 * cap, Hkv, D, dt=dt)
+    at = [3 * cap, 0, 2 * cap, cap]
+    inside = torch.zeros(4 * cap, dtype=torch.bool)
+    for a, n in zip(at, lk):
+        inside[a:a + n] = True
+    for t in (kc, vc):
+        t[~inside.cuda()] = float("nan")
+    s = starts(ln)
+    spans = [(s[i], ln[i], at[i], lk[i]) for i in range(4)]
+    want = ref.attention(q64, kc64, vc64, spans, D ** -0.5, causal)
+    o = torch.full((T + 5, Hq, D), 7.0, dtype=tdtype(dt), device="cuda")
+    hx.hexattn_fwd(q, kc, vc, o, None, ints(s), ints(at), ints(lk), causal=causal)
+    near(o[:T], want["o"][:T], want["o_mag"][:T], TOL[dt], "o")
+    assert bool((o[T:] == 7).all())
+
+
+def run_step(lens, n, Hq, Hkv, D, dt, seed, cap=None, max_len=None, fill=float("nan")):
+    g = torch.Generator().manual_seed(seed)
+    S, cap = len(lens), cap or max(lens) + 3
+    q64, q = normal(g, S, n, Hq, D, dt=dt)
+    kv64, kv = normal(g, S * cap, 2 * Hkv, D, dt=dt)
+    at = [((i * 7 + 3) % S if S % 7 else S - 1 - i) * cap + 1 for i in range(S)]
+    inside = torch.zeros(S * cap, dtype=torch.bool)
+    for a, m in zip(at, lens):
+        inside[a:a + m] = True
+    kv[~inside.cuda()] = fill
+    spans = [(i * n, n, at[i], lens[i]) for i in range(S)]
+    want = ref.attention(q64.reshape(S * n, Hq, D), kv64[:, :Hkv], kv64[:, Hkv:], spans,
+                         D ** -0.5, True)
+    max_len = max_len or max(lens)
+    o = nan(S, n, Hq, D, dt=dt)
+    nb = hx.hexattn_step_workspace(S, n, Hq, Hkv, D, max_len, hx._dtype_code(q))
+    ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda") if nb else None
+    hx.hexattn_step(q, kv[:, :Hkv], kv[:, Hkv:], o, ws, ints(at), ints(lens), max_len)
+    near(o.reshape(S * n, Hq, D), want["o"], want["o_mag"], TOL[dt], "o")
+    return o
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [(4, 4, 32), (6, 2, 40), (8, 1, 64), (12, 2, 80), (16, 4, 128),
+                                   (4, 2, 96)])
+@pytest.mark.parametrize("lens,n", [([1], 1), ([0, 1, 33, 128, 500], 1), ([1, 2, 129, 300], 3),
+                                    ([40, 7, 260], 9), ([2000], 1), ([90] * 150, 2)],
+                         ids=["one", "ragged", "three", "nine", "long", "many"])
+def test_step(lens, n, heads, dt):
+    torch_mod()
+    run_step(lens, n, *heads, dt, 31 + n + sum(heads), cap=max(lens) + 5)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_step_many_rows(dt):
+    """More rows than a tile: new tokens times the group's heads past 32."""
+    torch_mod()
+    run_step([300, 45], 5, 16, 1, 64, dt, 6, cap=310)
+    run_step([0, 3, 77], 40, 3, 1, 32, dt, 7, cap=90)
+
+
+def test_step_bound_on_lengths():
+    """max_len far above the lengths: runs without keys are left out."""
+    torch_mod()
+    run_step([5, 700, 0], 1, 4, 2, 64, "bf16", 9, cap=705, max_len=40000)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_step_agrees_with_forward(dt):
+    """Token by token over a growing cache gives the causal forward's rows."""
+    torch_mod()
+    g = torch.Generator().manual_seed(12)
+    T, Hq, Hkv, D = 40, 4, 2, 32
+    q64, q = normal(g, T, Hq, D, dt=dt)
+    k64, k = normal(g, T, Hkv, D, dt=dt)
+    v64, v = normal(g, T, Hkv, D, dt=dt)
+    want = ref.attention(q64, k64, v64, [(0, T, 0, T)], D ** -0.5, True)
+    for t in range(T):
+        o = nan(1, 1, Hq, D, dt=dt)
+        nb = hx.hexattn_step_workspace(1, 1, Hq, Hkv, D, T, hx._dtype_code(q))
+        ws = torch.empty(max(nb, 1), dtype=torch.uint8, device="cuda")
+        hx.hexattn_step(q[t].view(1, 1, Hq, D), k, v, o, ws, ints([0]), ints([t + 1]), T)
+        near(o[0], want["o"][t:t + 1], want["o_mag"][t:t + 1], TOL[dt], "token %d" % t)
+
+
+def test_step_past_32_bits():
+    """A cache of more than 2^31 elements a tensor: the last slots' tokens."""
+    torch_mod()
+    g = torch.Generator().manual_seed(3)
+    Hq, Hkv, D, m = 4, 2, 128, 200
+    Tk = (1 << 31) // (Hkv * D) + 4096
+    kc = torch.empty((Tk, Hkv, D), dtype=torch.bfloat16, device="cuda")
+    vc = torch.empty_like(kc)
+    q64, q = normal(g, 2, 1, Hq, D, dt="bf16")
+    at = [Tk - 300, 10]
+    k64, k = normal(g, 2 * m, Hkv, D, dt="bf16")
+    v64, v = normal(g, 2 * m, Hkv, D, dt="bf16")
+    for i, a in enumerate(at):
+        kc[a:a + m], vc[a:a + m] = k[i * m:(i + 1) * m], v[i * m:(i + 1) * m]
+    want = ref.attention(q64.reshape(2, Hq, D), k64, v64, [(0, 1, 0, m), (1, 1, m, m)], D ** -0.5,
+                         True)
+    o = nan(2, 1, Hq, D, dt="bf16")
+    nb = hx.hexattn_step_workspace(2, 1, Hq, Hkv, D, m, hx.HEX_BF16)
+    ws = torch.empty(max(nb, 1), dtype=torch.uint8, device="cuda")
+    hx.hexattn_step(q, kc, vc, o, ws, ints(at), ints([m, m]), m)
+    near(o.view(2, Hq, D), want["o"], want["o_mag"], 1e-2, "step")
+    o2 = nan(2, Hq, D, dt="bf16")
+    hx.hexattn_fwd(q.view(2, Hq, D), kc, vc, o2, None, ints([0, 1, 2]), ints(at), ints([m, m]),
+                   causal=True)
+    near(o2, want["o"], want["o_mag"], 1e-2, "forward")
+    # keys written past 2^31 elements, and only there
+    slots = ints([Tk - 1, -1, Tk, Tk - 7])
+    pos = torch.zeros((4, 1), device="cuda")
+    f, ax = torch.zeros(D // 2, device="cuda"), ints([0] * (D // 2))
+    k4, q4 = normal(g, 4, Hkv, D, dt="bf16")[1], normal(g, 4, Hq, D, dt="bf16")[1]
+    before = kc[Tk - 6:Tk - 1].clone()
+    hx.hexrotary_fwd(q4, k4, pos, f, ax, None, None, torch.empty_like(q4), kc, norm=False, v=k4,
+                     vo=vc, slot=slots)
+    for t in (kc, vc):
+        assert torch.equal(t[Tk - 1], k4[0]) and torch.equal(t[Tk - 7], k4[3])
+    assert torch.equal(kc[Tk - 6:Tk - 1].view(torch.int16), before.view(torch.int16))
+
+
+def positions(g, T, A):
+    """Positions up to thousands, as time slices are, and fractions."""
+    return torch.rand((T, A), generator=g) * torch.tensor([4096.0, 50.0, 40.0, 3.0][:A])
+
+
+def frequencies(D, A):
+    n = D // 2
+    f = torch.tensor([1000.0 ** (-(j // A) / max(1, n // A)) for j in range(n)])
+    f[-1] = 0.0
+    axis = [j % A for j in range(n)]
+    if n > 3:
+        axis[2], axis[3] = -1, A  # no such axis: pairs left as they are
+    return f.float(), axis
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("T,Hq,Hkv,D,A", [(1, 1, 1, 8, 1), (7, 4, 2, 32, 3), (33, 6, 3, 40, 3),
+                                          (129, 5, 1, 64, 2), (50, 8, 8, 80, 4), (65, 4, 1, 96, 3),
+                                          (9000, 3, 1, 128, 3), (0, 2, 1, 16, 3)])
+def test_rotary(T, Hq, Hkv, D, A, norm, dt):
+    """Limits: float32 a few roundings and the angle's 1e-7: 2e-6 of the
+    magnitudes; bfloat16 2^-8 of the result besides.  The weights' gradients
+    are float32 sums."""
+    torch_mod()
+    g = torch.Generator().manual_seed(T + D)
+    qkv64, qkv = normal(g, T, Hq + 2 * Hkv, D, dt=dt)
+    q64, k64 = qkv64[:, :Hq], qkv64[:, Hq:Hq + Hkv]
+    q, k = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv]
+    (wq64, wq), (wk64, wk) = (normal(g, D, dt=dt, std=0.3, mean=1.0) for _ in range(2))
+    (gq64, gq), (gk64, gk) = normal(g, T, Hq, D, dt=dt), normal(g, T, Hkv, D, dt=dt)
+    pos = positions(g, T, A)
+    f, axis = frequencies(D, A)
+    args = (pos.cuda(), f.cuda(), ints(axis))
+    qo, ko = nan(T, Hq, D, dt=dt), nan(T, Hkv, D, dt=dt)
+    hx.hexrotary_fwd(q, k, *args, wq, wk, qo, ko, eps=1e-5, norm=norm)
+    d = nan(T, Hq + 2 * Hkv, D, dt=dt)
+    dq, dk = d[:, :Hq], d[:, Hq:Hq + Hkv]
+    dwq, dwk = (nan(D), nan(D)) if norm else (None, None)
+    nb = hx.hexrotary_bwd_workspace(T, Hq, Hkv, D, hx._dtype_code(q)) if norm else 0
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda") if nb else None
+    hx.hexrotary_bwd(q if norm else None, k if norm else None, *args, wq, wk, gq, gk, dq, dk, dwq,
+                     dwk, ws, eps=1e-5, norm=norm)
+    assert torch.isnan(d[:, Hq + Hkv:]).all()
+    for x, w, gy, got, dx, dw in ((q64, wq64, gq64, qo, dq, dwq), (k64, wk64, gk64, ko, dk, dwk)):
+        r = ref.rotary(x, w, pos, f, axis, 1e-5, norm, gy)
+        for t, a, b in ((got, r[0], r[1]), (dx, r[2], r[3])):
+            near(t, a, 2e-6 * b + (2.0 ** -8 * a.abs() if dt == "bf16" else 0), 1.0, "rows")
+        if norm:
+            near(dw, r[4], r[5], 1e-5, "weights")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rotary_gradients_against_differences(dt):
+    torch_mod()
+    T, H, D = 11, 2, 24
+    g = torch.Generator().manual_seed(4)
+    x64, x = normal(g, T, H, D, dt=dt)
+    w64, w = normal(g, D, dt=dt, std=0.3, mean=1.0)
+    y64, y = normal(g, T, H, D, dt=dt)
+    pos = positions(g, T, 3)
+    f, axis = frequencies(D, 3)
+    dx, dk = nan(T, H, D, dt=dt), nan(T, H, D, dt=dt)
+    dw, dwk = nan(D), nan(D)
+    ws = torch.empty(hx.hexrotary_bwd_workspace(T, H, H, D, hx._dtype_code(x)), dtype=torch.uint8,
+                     device="cuda")
+    hx.hexrotary_bwd(x, x, pos.cuda(), f.cuda(), ints(axis), w, w, y, y, dx, dk, dw, dwk, ws)
+    assert torch.equal(dx, dk) and torch.equal(dw, dwk)
+    full = ref.rotary(x64, w64, pos, f, axis, 1e-6, True, y64)
+    for got, at, mag in ((dx, 0, full[3]), (dw, 1, full[5])):
+        u = torch.randn((x64, w64)[at].shape, generator=g, dtype=torch.float64)
+        loss = []
+        for e in (1e-4, -1e-4):
+            moved = [x64, w64]
+            moved[at] = moved[at] + e * u
+            loss.append(float((ref.rotary(*moved, pos, f, axis, 1e-6, True)[0] * y64).sum()))
+        tol = 1e-5 if dt == "f32" or at == 1 else 2.0 ** -8
+        lim = tol * float((mag * u.abs()).sum()) + 1e-6
+        assert abs(float((got.double().cpu() * u).sum()) - (loss[0] - loss[1]) / 2e-4) <= lim
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rotary_into_cache(dt):
+    """Keys and values go to their slots, tokens without a slot nowhere, and
+    the rest of the caches stays as it is."""
+    torch_mod()
+    g = torch.Generator().manual_seed(14)
+    T, Hq, Hkv, D, n = 9, 4, 2, 64, 40
+    qkv64, qkv = normal(g, T, Hq + 2 * Hkv, D, dt=dt)
+    cut = lambda t: (t[:, :Hq], t[:, Hq:Hq + Hkv], t[:, Hq + Hkv:])
+    q, k, v = cut(qkv)
+    kv = nan(n, 2 * Hkv, D, dt=dt)
+    kc, vc = kv[:, :Hkv], kv[:, Hkv:]
+    slot = [3, 39, -1, 0, 17, 40, 18, 1 << 30, 21]
+    pos = positions(g, T, 3)
+    f, axis = frequencies(D, 3)
+    qo = nan(T, Hq, D, dt=dt)
+    w64, w = normal(g, D, dt=dt, std=0.3, mean=1.0)
+    hx.hexrotary_fwd(q, k, pos.cuda(), f.cuda(), ints(axis), None, w, qo, kc, v=v, vo=vc,
+                     slot=ints(slot))
+    ones = torch.ones(D, dtype=torch.float64)
+    want, mag = ref.rotary(cut(qkv64)[0], ones, pos, f, axis, 1e-6, True)
+    lim = lambda a, b: 2e-6 * b + (2.0 ** -8 * a.abs() if dt == "bf16" else 0)
+    near(qo, want, lim(want, mag), 1.0, "queries")
+    want, mag = ref.rotary(cut(qkv64)[1], w64, pos, f, axis, 1e-6, True)
+    used = []
+    for t, s in enumerate(slot):
+        if 0 <= s < n:
+            near(kc[s], want[t], lim(want[t], mag[t]), 1.0, "key %d" % t)
+            assert torch.equal(vc[s], v[t])
+            used.append(s)
+    rest = [i for i in range(n) if i not in used]
+    assert torch.isnan(kv[rest]).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 4, 7, 8, 9, 2047, 2048, 2049, 5001])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.999])
+def test_dropout(n, p, dt):
+    torch_mod()
+    g = torch.Generator().manual_seed(n)
+    x64, x = normal(g, n, dt=dt)
+    r64, r = normal(g, n, dt=dt)
+    seed, at, call = 0x123456789ABCDEF0 + n, (1 << 33) + 5, 3
+    rng = torch.tensor([seed, at], dtype=torch.int64, device="cuda")
+    bits = ref.philox(n, seed, at + call)
+    kept = torch.from_numpy(bits >= math.floor(p * 2 ** 32)).double() / (1 - p)
+    for res64, res in ((r64, r), (None, None)):
+        y = nan(n, dt=dt)
+        hx.hexdropout(x, res, y, p, rng, call)
+        a, b = x64 * kept, res64 if res is not None else torch.zeros_like(x64)
+        mag = a.abs() + b.abs()
+        near(y, a + b, mag, 2.0 ** -22 if dt == "f32" else 2.0 ** -8 + 2.0 ** -22, "y")
+        assert bool((y[(mag == 0).cuda()] == 0).all())
+
+
+def test_dropout_known_words():
+    """Philox 4x32-10 with key and counter 0: the generator's published words,
+    by the elements kept at thresholds on either side of them."""
+    torch_mod()
+    words = [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    assert ref.philox(4, 0, 0).tolist() == words
+    rng = torch.zeros(2, dtype=torch.int64, device="cuda")
+    x = torch.ones(4, device="cuda")
+    for i, w in enumerate(words):
+        for d, kept in ((0, True), (1, False)):
+            y = torch.empty_like(x)
+            hx.hexdropout(x, None, y, (w + d) / 2.0 ** 32, rng)
+            assert bool(y[i] != 0) == kept
+
+
+def test_calls_on_another_stream():
+    """Work enqueued on a side stream, whose inputs it makes itself."""
+    torch_mod()
+    g = torch.Generator().manual_seed(9)
+    T, H, D = 300, 4, 64
+    q64, q = normal(g, T, H, D, dt="bf16")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        q2 = (q.float() * 2).to(torch.bfloat16)
+        o = torch.empty_like(q)
+        hx.hexattn_fwd(q2, q2, q2, o, None, ints([0, 100, T]), causal=True)
+    side.synchronize()
+    want = ref.attention(2 * q64, 2 * q64, 2 * q64, [(0, 100, 0, 100), (100, 200, 100, 200)],
+                         D ** -0.5, True)
+    near(o, want["o"], want["o_mag"], 1e-2, "o")
+
+
+def test_graph_replays():
+    """Rotation, attention, its gradients, a step and dropout recorded once and
+    replayed with other inputs: every replay gives what eager calls give."""
+    torch_mod()
+    g = torch.Generator().manual_seed(19)
+    T, Hq, Hkv, D = 200, 4, 2, 64
+    start, lens = ints([0, 60, 61, T]), ints([60, 1, T - 61])
+    f, axis = frequencies(D, 3)
+    pos, f, axis = positions(g, T, 3).cuda(), f.cuda(), ints(axis)
+    qkv = torch.empty((T, Hq + 2 * Hkv, D), dtype=torch.bfloat16, device="cuda")
+    rng = torch.zeros(2, dtype=torch.int64, device="cuda")
+    dt = hx.HEX_BF16
+    ws = torch.empty(hx.hexattn_bwd_workspace(T, T, 3, Hq, Hkv, D, dt), dtype=torch.uint8,
+                     device="cuda")
+    ws2 = torch.empty(max(1, hx.hexattn_step_workspace(3, 1, Hq, Hkv, D, T, dt)),
+                      dtype=torch.uint8, device="cuda")
+    b16 = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+    qo, ko, o, y = b16(T, Hq, D), b16(T, Hkv, D), b16(T, Hq, D), b16(T, Hq, D)
+    lse, d, so = torch.empty((T, Hq), device="cuda"), b16(T, Hq + 2 * Hkv, D), b16(3, 1, Hq, D)
+
+    def work():
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        hx.hexrotary_fwd(q, k, pos, f, axis, None, None, qo, ko)
+        hx.hexattn_fwd(qo, ko, v, o, lse, start, causal=True)
+        hx.hexdropout(o, qo, y, 0.3, rng)
+        hx.hexattn_bwd(qo, ko, v, o, lse, y, d[:, :Hq], d[:, Hq:Hq + Hkv], d[:, Hq + Hkv:], ws,
+                       start, causal=True)
+        hx.hexattn_step(qo[:3].view(3, 1, Hq, D), ko, v, so, ws2, start[:3], lens, T)
+
+    outs = (qo, ko, o, lse, y, d, so)
+    qkv.normal_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for i in range(4):
+        qkv.normal_()
+        rng += 1
+        work()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b), "replay %d" % i
+
+
+def test_offsets_out_of_bounds():
+    """Offsets and lengths past the tensors are cut to them: results follow
+    the cut ones and nothing outside is read or written."""
+    torch_mod()
+    g = torch.Generator().manual_seed(23)
+    T, H, D = 50, 2, 32
+    q64, q = normal(g, T, H, D)
+    want = ref.attention(q64, q64, q64, [(0, 20, 0, 20), (20, 30, 20, 30)], D ** -0.5, False)
+    o = nan(T, H, D)
+    hx.hexattn_fwd(q, q, q, o, None, ints([-5, 20, 1 << 30]))
+    near(o, want["o"], want["o_mag"], 1e-5, "o")
+    o = nan(2, 1, H, D)
+    want = ref.attention(q64[:2], q64, q64, [(0, 1, 40, 10), (1, 1, 0, 0)], D ** -0.5, False)
+    nb = hx.hexattn_step_workspace(2, 1, H, H, D, T, hx.HEX_F32)
+    ws = torch.empty(max(nb, 1), dtype=torch.uint8, device="cuda")
+    hx.hexattn_step(q[:2].view(2, 1, H, D), q, q, o, ws, ints([40, 7]), ints([99, -3]), T)
+    near(o.view(2, H, D), want["o"], want["o_mag"], 1e-5, "step")

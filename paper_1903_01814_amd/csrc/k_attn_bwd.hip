@@ -21,7 +21,7 @@ namespace {
 // ---- dq: rows as in the forward, 32 NQ a wave, BK keys a tile.
 //   X^T = K Q^T and dP^T = V dO^T (keys as rows), dQ^T += K^T dS^T
 template <typename E, int DC, int NQ, int BK>
-__global__ __launch_bounds__(256) void attn_dq_k(const E *q, const E *k, const E *v, const E *o,
+__global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, const E *v, const E *o,
                                                  const float *lse, const E *dout, E *dq,
                                                  float *delta, AttnArgs a, AttnGrads gr)
 {
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void attn_dq_k(const E *q, const E *k, const E
 //   X = Q K^T and dP = dO V^T (query rows as rows; a lane holds one key),
 //   dV^T += dO^T P, dK^T += Q^T dS
 template <typename E, int DC, int BR>
-__global__ __launch_bounds__(256) void attn_dkv_k(const E *q, const E *k, const E *v,
+__global__ __launch_bounds__(256, 2) void attn_dkv_k(const E *q, const E *k, const E *v,
                                                   const float *lse, const E *dout,
                                                   const float *delta, E *dk, E *dv, AttnArgs a,
                                                   AttnGrads gr)
@@ -218,7 +218,10 @@ __global__ __launch_bounds__(256) void attn_dkv_k(const E *q, const E *k, const 
     constexpr int NCH = BR * TL::CPR / 256;
     static_assert(BR * TL::CPR % 256 == 0 && BR <= 64, "");
     constexpr int BUF = 2 * TB + 4 * BR * 4; // Q, dO; lse, delta, keys seen, lse's rest
-    __shared__ __align__(16) unsigned char smem[2 * BUF];
+    // the values' operands stay in registers where they fit beside the sums
+    constexpr bool VL = DT > 2;
+    __shared__ __align__(16) unsigned char smem[2 * BUF + (VL ? TL::bytes(128) : 0)];
+    unsigned char *vl = smem + 2 * BUF;
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = lane >> 5, col = lane & 31;
@@ -235,12 +238,21 @@ __global__ __launch_bounds__(256) void attn_dkv_k(const E *q, const E *k, const 
     const int rows = n * g.G, ahead = m - n;
 
     const int key = key0 + wave * 32 + col, kc = min(key, m - 1);
-    Frag kf[DS], vf[DS];
+    Frag kf[DS], vf[VL ? 1 : DS];
 #pragma unroll
     for (int s = 0; s < DS; ++s) {
         kf[s] = load_frag<E>(k + (sp.begin + kc) * a.ldk + kvh * a.D, 16 * s + 8 * h, a.D);
-        vf[s] = load_frag<E>(v + (sp.begin + kc) * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
+        if constexpr (!VL)
+            vf[s] = load_frag<E>(v + (sp.begin + kc) * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
     }
+    if constexpr (VL)
+        for (int e = threadIdx.x; e < 128 * TL::CPR; e += 256) {
+            const int c = e % TL::CPR * Elem<E>::VEC;
+            const int64_t r = sp.begin + min(key0 + e / TL::CPR, m - 1);
+            *reinterpret_cast<uint4 *>(vl + TL::chunk_at(e / TL::CPR, e % TL::CPR)) =
+                c < a.D ? *reinterpret_cast<const uint4 *>(v + r * a.ldv + kvh * a.D + c)
+                        : uint4{0, 0, 0, 0};
+        }
     // first row that sees a key of the block
     const int tile0 = a.causal ? static_cast<int>(static_cast<int64_t>(max(0, key0 - ahead)) * g.G / BR) : 0;
     const int ntiles = (rows + BR - 1) / BR;
@@ -324,7 +336,8 @@ __global__ __launch_bounds__(256) void attn_dkv_k(const E *q, const E *k, const 
 #pragma unroll
                 for (int s = 0; s < DS; ++s) {
                     x = add_product(TL::read_cols(qt, 32 * t + col, s, h), kf[s], x);
-                    dp = add_product(TL::read_cols(gt, 32 * t + col, s, h), vf[s], dp);
+                    const Frag vs = VL ? TL::read_cols(vl, wave * 32 + col, s, h) : vf[VL ? 0 : s];
+                    dp = add_product(TL::read_cols(gt, 32 * t + col, s, h), vs, dp);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -383,7 +396,7 @@ hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *l
                   hipStream_t st)
 {
     constexpr bool F32 = sizeof(E) == 4;
-    constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64, BR = !F32 && DC % 64 ? 64 : 32;
+    constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64, BR = !F32 && DC != 128 ? 64 : 32;
     AttnArgs b = a;
     a.slots = attn_slots(a.Tq, a.group.G, 128 * NQ, a.S);
     HEX_LAUNCH((attn_dq_k<E, DC, NQ, BK>), dim3(static_cast<uint32_t>(a.slots) * a.Hkv), dim3(256),

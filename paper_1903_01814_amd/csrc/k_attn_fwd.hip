@@ -26,7 +26,7 @@ constexpr float kSlack = 8.f; // in powers of two
 
 // NQ blocks of 32 rows a wave, BK keys a tile.
 template <typename E, int DC, int NQ, int BK>
-__global__ __launch_bounds__(256) void attn_fwd_k(const E *q, const E *k, const E *v, E *o,
+__global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, const E *v, E *o,
                                                   float *lse, AttnArgs a)
 {
     using TL = Tile<E, DC>;

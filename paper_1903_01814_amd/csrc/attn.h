@@ -143,56 +143,77 @@ template <typename E, int DC> struct Tile {
         return row * PITCH + ((chunk ^ swz(row)) << 4);
     }
 
-    // operand with the head dimension as contraction: row `row` (per lane),
-    // elements 16 s + 8 h ..
+    // Operand with the head dimension as contraction: row `row` (per lane),
+    // elements 16 s + 8 h ..  The lane's part of its address is made once
+    // (cols_at), a step changes it by an exclusive or, rows by an offset.
+    __device__ __forceinline__ static int cols_at(int row, int h)
+    {
+        return row * PITCH + (((sizeof(E) == 2 ? h : 2 * h) ^ swz(row)) << 4);
+    }
     __device__ __forceinline__ static typename Elem<E>::Frag read_cols(const unsigned char *t,
-                                                                       int row, int s, int h)
+                                                                       int at, int s)
     {
         if constexpr (sizeof(E) == 2) {
-            return *reinterpret_cast<const bf16x8 *>(t + chunk_at(row, 2 * s + h));
+            return *reinterpret_cast<const bf16x8 *>(t + (at ^ (s << 5)));
         } else {
             FragF32 f;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float4 u =
-                    *reinterpret_cast<const float4 *>(t + chunk_at(row, 4 * s + 2 * h + j));
+                const float4 u = *reinterpret_cast<const float4 *>(t + (at ^ (s << 6 | j << 4)));
                 f.v[4 * j] = u.x, f.v[4 * j + 1] = u.y, f.v[4 * j + 2] = u.z, f.v[4 * j + 3] = u.w;
             }
             return f;
         }
     }
 
-    // operand with rows as contraction, in the order of a result's registers:
-    // element i is row row0 + 8 (i / 4) + 4 h + i % 4, column 32 d + lane % 32.
-    // bfloat16: the transposing read (16 lanes read four rows of 16 columns,
-    // lane i of them receives column i of the four rows).
-    __device__ __forceinline__ static typename Elem<E>::Frag read_rows(unsigned char *t, int row0,
-                                                                       int d, int lane)
+    // Operand with rows as contraction, in the order of a result's registers:
+    // element i is row row0 + 8 (i / 4) + 4 h + i % 4 (row0 a multiple of 16),
+    // column 32 d + lane % 32.  bfloat16: the transposing read (16 lanes read
+    // four rows of 16 columns, lane i of them receives column i of the four
+    // rows).
+    struct RowsAt {
+        int a, b;
+    };
+    __device__ __forceinline__ static RowsAt rows_at(int lane)
     {
         const int h = lane >> 5;
         if constexpr (sizeof(E) == 2) {
+            const int r = 4 * h + ((lane & 15) >> 2);
+            const int c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), o = 8 * (lane & 1);
+            return RowsAt{chunk_at(r, c) + o, chunk_at(r + 8, c) + o};
+        } else {
+            return RowsAt{chunk_at(4 * h, (lane & 31) >> 2) + 4 * (lane & 3), 0};
+        }
+    }
+    __device__ __forceinline__ static typename Elem<E>::Frag read_rows(unsigned char *t, RowsAt at,
+                                                                       int row0, int d)
+    {
+        if constexpr (sizeof(E) == 2) {
             using lp = __attribute__((address_space(3))) shortx4 *;
-            const int r = row0 + 4 * h + ((lane & 15) >> 2);
-            const int c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const int o = 8 * (lane & 1);
-            const shortx4 lo =
-                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(t + chunk_at(r, c) + o));
-            const shortx4 hi =
-                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(t + chunk_at(r + 8, c) + o));
+            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lp)(t + row0 * PITCH + (at.a ^ (d << 6))));
+            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lp)(t + row0 * PITCH + (at.b ^ (d << 6))));
             return __builtin_bit_cast(bf16x8,
                                       __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
+            // the permutation of row 8 (i / 4) + 4 h + i % 4 is that of row 4 h
+            // and that of the rest, by exclusive or
             FragF32 f;
-            const int e = 32 * d + (lane & 31);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int r = row0 + 8 * (i >> 2) + 4 * h + (i & 3);
-                f.v[i] = *reinterpret_cast<const float *>(t + chunk_at(r, e >> 2) + 4 * (e & 3));
+                const int r = 8 * (i >> 2) + (i & 3);
+                f.v[i] = *reinterpret_cast<const float *>(t + (row0 + r) * PITCH +
+                                                          (at.a ^ (d << 7 | swz(r) << 4)));
             }
             return f;
         }
     }
 };
+
+// Keeps the compiler from making all of a loop's LDS addresses before the loop
+// and holding them in registers: they cost one exclusive or each.
+__device__ __forceinline__ void in_loop(int &v) { asm volatile("" : "+v"(v)); }
 
 // the sum, and the maximum, of a lane's value and lane ^ 32's: the swap gives
 // both lanes the lower half's value and the upper half's
@@ -293,6 +314,16 @@ __device__ __forceinline__ void store4(bf16raw *p, float x, float y, float z, fl
 {
     *reinterpret_cast<ushort4 *>(p) =
         ushort4{from_f<bf16raw>(x), from_f<bf16raw>(y), from_f<bf16raw>(z), from_f<bf16raw>(w)};
+}
+
+// registers 4 i .. 4 i + 3
+__device__ __forceinline__ float4 quad(const floatx16 &x, int i)
+{
+    return float4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+}
+__device__ __forceinline__ void add_quad(floatx16 &x, int i, const float4 &y)
+{
+    x[4 * i] += y.x, x[4 * i + 1] += y.y, x[4 * i + 2] += y.z, x[4 * i + 3] += y.w;
 }
 
 // one lane's results of a column: registers 4 i .. 4 i + 3 are elements

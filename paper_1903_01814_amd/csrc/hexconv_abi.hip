@@ -1060,7 +1060,7 @@ size_t hexattn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, hex_
 {
     if (check_attn(S, Tq, Tk, Hq, Hkv, D, dt) != HEX_OK)
         return 0;
-    return static_cast<size_t>(Tq) * Hq * sizeof(float);
+    return hexk::attn_bwd_workspace(Tq, Tk, S, Hq, Hkv, D, static_cast<Dtype>(dt));
 }
 
 int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
@@ -1085,15 +1085,15 @@ int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, cons
     if (q_start == nullptr || k_start == nullptr)
         return HEX_ERR_INVALID_ARG;
     if (Tq > 0 && (q == nullptr || o == nullptr || lse == nullptr || dout == nullptr ||
-                   dq == nullptr || ws == nullptr ||
-                   ws_bytes < hexattn_bwd_workspace(Tq, Tk, S, Hq, Hkv, D, dt)))
+                   dq == nullptr))
+        return HEX_ERR_INVALID_ARG;
+    if (ws == nullptr || ws_bytes < hexattn_bwd_workspace(Tq, Tk, S, Hq, Hkv, D, dt))
         return HEX_ERR_INVALID_ARG;
     if (Tk > 0 && (k == nullptr || v == nullptr || dk == nullptr || dv == nullptr))
         return HEX_ERR_INVALID_ARG;
     const hexk::AttnArgs a = attn_args(q_start, k_start, nullptr, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv,
                                  ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0);
-    return launched(hexk::attn_bwd(q, k, v, o, lse, dout, dq, dk, dv, static_cast<float *>(ws), a,
-                                   hexk::AttnGrads{lddout, lddq, lddk, lddv},
+    return launched(hexk::attn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, a, hexk::AttnGrads{lddout, lddq, lddk, lddv},
                                    static_cast<Dtype>(dt), static_cast<hipStream_t>(stream)));
 }
 

@@ -8,9 +8,9 @@
 // Two kernels, each with its sums in registers: attn_dq_k walks the keys for a
 // tile of rows (and computes D_i), attn_dkv_k the rows for a tile of keys,
 // with all query heads that share the key head among its rows.  The scores
-// and do . v are computed twice, 7 products in place of 5; in exchange
-// nothing is added through memory, every sum has one order and the result is
-// the same from run to run.
+// and do . v are computed twice, 7 products in place of 5; in exchange no sum
+// is added up by atomics, each has one order and the result is the same from
+// run to run.
 #include "attn.h"
 #include "kernels.h"
 
@@ -18,12 +18,219 @@ namespace hexk {
 namespace attn {
 namespace {
 
+// ---- how the keys' work is divided.  A tile of 128 keys of one sequence and
+// key head takes as many units as it has tiles of rows that see it, and kFixed
+// for its own loads and stores.  Causal, a sequence's first keys have the whole
+// sequence's rows and its last ones a few, and sequences differ: one block a
+// tile left the card idle behind the longest (24 sequences of 500 to 5000
+// tokens, 16 heads of 128 on 4: 455 TFLOP/s, against 762 where all are alike).
+// So a tile of more than a share, 1 / pl.shares of its head's units (a few
+// shares for each block that the card holds at once), is divided evenly among
+// its rows.  The list of the pieces, large ones first by classes of size, is
+// made by one block of the first kernel; the second's blocks take them off it
+// one after another.
+// The pieces of a divided tile leave their sums in the workspace, and a third
+// kernel adds them up in their order, so that the result does not depend on
+// which block took what.  (The last block to end as the one that adds, without
+// that kernel: its fences write back and drop a die's whole cache, 1904 -> 2282
+// us where many tiles are divided.)
+constexpr int kFixed = 4;
+constexpr int kShares = 3;  // shares of all heads for each block that the card holds
+constexpr int kClasses = 8; // of pieces by size
+constexpr int kLeast = 24; // units of a share at least: small tiles stay whole
+
+// one sequence's units: k i - a0 is the first row tile that sees key tile i
+struct KeyUnits {
+    int a0, k, nt, tiles; // nt row tiles, key tiles
+    int lo, hi;           // key tiles that all rows see, that any row sees
+    __device__ __forceinline__ int first(int i) const
+    {
+        const int64_t t = static_cast<int64_t>(k) * i - a0;
+        return static_cast<int>(t < 0 ? 0 : t < nt ? t : nt);
+    }
+    // units of the key tiles before j: nt each up to lo, nt + a0 - k i up to hi
+    __device__ __forceinline__ int64_t before(int j) const
+    {
+        const int64_t l = min(lo, j), h = max(min(hi, j), min(lo, j));
+        return l * nt + (h - l) * (static_cast<int64_t>(nt) + a0) -
+               k * ((l + h - 1) * (h - l) / 2) + static_cast<int64_t>(kFixed) * j;
+    }
+};
+
+__device__ __forceinline__ KeyUnits key_units(const AttnArgs &a, const KeyPlan &pl, int n, int m)
+{
+    KeyUnits u;
+    u.nt = (n * a.group.G + pl.row_tile - 1) / pl.row_tile;
+    u.tiles = (m + 127) / 128;
+    u.k = u.a0 = 0;
+    u.lo = u.hi = u.tiles;
+    if (a.causal) {
+        const int64_t x = static_cast<int64_t>(m - n) * a.group.G; // row_tile: a power of two
+        u.a0 = static_cast<int>((x + pl.row_tile - 1) >> pl.row_shift);
+        u.k = (128 >> pl.row_shift) * a.group.G;
+        u.lo = u.a0 >= 0 ? u.a0 / u.k + 1 : 0;
+        u.hi = u.nt + u.a0 >= 0 ? (u.nt + u.a0) / u.k + 1 : 0;
+    }
+    return u;
+}
+
+struct Sequence {
+    int q0, n, k0, m;
+};
+__device__ __forceinline__ Sequence sequence(const AttnArgs &a, int s)
+{
+    Sequence r;
+    r.q0 = clamp_start(a.q_start, s, a.Tq);
+    r.n = max(0, clamp_start(a.q_start, s + 1, a.Tq) - r.q0);
+    r.k0 = clamp_start(a.k_start, s, a.Tk);
+    r.m = max(0, clamp_start(a.k_start, s + 1, a.Tk) - r.k0);
+    return r;
+}
+
+// One block of 256 threads: the list of pieces of one head (all heads' are
+// alike), a thread taking a tile at a time.  lds: kPlanLds bytes.
+constexpr int kPlanLds = 512 * 8 + (256 + 1) * kClasses * 4 + 2 * 4;
+
+__device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *lds)
+{
+    int64_t *before = reinterpret_cast<int64_t *>(lds); // units, tiles before each
+    int64_t *tbefore = before + 256;                    // thread's run of sequences
+    int *counts = reinterpret_cast<int *>(tbefore + 256); // [classes][256]
+    int *ends = counts + 256 * kClasses;                  // [classes]; slots, divided tiles
+    const int tid = threadIdx.x;
+    const int run = (a.S + 255) / 256;
+    const int s0 = min(a.S, tid * run), s1 = min(a.S, s0 + run);
+    int64_t sum = 0, tiles = 0;
+    for (int s = s0; s < s1; ++s) {
+        const Sequence q = sequence(a, s);
+        const KeyUnits u = key_units(a, pl, q.n, q.m);
+        pl.before[s] = static_cast<int>(tiles); // within the run
+        sum += u.before(u.tiles);
+        tiles += u.tiles;
+    }
+    before[tid] = sum;
+    tbefore[tid] = tiles;
+    if (tid < 2)
+        ends[kClasses + tid] = 0;
+    __syncthreads();
+    for (int d = 1; d < 256; d <<= 1) {
+        const int64_t v = tid >= d ? before[tid - d] : 0, w = tid >= d ? tbefore[tid - d] : 0;
+        __syncthreads();
+        before[tid] += v;
+        tbefore[tid] += w;
+        __syncthreads();
+    }
+    const int64_t all = before[255];
+    // offsets that do not ascend can ask for more than the list holds: none then
+    const int all_tiles =
+        tbefore[255] > pl.room - 2 * pl.shares ? 0 : static_cast<int>(tbefore[255]);
+    __syncthreads();
+    tbefore[tid] -= tiles;
+    __syncthreads();
+    const int64_t share = max((all + pl.shares - 1) / pl.shares, static_cast<int64_t>(kLeast));
+    // tile w: its piece (without rows and slot), its rows, its class
+    int t0, rows, cls;
+    KeyPiece pc;
+    auto tile = [&](int w) {
+        // the last run, then sequence, whose first tile is not past w
+        int c = 0, len = 256;
+        while (len > 1) {
+            const int half = len >> 1;
+            const bool ok = tbefore[c + half] <= w;
+            c = ok ? c + half : c;
+            len = ok ? len - half : half;
+        }
+        const int left = w - static_cast<int>(tbefore[c]);
+        int s = min(c * run, a.S - 1);
+        len = max(1, min(run, a.S - s));
+        while (len > 1) {
+            const int half = len >> 1;
+            const bool ok = pl.before[s + half] <= left;
+            s = ok ? s + half : s;
+            len = ok ? len - half : half;
+        }
+        const Sequence q = sequence(a, s);
+        const KeyUnits ku = key_units(a, pl, q.n, q.m);
+        const int j = left - pl.before[s];
+        t0 = ku.first(j);
+        rows = ku.nt - t0;
+        // divided only where that takes off a fifth and more
+        pc.parts = 4 * static_cast<int64_t>(rows + kFixed) <= 5 * share
+                       ? 1
+                       : static_cast<int>((rows + share - 1) / share);
+        pc.q0 = q.q0, pc.n = q.n, pc.k0 = q.k0, pc.m = q.m, pc.key0 = j * 128;
+        const int64_t size = rows / pc.parts + kFixed; // up to 5/4 of a share
+        cls = kClasses - 1 - static_cast<int>(min(6 * size / share, INT64_C(kClasses - 1)));
+    };
+    // a thread takes tiles that follow one another, and they keep their order
+    // within a class: neighbours run at about the same time and read the same
+    // rows
+    const int each = (all_tiles + 255) / 256;
+    const int w0 = min(all_tiles, tid * each), w1 = min(all_tiles, w0 + each);
+    for (int c = 0; c < kClasses; ++c)
+        counts[c * 256 + tid] = 0;
+    for (int w = w0; w < w1; ++w) {
+        tile(w);
+        counts[cls * 256 + tid] += pc.parts;
+    }
+    __syncthreads();
+    for (int d = 1; d < 256; d <<= 1) {
+        int v[kClasses];
+#pragma unroll
+        for (int c = 0; c < kClasses; ++c)
+            v[c] = tid >= d ? counts[c * 256 + tid - d] : 0;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < kClasses; ++c)
+            counts[c * 256 + tid] += v[c];
+        __syncthreads();
+    }
+    if (tid == 0) {
+        *pl.next = pl.blocks; // the first ones are the blocks' own numbers
+        int at = 0;
+        for (int c = 0; c < kClasses; ++c) {
+            at += counts[c * 256 + 255];
+            ends[c] = pl.ends[c] = at;
+        }
+    }
+    __syncthreads();
+    // this thread's next place in each class: counted from the class's end
+    for (int c = 0; c < kClasses; ++c) {
+        const int last = counts[c * 256 + 255];
+        const int here = tid > 0 ? counts[c * 256 + tid - 1] : 0;
+        __syncthreads();
+        counts[c * 256 + tid] = ends[c] - last + here;
+        __syncthreads();
+    }
+    for (int w = w0; w < w1; ++w) {
+        tile(w);
+        const int at = counts[cls * 256 + tid];
+        counts[cls * 256 + tid] = at + pc.parts;
+        // which slot a piece has decides nothing
+        const int slot = pc.parts > 1 ? atomicAdd(ends + kClasses, pc.parts) : 0;
+        for (int i = 0; i < pc.parts; ++i) {
+            pc.row0 = t0 + static_cast<int>(static_cast<int64_t>(rows) * i / pc.parts);
+            pc.row1 = t0 + static_cast<int>(static_cast<int64_t>(rows) * (i + 1) / pc.parts);
+            pc.slot = slot + i;
+            pl.list[at + i] = pc;
+        }
+        if (pc.parts > 1) {
+            pc.slot = slot;
+            pl.divided[atomicAdd(ends + kClasses + 1, 1)] = pc;
+        }
+    }
+    __syncthreads();
+    if (tid == 0)
+        pl.ends[kClasses] = ends[kClasses + 1];
+}
+
 // ---- dq: rows as in the forward, 32 NQ a wave, BK keys a tile.
 //   X^T = K Q^T and dP^T = V dO^T (keys as rows), dQ^T += K^T dS^T
 template <typename E, int DC, int NQ, int BK>
 __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, const E *v, const E *o,
                                                  const float *lse, const E *dout, E *dq,
-                                                 float *delta, AttnArgs a, AttnGrads gr)
+                                                 float *delta, AttnArgs a, AttnGrads gr,
+                                                    KeyPlan pl)
 {
     using TL = Tile<E, DC>;
     using Frag = typename Elem<E>::Frag;
@@ -33,10 +240,16 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     static_assert(BK * TL::CPR % 256 == 0, "");
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
 
+    if (blockIdx.x == 0) {
+        static_assert(sizeof(smem) >= kPlanLds, "");
+        make_plan(a, pl, smem);
+        return;
+    }
+
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = lane >> 5, col = lane & 31;
-    const int kvh = blockIdx.x % a.Hkv;
-    const int w = a.slots - 1 - static_cast<int>(blockIdx.x / a.Hkv);
+    const int kvh = (blockIdx.x - 1) % a.Hkv;
+    const int w = a.slots - 1 - static_cast<int>((blockIdx.x - 1) / a.Hkv);
     const Group g = a.group;
     const Span sp = find_span<TR>(a.q_start, a.S, a.Tq, g.G, w);
     const int rows = sp.n * g.G;
@@ -120,6 +333,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
         }
     };
 
+    int ca = TL::cols_at(col, h);
+    typename TL::RowsAt ra = TL::rows_at(lane);
     floatx16 acc[NQ][DT];
 #pragma unroll
     for (int b = 0; b < NQ; ++b)
@@ -135,6 +350,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     for (int j = 0; j < ntiles; ++j) {
         unsigned char *kt = smem + (j & 1) * 2 * TB, *vt = kt + TB;
         const bool more = j + 1 < ntiles;
+        in_loop(ca), in_loop(ra.a), in_loop(ra.b);
         if (more)
             load(j + 1);
         if (j * BK < most) {
@@ -147,8 +363,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
                     x[b] = dp[b] = floatx16{};
 #pragma unroll
                 for (int s = 0; s < DS; ++s) {
-                    const Frag kf = TL::read_cols(kt, 32 * t + col, s, h);
-                    const Frag vf = TL::read_cols(vt, 32 * t + col, s, h);
+                    const Frag kf = TL::read_cols(kt + 32 * t * TL::PITCH, ca, s);
+                    const Frag vf = TL::read_cols(vt + 32 * t * TL::PITCH, ca, s);
 #pragma unroll
                     for (int b = 0; b < NQ; ++b) {
                         x[b] = add_product(kf, qf[b][s], x[b]);
@@ -178,7 +394,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
                         sf[b] = to_frag<E>(x[b], s);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
-                        const Frag kf = TL::read_rows(kt, 32 * t + 16 * s, d, lane);
+                        const Frag kf = TL::read_rows(kt, ra, 32 * t + 16 * s, d);
 #pragma unroll
                         for (int b = 0; b < NQ; ++b)
                             acc[b][d] = mma(kf, sf[b], acc[b][d]);
@@ -202,14 +418,23 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     }
 }
 
-// ---- dk and dv: 128 keys a block, 32 a wave; BR rows a tile.
+// Rows a step of attn_dkv_k takes, and the blocks of it that a compute unit
+// holds at once (registers and LDS).
+constexpr int dkv_rows(bool f32, int DC) { return !f32 && DC <= 96 ? 64 : 32; }
+constexpr int dkv_per_cu(bool f32, int DC)
+{
+    return DC <= 32 && !f32 ? 4 : DC <= 64 || !f32 ? 2 : 1;
+}
+
+// ---- dk and dv: tiles of 128 keys, 32 a wave; BR rows a step.
 //   X = Q K^T and dP = dO V^T (query rows as rows; a lane holds one key),
 //   dV^T += dO^T P, dK^T += Q^T dS
+// Blocks take pieces off the list until it is empty.
 template <typename E, int DC, int BR>
-__global__ __launch_bounds__(256, 2) void attn_dkv_k(const E *q, const E *k, const E *v,
-                                                  const float *lse, const E *dout,
-                                                  const float *delta, E *dk, E *dv, AttnArgs a,
-                                                  AttnGrads gr)
+__global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_k(const E *q, const E *k, const E *v,
+                                                     const float *lse, const E *dout,
+                                                     const float *delta, E *dk, E *dv, AttnArgs a,
+                                                     AttnGrads gr, KeyPlan pl)
 {
     using TL = Tile<E, DC>;
     using Frag = typename Elem<E>::Frag;
@@ -219,206 +444,279 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_k(const E *q, const E *k, con
     static_assert(BR * TL::CPR % 256 == 0 && BR <= 64, "");
     constexpr int BUF = 2 * TB + 4 * BR * 4; // Q, dO; lse, delta, keys seen, lse's rest
     // the values' operands stay in registers where they fit beside the sums
-    constexpr bool VL = DT > 2;
+    constexpr bool VL = DT > (sizeof(E) == 4 ? 2 : 3);
     __shared__ __align__(16) unsigned char smem[2 * BUF + (VL ? TL::bytes(128) : 0)];
+    __shared__ int next, ends[kClasses];
     unsigned char *vl = smem + 2 * BUF;
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = lane >> 5, col = lane & 31;
-    const int kvh = blockIdx.x % a.Hkv;
     const Group g = a.group;
-    const Span sp =
-        find_span<128>(a.k_start, a.S, a.Tk, 1, static_cast<int>(blockIdx.x / a.Hkv));
-    const int m = sp.n;
-    if (static_cast<int64_t>(sp.tile) * 128 >= m)
-        return;
-    const int key0 = sp.tile * 128;
-    const int qb = clamp_start(a.q_start, sp.seq, a.Tq);
-    const int n = max(0, clamp_start(a.q_start, sp.seq + 1, a.Tq) - qb);
-    const int rows = n * g.G, ahead = m - n;
-
-    const int key = key0 + wave * 32 + col, kc = min(key, m - 1);
-    Frag kf[DS], vf[VL ? 1 : DS];
-#pragma unroll
-    for (int s = 0; s < DS; ++s) {
-        kf[s] = load_frag<E>(k + (sp.begin + kc) * a.ldk + kvh * a.D, 16 * s + 8 * h, a.D);
-        if constexpr (!VL)
-            vf[s] = load_frag<E>(v + (sp.begin + kc) * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
-    }
-    if constexpr (VL)
-        for (int e = threadIdx.x; e < 128 * TL::CPR; e += 256) {
-            const int c = e % TL::CPR * Elem<E>::VEC;
-            const int64_t r = sp.begin + min(key0 + e / TL::CPR, m - 1);
-            *reinterpret_cast<uint4 *>(vl + TL::chunk_at(e / TL::CPR, e % TL::CPR)) =
-                c < a.D ? *reinterpret_cast<const uint4 *>(v + r * a.ldv + kvh * a.D + c)
-                        : uint4{0, 0, 0, 0};
-        }
-    // first row that sees a key of the block
-    const int tile0 = a.causal ? static_cast<int>(static_cast<int64_t>(max(0, key0 - ahead)) * g.G / BR) : 0;
-    const int ntiles = (rows + BR - 1) / BR;
-
-    const E *qp = q + qb * a.ldq + static_cast<int64_t>(kvh) * g.G * a.D;
-    const E *gp = dout + qb * gr.lddo + static_cast<int64_t>(kvh) * g.G * a.D;
-    const float *lp = lse + static_cast<int64_t>(qb) * a.Hq + kvh * g.G;
-    const float *dp0 = delta + static_cast<int64_t>(qb) * a.Hq + kvh * g.G;
-    uint4 qs[NCH], gs[NCH];
-    Ref ls{0.f, 0.f};
-    float ds = 0.f;
-    int sees = 0;
-    auto load = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            const int c = e % TL::CPR * Elem<E>::VEC;
-            const int r = min(tile * BR + e / TL::CPR, rows - 1);
-            const int t = row_token(g, r), hd = r - t * g.G;
-            qs[i] = gs[i] = uint4{0, 0, 0, 0};
-            if (c < a.D) {
-                qs[i] = *reinterpret_cast<const uint4 *>(qp + t * a.ldq + hd * a.D + c);
-                gs[i] = *reinterpret_cast<const uint4 *>(gp + t * gr.lddo + hd * a.D + c);
-            }
-        }
-        if (threadIdx.x < BR) {
-            const int r = tile * BR + threadIdx.x;
-            const int t = row_token(g, min(r, rows - 1)), hd = min(r, rows - 1) - t * g.G;
-            const float l = lp[static_cast<int64_t>(t) * a.Hq + hd];
-            // rows past the end and rows that saw no key: every p is 0
-            ls = r >= rows || l == -HUGE_VALF ? Ref{HUGE_VALF, 0.f} : ref_of_lse(l);
-            ds = dp0[static_cast<int64_t>(t) * a.Hq + hd];
-            sees = r >= rows ? 0 : a.causal ? max(0, t + ahead + 1) : m;
-        }
-    };
-    auto store = [&](unsigned char *t) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            const int p = TL::chunk_at(e / TL::CPR, e % TL::CPR);
-            *reinterpret_cast<uint4 *>(t + p) = qs[i];
-            *reinterpret_cast<uint4 *>(t + TB + p) = gs[i];
-        }
-        if (threadIdx.x < BR) {
-            float *f = reinterpret_cast<float *>(t + 2 * TB);
-            f[threadIdx.x] = ls.hi;
-            f[BR + threadIdx.x] = ds;
-            reinterpret_cast<int *>(f)[2 * BR + threadIdx.x] = sees;
-            f[3 * BR + threadIdx.x] = ls.lo;
-        }
-    };
-
-    floatx16 dka[DT], dva[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-        dka[d] = dva[d] = floatx16{};
-
-    if (tile0 < ntiles) {
-        load(tile0);
-        store(smem);
-    }
+    if (threadIdx.x < kClasses)
+        ends[threadIdx.x] = pl.ends[threadIdx.x] * a.Hkv;
     __syncthreads();
-    for (int j = tile0; j < ntiles; ++j) {
-        unsigned char *qt = smem + ((j - tile0) & 1) * BUF, *gt = qt + TB;
-        const float *lt = reinterpret_cast<const float *>(qt + 2 * TB), *dt = lt + BR;
-        const int *st = reinterpret_cast<const int *>(dt + BR);
-        const bool more = j + 1 < ntiles;
-        if (more)
-            load(j + 1);
-        // the first row of a tile sees the fewest keys, the last (of the rows
-        // there are) the most
-        const int first_sees = a.causal ? row_token(g, min(j * BR, rows - 1)) + ahead + 1 : m;
-        const int last_sees =
-            a.causal ? row_token(g, min((j + 1) * BR, rows) - 1) + ahead + 1 : m;
-        const int wkey = key0 + wave * 32;
-        if (wkey < last_sees) {
-            const bool masked = wkey + 32 > first_sees;
+    int w = blockIdx.x;
+#pragma unroll 1
+    while (w < ends[kClasses - 1]) {
+        // the number after this one, asked for now and needed at the end
+        int after = 0;
+        if (threadIdx.x == 0)
+            after = atomicAdd(pl.next, 1);
+        // class after class, of all heads each
+        int c = 0;
+        while (w >= ends[c])
+            ++c;
+        const int first = __builtin_amdgcn_readfirstlane(c > 0 ? ends[c - 1] : 0) / a.Hkv;
+        const int of = __builtin_amdgcn_readfirstlane(ends[c]) / a.Hkv - first;
+        const int i = w - first * a.Hkv, kvh = i / of;
+        const KeyPiece pc = pl.list[first + i - kvh * of];
+        const int key0 = pc.key0, m = pc.m, rows = pc.n * g.G, ahead = m - pc.n;
+        const int tile0 = pc.row0, ntiles = pc.row1;
+
+        const int key = key0 + wave * 32 + col, kc = min(key, m - 1);
+        Frag kf[DS], vf[VL ? 1 : DS];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                floatx16 x = floatx16{}, dp = floatx16{};
+        for (int s = 0; s < DS; ++s) {
+            const int64_t at = pc.k0 + kc;
+            kf[s] = load_frag<E>(k + at * a.ldk + kvh * a.D, 16 * s + 8 * h, a.D);
+            if constexpr (!VL)
+                vf[s] = load_frag<E>(v + at * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
+        }
+        if constexpr (VL)
+            for (int e = threadIdx.x; e < 128 * TL::CPR; e += 256) {
+                const int c = e % TL::CPR * Elem<E>::VEC;
+                const int64_t r = pc.k0 + min(key0 + e / TL::CPR, m - 1);
+                *reinterpret_cast<uint4 *>(vl + TL::chunk_at(e / TL::CPR, e % TL::CPR)) =
+                    c < a.D ? *reinterpret_cast<const uint4 *>(v + r * a.ldv + kvh * a.D + c)
+                            : uint4{0, 0, 0, 0};
+            }
+
+        const E *qp = q + pc.q0 * a.ldq + static_cast<int64_t>(kvh) * g.G * a.D;
+        const E *gp = dout + pc.q0 * gr.lddo + static_cast<int64_t>(kvh) * g.G * a.D;
+        const float *lp = lse + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
+        const float *dp0 = delta + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
+        uint4 qs[NCH], gs[NCH];
+        Ref ls{0.f, 0.f};
+        float ds = 0.f;
+        int sees = 0;
+        auto load = [&](int tile) {
 #pragma unroll
-                for (int s = 0; s < DS; ++s) {
-                    x = add_product(TL::read_cols(qt, 32 * t + col, s, h), kf[s], x);
-                    const Frag vs = VL ? TL::read_cols(vl, wave * 32 + col, s, h) : vf[VL ? 0 : s];
-                    dp = add_product(TL::read_cols(gt, 32 * t + col, s, h), vs, dp);
+            for (int i = 0; i < NCH; ++i) {
+                const int e = threadIdx.x + 256 * i;
+                const int c = e % TL::CPR * Elem<E>::VEC;
+                const int r = min(tile * BR + e / TL::CPR, rows - 1);
+                const int t = row_token(g, r), hd = r - t * g.G;
+                qs[i] = gs[i] = uint4{0, 0, 0, 0};
+                if (c < a.D) {
+                    qs[i] = *reinterpret_cast<const uint4 *>(qp + t * a.ldq + hd * a.D + c);
+                    gs[i] = *reinterpret_cast<const uint4 *>(gp + t * gr.lddo + hd * a.D + c);
                 }
+            }
+            if (threadIdx.x < BR) {
+                const int r = tile * BR + threadIdx.x;
+                const int t = row_token(g, min(r, rows - 1)), hd = min(r, rows - 1) - t * g.G;
+                const float l = lp[static_cast<int64_t>(t) * a.Hq + hd];
+                // rows past the end and rows that saw no key: every p is 0
+                ls = r >= rows || l == -HUGE_VALF ? Ref{HUGE_VALF, 0.f} : ref_of_lse(l);
+                ds = dp0[static_cast<int64_t>(t) * a.Hq + hd];
+                sees = r >= rows ? 0 : a.causal ? max(0, t + ahead + 1) : m;
+            }
+        };
+        auto store = [&](unsigned char *t) {
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                const int e = threadIdx.x + 256 * i;
+                const int p = TL::chunk_at(e / TL::CPR, e % TL::CPR);
+                *reinterpret_cast<uint4 *>(t + p) = qs[i];
+                *reinterpret_cast<uint4 *>(t + TB + p) = gs[i];
+            }
+            if (threadIdx.x < BR) {
+                float *f = reinterpret_cast<float *>(t + 2 * TB);
+                f[threadIdx.x] = ls.hi;
+                f[BR + threadIdx.x] = ds;
+                reinterpret_cast<int *>(f)[2 * BR + threadIdx.x] = sees;
+                f[3 * BR + threadIdx.x] = ls.lo;
+            }
+        };
+
+        const unsigned char *vw = vl + wave * 32 * TL::PITCH;
+        int ca = TL::cols_at(col, h);
+        typename TL::RowsAt ra = TL::rows_at(lane);
+        floatx16 dka[DT], dva[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            dka[d] = dva[d] = floatx16{};
+
+        if (tile0 < ntiles) {
+            load(tile0);
+            store(smem);
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int j = tile0; j < ntiles; ++j) {
+            unsigned char *qt = smem + ((j - tile0) & 1) * BUF, *gt = qt + TB;
+            const float *lt = reinterpret_cast<const float *>(qt + 2 * TB), *dt = lt + BR;
+            const int *st = reinterpret_cast<const int *>(dt + BR);
+            const bool more = j + 1 < ntiles;
+            in_loop(ca), in_loop(ra.a), in_loop(ra.b);
+            if (more)
+                load(j + 1);
+            // the first row of a tile sees the fewest keys, the last (of the
+            // rows there are) the most
+            const int first_sees = a.causal ? row_token(g, min(j * BR, rows - 1)) + ahead + 1 : m;
+            const int last_sees =
+                a.causal ? row_token(g, min((j + 1) * BR, rows) - 1) + ahead + 1 : m;
+            const int wkey = key0 + wave * 32;
+            if (wkey < last_sees) {
+                const bool masked = wkey + 32 > first_sees;
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    floatx16 x = floatx16{}, dp = floatx16{};
+#pragma unroll
+                    for (int s = 0; s < DS; ++s) {
+                        x = add_product(TL::read_cols(qt + 32 * t * TL::PITCH, ca, s), kf[s], x);
+                        const Frag vs =
+                            VL ? TL::read_cols(vw, ca, s) : vf[VL ? 0 : s];
+                        dp = add_product(TL::read_cols(gt + 32 * t * TL::PITCH, ca, s), vs, dp);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = 32 * t + 8 * i + 4 * h;
+                        const float4 l4 = *reinterpret_cast<const float4 *>(lt + at);
+                        const float4 d4 = *reinterpret_cast<const float4 *>(dt + at);
+                        const float l[4] = {l4.x, l4.y, l4.z, l4.w};
+                        const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
+                        float4 r4{0.f, 0.f, 0.f, 0.f};
+                        if constexpr (sizeof(E) == 4)
+                            r4 = *reinterpret_cast<const float4 *>(lt + 3 * BR + at);
+                        const float ll[4] = {r4.x, r4.y, r4.z, r4.w};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float p = prob<E>(x[4 * i + r], a, l[r], ll[r]);
+                            x[4 * i + r] = p;
+                            dp[4 * i + r] = p * (dp[4 * i + r] - dd[r]);
+                        }
+                        if (masked) {
+                            const int4 s4 = *reinterpret_cast<const int4 *>(st + at);
+                            const int sees4[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (key >= sees4[r])
+                                    x[4 * i + r] = dp[4 * i + r] = 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const Frag pf = to_frag<E>(x, s), sf = to_frag<E>(dp, s);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            dva[d] = mma(TL::read_rows(gt, ra, 32 * t + 16 * s, d), pf, dva[d]);
+                            dka[d] = mma(TL::read_rows(qt, ra, 32 * t + 16 * s, d), sf, dka[d]);
+                        }
+                    }
+                }
+            }
+            if (more)
+                store(smem + ((j + 1 - tile0) & 1) * BUF);
+            __syncthreads();
+        }
+
+        if (pc.parts > 1) {
+            float4 *part = pl.part +
+                           (2 * static_cast<int64_t>(kvh) * pl.shares + pc.slot) * (2 * DT * 4 * 256) +
+                           threadIdx.x;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = 32 * t + 8 * i + 4 * h;
-                    const float4 l4 = *reinterpret_cast<const float4 *>(lt + at);
-                    const float4 d4 = *reinterpret_cast<const float4 *>(dt + at);
-                    const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
-                    float4 r4{0.f, 0.f, 0.f, 0.f};
-                    if constexpr (sizeof(E) == 4)
-                        r4 = *reinterpret_cast<const float4 *>(lt + 3 * BR + at);
-                    const float ll[4] = {r4.x, r4.y, r4.z, r4.w};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float p = prob<E>(x[4 * i + r], a, l[r], ll[r]);
-                        x[4 * i + r] = p;
-                        dp[4 * i + r] = p * (dp[4 * i + r] - dd[r]);
-                    }
-                    if (masked) {
-                        const int4 s4 = *reinterpret_cast<const int4 *>(st + at);
-                        const int sees4[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (key >= sees4[r])
-                                x[4 * i + r] = dp[4 * i + r] = 0.f;
-                    }
+                    part[(d * 4 + i) * 256] = quad(dka[d], i);
+                    part[((DT + d) * 4 + i) * 256] = quad(dva[d], i);
                 }
+        } else if (key < m) {
+            E *kp = dk + (pc.k0 + key) * gr.lddk + kvh * a.D;
+            E *vp = dv + (pc.k0 + key) * gr.lddv + kvh * a.D;
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const Frag pf = to_frag<E>(x, s), sf = to_frag<E>(dp, s);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        dva[d] = mma(TL::read_rows(gt, 32 * t + 16 * s, d, lane), pf, dva[d]);
-                        dka[d] = mma(TL::read_rows(qt, 32 * t + 16 * s, d, lane), sf, dka[d]);
-                    }
-                }
+            for (int d = 0; d < DT; ++d) {
+                store_col(kp, dka[d], 32 * d + 4 * h, a.D, a.scale);
+                store_col(vp, dva[d], 32 * d + 4 * h, a.D, 1.f);
             }
         }
-        if (more)
-            store(smem + ((j + 1 - tile0) & 1) * BUF);
+        if (threadIdx.x == 0)
+            next = after;
+        __syncthreads();
+        w = __builtin_amdgcn_readfirstlane(next);
         __syncthreads();
     }
+}
 
-    if (key >= m)
+// Adds up the pieces of divided tiles: block = (head, divided tile, 32 elements
+// of dk or dv), thread = the lane that holds them in attn_dkv_k.
+template <typename E, int DC>
+__global__ __launch_bounds__(256) void attn_dkv_join_k(E *dk, E *dv, AttnArgs a, AttnGrads gr,
+                                                       KeyPlan pl)
+{
+    constexpr int DT = DC / 32;
+    const int item = blockIdx.x % pl.shares, kvh = blockIdx.x / pl.shares;
+    if (item >= pl.ends[kClasses])
         return;
-    E *kp = dk + (sp.begin + key) * gr.lddk + kvh * a.D, *vp = dv + (sp.begin + key) * gr.lddv + kvh * a.D;
+    const KeyPiece pc = pl.divided[item];
+    const int which = blockIdx.y; // dk's tiles of 32 elements, then dv's
+    floatx16 sum = floatx16{};
+    for (int i = 0; i < pc.parts; ++i) {
+        const float4 *p = pl.part +
+                          (2 * static_cast<int64_t>(kvh) * pl.shares + pc.slot + i) *
+                              (2 * DT * 4 * 256) +
+                          which * 4 * 256 + threadIdx.x;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-        store_col(kp, dka[d], 32 * d + 4 * h, a.D, a.scale);
-        store_col(vp, dva[d], 32 * d + 4 * h, a.D, 1.f);
+        for (int c = 0; c < 4; ++c)
+            add_quad(sum, c, p[c * 256]);
     }
+    const int lane = threadIdx.x & 63;
+    const int key = pc.key0 + (threadIdx.x >> 6) * 32 + (lane & 31), c0 = 4 * (lane >> 5);
+    if (key >= pc.m)
+        return;
+    const int64_t at = pc.k0 + key;
+    if (which < DT)
+        store_col(dk + at * gr.lddk + kvh * a.D, sum, 32 * which + c0, a.D, a.scale);
+    else
+        store_col(dv + at * gr.lddv + kvh * a.D, sum, 32 * (which - DT) + c0, a.D, 1.f);
 }
 
 template <typename E, int DC>
 hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *lse, const E *dout,
                   E *dq, E *dk, E *dv, float *delta, AttnArgs a, const AttnGrads &gr,
-                  hipStream_t st)
+                  const KeyPlan &pl, hipStream_t st)
 {
     constexpr bool F32 = sizeof(E) == 4;
-    constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64, BR = !F32 && DC != 128 ? 64 : 32;
-    AttnArgs b = a;
+    constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 128 * NQ, a.S);
-    HEX_LAUNCH((attn_dq_k<E, DC, NQ, BK>), dim3(static_cast<uint32_t>(a.slots) * a.Hkv), dim3(256),
-               0, st, q, k, v, o, lse, dout, dq, delta, a, gr);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
+    // one block more, the first, divides the keys' work
+    HEX_LAUNCH((attn_dq_k<E, DC, NQ, BK>), dim3(static_cast<uint32_t>(a.slots) * a.Hkv + 1),
+               dim3(256), 0, st, q, k, v, o, lse, dout, dq, delta, a, gr, pl);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.Tk == 0)
         return e;
-    b.slots = attn_slots(a.Tk, 1, 128, a.S);
-    HEX_LAUNCH((attn_dkv_k<E, DC, BR>), dim3(static_cast<uint32_t>(b.slots) * a.Hkv), dim3(256), 0,
-               st, q, k, v, lse, dout, delta, dk, dv, b, gr);
+    HEX_LAUNCH((attn_dkv_k<E, DC, dkv_rows(F32, DC)>), dim3(static_cast<uint32_t>(pl.blocks)),
+               dim3(256), 0, st, q, k, v, lse, dout, delta, dk, dv, a, gr, pl);
+    e = hipGetLastError();
+    // no tile of so few rows is divided
+    const int64_t row_tiles = static_cast<int64_t>(a.Tq) * a.group.G / pl.row_tile + 1;
+    if (e != hipSuccess || row_tiles + kFixed <= kLeast)
+        return e;
+    HEX_LAUNCH((attn_dkv_join_k<E, DC>), dim3(static_cast<uint32_t>(pl.shares) * a.Hkv, DC / 16),
+               dim3(256), 0, st, dk, dv, a, gr, pl);
     return hipGetLastError();
 }
 
 template <typename E>
 hipError_t by_dim(const void *q, const void *k, const void *v, const void *o, const float *lse,
                   const void *dout, void *dq, void *dk, void *dv, float *delta, const AttnArgs &a,
-                  const AttnGrads &gr, hipStream_t st)
+                  const AttnGrads &gr, const KeyPlan &pl, hipStream_t st)
 {
     const auto run = [&](auto f) {
         return f(static_cast<const E *>(q), static_cast<const E *>(k), static_cast<const E *>(v),
                  static_cast<const E *>(o), lse, static_cast<const E *>(dout), static_cast<E *>(dq),
-                 static_cast<E *>(dk), static_cast<E *>(dv), delta, a, gr, st);
+                 static_cast<E *>(dk), static_cast<E *>(dv), delta, a, gr, pl, st);
     };
     if (a.D <= 32)
         return run(launch<E, 32>);
@@ -429,16 +727,70 @@ hipError_t by_dim(const void *q, const void *k, const void *v, const void *o, co
     return run(launch<E, 128>);
 }
 
+size_t round16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
+
+// the workspace: delta, the plan's parts, partial sums
+struct BwdSpace {
+    size_t before, next, ends, divided, list, part, bytes;
+    int shares, blocks, room, row_tile;
+};
+BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
+{
+    const int DC = (D + 31) / 32 * 32;
+    const bool f32 = dt == F32;
+    BwdSpace w;
+    w.row_tile = dkv_rows(f32, DC);
+    // no more shares of a head than make kLeast units each, no more blocks
+    // than pieces
+    const double tiles = Tk / 128 + static_cast<double>(S);
+    const double units = tiles * (static_cast<double>(Tq) * (Hq / Hkv) / w.row_tile + 1 + kFixed);
+    const int held = dkv_per_cu(f32, DC) * device_cus();
+    const int most = (kShares * held + Hkv - 1) / Hkv;
+    w.shares = units / kLeast + 1 < most ? static_cast<int>(units / kLeast) + 1 : most;
+    // a divided tile has more than a share, so that there are fewer of them
+    // than shares, and fewer pieces of them than twice that
+    w.room = static_cast<int>(tiles) + 2 * w.shares;
+    w.blocks = static_cast<double>(w.room) * Hkv < held ? w.room * Hkv : held;
+    w.before = round16(static_cast<size_t>(Tq) * Hq * sizeof(float));
+    w.next = (w.before + static_cast<size_t>(S) * sizeof(int) + 255) & ~static_cast<size_t>(255);
+    w.ends = w.next + 256; // the counter in a cache line of its own
+    w.divided = w.ends + 256;
+    w.list = w.divided + round16(static_cast<size_t>(w.shares) * sizeof(KeyPiece));
+    w.part = w.list + round16(static_cast<size_t>(w.room) * sizeof(KeyPiece));
+    w.bytes = w.part + static_cast<size_t>(w.shares) * Hkv * 2 * (2 * 128 * DC) * sizeof(float);
+    return w;
+}
+
 } // namespace
 } // namespace attn
 
 hipError_t attn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
-                    const void *dout, void *dq, void *dk, void *dv, float *delta,
-                    const AttnArgs &a, const AttnGrads &gr, Dtype dt, hipStream_t st)
+                    const void *dout, void *dq, void *dk, void *dv, void *ws, const AttnArgs &a,
+                    const AttnGrads &gr, Dtype dt, hipStream_t st)
 {
+    const attn::BwdSpace w = attn::bwd_space(a.Tq, a.Tk, a.S, a.Hq, a.Hkv, a.D, dt);
+    unsigned char *p = static_cast<unsigned char *>(ws);
+    KeyPlan pl;
+    pl.before = reinterpret_cast<int *>(p + w.before);
+    pl.next = reinterpret_cast<int *>(p + w.next);
+    pl.ends = reinterpret_cast<int *>(p + w.ends);
+    pl.divided = reinterpret_cast<KeyPiece *>(p + w.divided);
+    pl.list = reinterpret_cast<KeyPiece *>(p + w.list);
+    pl.part = reinterpret_cast<float4 *>(p + w.part);
+    pl.shares = w.shares;
+    pl.blocks = w.blocks;
+    pl.room = w.room;
+    pl.row_tile = w.row_tile;
+    pl.row_shift = w.row_tile == 64 ? 6 : 5;
+    float *delta = static_cast<float *>(ws);
     return dt == F32
-               ? attn::by_dim<float>(q, k, v, o, lse, dout, dq, dk, dv, delta, a, gr, st)
-               : attn::by_dim<bf16raw>(q, k, v, o, lse, dout, dq, dk, dv, delta, a, gr, st);
+               ? attn::by_dim<float>(q, k, v, o, lse, dout, dq, dk, dv, delta, a, gr, pl, st)
+               : attn::by_dim<bf16raw>(q, k, v, o, lse, dout, dq, dk, dv, delta, a, gr, pl, st);
+}
+
+size_t attn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
+{
+    return attn::bwd_space(Tq, Tk, S, Hq, Hkv, D, dt).bytes;
 }
 
 } // namespace hexk

@@ -114,6 +114,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
         }
     };
 
+    int ca = TL::cols_at(col, h);
+    typename TL::RowsAt ra = TL::rows_at(lane);
     floatx16 acc[NQ][DT];
     float mx[NQ], sum[NQ];
 #pragma unroll
@@ -133,6 +135,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
     for (int j = 0; j < ntiles; ++j) {
         unsigned char *kt = smem + (j & 1) * 2 * TB, *vt = kt + TB;
         const bool more = j + 1 < ntiles;
+        in_loop(ca), in_loop(ra.a), in_loop(ra.b);
         if (more)
             load(j + 1);
         if (j * BK < most) {
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
                     x[b][t] = floatx16{};
 #pragma unroll
                 for (int s = 0; s < DS; ++s) {
-                    const Frag kf = TL::read_cols(kt, 32 * t + col, s, h);
+                    const Frag kf = TL::read_cols(kt + 32 * t * TL::PITCH, ca, s);
 #pragma unroll
                     for (int b = 0; b < NQ; ++b)
                         x[b][t] = add_product(kf, qf[b][s], x[b][t]);
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
                         pf[b] = to_frag<E>(x[b][t], s);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
-                        const Frag vf = TL::read_rows(vt, 32 * t + 16 * s, d, lane);
+                        const Frag vf = TL::read_rows(vt, ra, 32 * t + 16 * s, d);
 #pragma unroll
                         for (int b = 0; b < NQ; ++b)
                             acc[b][d] = mma(vf, pf[b], acc[b][d]);

@@ -87,6 +87,8 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const
         }
     };
 
+    int ca = TL::cols_at(col, h);
+    typename TL::RowsAt ra = TL::rows_at(lane);
     floatx16 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -98,6 +100,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const
         load(k0);
     for (; k0 < end; k0 += kStepWaves * BK) {
         store();
+        in_loop(ca), in_loop(ra.a), in_loop(ra.b);
         // one wave's LDS reads and writes keep their order; this keeps the
         // compiler to it
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const
         floatx16 x = floatx16{};
 #pragma unroll
         for (int s = 0; s < DS; ++s)
-            x = add_product(TL::read_cols(kt, col, s, h), qf[s], x);
+            x = add_product(TL::read_cols(kt, ca, s), qf[s], x);
         // keys past the run belong to another block or do not exist
         const int left = min(see, end) - k0 - 4 * h;
         float top = -HUGE_VALF;
@@ -137,7 +140,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const
             const Frag pf = to_frag<E>(x, s);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
-                acc[d] = mma(TL::read_rows(vt, 16 * s, d, lane), pf, acc[d]);
+                acc[d] = mma(TL::read_rows(vt, ra, 16 * s, d), pf, acc[d]);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();

@@ -277,11 +277,28 @@ struct AttnGrads {
 hipError_t attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse,
                     const AttnArgs &a, Dtype dt, hipStream_t st);
 
-// delta: a float per query row [Tq][Hq], written by the first kernel and read
-// by the second; k_len is not used (a key belongs to one sequence)
+// A piece of the gradient's second kernel: 128 keys from key0 on of the
+// sequence with queries q0 .. q0 + n and keys k0 .. k0 + m, and the row tiles
+// row0 .. row1 of them.  parts > 1: one of so many of its tile, whose sums go
+// to partial sum `slot`.
+struct KeyPiece {
+    int q0, n, k0, m, key0, row0, row1, parts, slot, pad[3];
+};
+// How that kernel's work is divided: tiles before each sequence [S]; next
+// number; pieces up to the end of each class of size, and divided tiles [8 + 1];
+// first pieces of the divided tiles [shares]; the list [room]; partial sums
+// [Hkv][2 shares].
+struct KeyPlan {
+    int *before, *next, *ends;
+    KeyPiece *divided, *list;
+    float4 *part;
+    int shares, blocks, room, row_tile, row_shift; // row_tile = 2^row_shift
+};
+// k_len is not used (a key belongs to one sequence)
+size_t attn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt);
 hipError_t attn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
-                    const void *dout, void *dq, void *dk, void *dv, float *delta,
-                    const AttnArgs &a, const AttnGrads &gr, Dtype dt, hipStream_t st);
+                    const void *dout, void *dq, void *dk, void *dv, void *ws, const AttnArgs &a,
+                    const AttnGrads &gr, Dtype dt, hipStream_t st);
 
 // New tokens over a cache: runs of `chunk` keys, `splits` of them at most,
 // row_tiles tiles of 32 rows; rows = S n Hq in all.

@@ -129,7 +129,7 @@ def test_dropout_refuses(kw, status):
 
 def test_workspace_of_bad_arguments():
     assert hx.hexattn_bwd_workspace(9, 9, 2, 3, 2, 32, 0) == 0
-    assert hx.hexattn_bwd_workspace(9, 9, 2, 4, 2, 32, 0) == 9 * 4 * 4
+    assert hx.hexattn_bwd_workspace(9, 9, 2, 4, 2, 32, 0) >= 9 * 4 * 4
     assert hx.hexattn_step_workspace(0, 1, 4, 2, 32, 100, 0) == 0
     assert hx.hexrotary_bwd_workspace(0, 4, 2, 32, 0) == 0
 

@@ -1126,7 +1126,7 @@ int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws,
         return HEX_ERR_UNSUPPORTED;
     const hexk::StepPlan p = hexk::step_plan(S, n, Hq, Hkv, max_len);
     if (static_cast<int64_t>(S) * Hkv * p.row_tiles > kMaxBlocks / p.splits ||
-        p.rows * (D / 4) / 256 > kMaxBlocks)
+        p.rows > kMaxBlocks)
         return HEX_ERR_UNSUPPORTED;
     const size_t need = hexk::step_workspace(p, D);
     if (ws_bytes < need || (need > 0 && ws == nullptr))

@@ -19,11 +19,11 @@ namespace attn {
 namespace {
 
 constexpr int kStepWaves = 4;
+constexpr int kMaxRuns = 1024; // of a row, to be joined in LDS
 
 template <typename E, int DC>
-__global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const E *k, const E *v,
-                                                               E *o, float *part, float2 *stat,
-                                                               AttnArgs a, StepPlan pl)
+__global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void attn_step_k(
+    const E *q, const E *k, const E *v, E *o, float *part, float2 *stat, AttnArgs a, StepPlan pl)
 {
     using TL = Tile<E, DC>;
     using Frag = typename Elem<E>::Frag;
@@ -36,12 +36,15 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = lane >> 5, col = lane & 31;
+    // Runs outermost: late ones, which only long sequences have, are spread
+    // over all dies (blocks go to the 8 dies in turn; with the runs inside, the
+    // same few dies got them, 19 to 45 us for one batch)
     uint32_t id = blockIdx.x;
     const int kvh = id % a.Hkv;
     id /= a.Hkv;
-    const int split = id % pl.splits;
-    id /= pl.splits;
-    const int rt = id % pl.row_tiles, seq = id / pl.row_tiles;
+    const int seq = id % a.S;
+    id /= a.S;
+    const int rt = id % pl.row_tiles, split = id / pl.row_tiles;
     const Group g = a.group;
     const int rows = pl.n * g.G;
 
@@ -208,38 +211,75 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_k(const E *q, const
     }
 }
 
-// Joins the runs of a row in their order: thread = 4 elements of a row.
-template <typename E>
-__global__ __launch_bounds__(256) void attn_join_k(const float *part, const float2 *stat, E *o,
+// Joins the runs of a row: block = row, thread = 4 elements and every ny-th run.
+// NT threads: a wave where there are few runs and many rows.
+template <typename E, int NT>
+__global__ __launch_bounds__(NT) void attn_join_k(const float *part, const float2 *stat, E *o,
                                                    AttnArgs a, StepPlan pl)
 {
-    const int per = a.D / 4;
-    const int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = e / per;
-    if (row >= pl.rows)
-        return;
-    const int c = static_cast<int>(e - row * per) * 4;
+    __shared__ float weight[kMaxRuns];
+    constexpr int NW = NT / 64;
+    __shared__ float red[2][NW];
+    __shared__ __align__(16) float4 sums[NT];
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
     int kb, m;
     key_span(a, static_cast<int>(row / (static_cast<int64_t>(pl.n) * a.Hq)), kb, m);
     const int runs = (m + pl.chunk - 1) / pl.chunk;
-    float top = -HUGE_VALF, l = 0.f;
+    // the largest maximum, then every run's weight and the sum of the weights
+    float top = -HUGE_VALF;
+    for (int i = tid; i < runs; i += NT)
+        top = fmaxf(top, stat[i * pl.rows + row].x);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+        top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0)
+        red[0][tid >> 6] = top;
+    __syncthreads();
+    top = red[0][0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i)
+        top = fmaxf(top, red[0][i]);
+    float l = 0.f;
+    for (int i = tid; i < runs; i += NT) {
+        const float2 st = stat[i * pl.rows + row];
+        // a run of which no key is seen has no maximum
+        const float w = st.x == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(st.x - top);
+        weight[i] = w;
+        l = fmaf(st.y, w, l);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+        l += __shfl_xor(l, d);
+    if ((tid & 63) == 0)
+        red[1][tid >> 6] = l;
+    __syncthreads();
+    l = red[1][0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i)
+        l += red[1][i];
+    const int per = a.D / 4, ny = NT / per;
+    const int c = tid % per, y = tid / per;
     float4 s{0, 0, 0, 0};
-    for (int i = 0; i < runs; ++i) {
-        const int64_t at = i * pl.rows + row;
-        const float2 st = stat[at];
-        if (st.y == 0.f)
-            continue; // no key of the run is seen
-        const float4 u = *reinterpret_cast<const float4 *>(part + at * a.D + c);
-        const float to = fmaxf(top, st.x);
-        const float f = top == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(top - to);
-        const float w = __builtin_amdgcn_exp2f(st.x - to);
-        top = to;
-        l = l * f + st.y * w;
-        s.x = s.x * f + u.x * w, s.y = s.y * f + u.y * w;
-        s.z = s.z * f + u.z * w, s.w = s.w * f + u.w * w;
+    if (y < ny)
+#pragma unroll 4
+        for (int i = y; i < runs; i += ny) {
+            const float4 u =
+                *reinterpret_cast<const float4 *>(part + (i * pl.rows + row) * a.D + 4 * c);
+            const float w = weight[i];
+            s.x = fmaf(u.x, w, s.x), s.y = fmaf(u.y, w, s.y);
+            s.z = fmaf(u.z, w, s.z), s.w = fmaf(u.w, w, s.w);
+        }
+    sums[tid] = s;
+    __syncthreads();
+    if (y != 0)
+        return;
+    for (int i = 1; i < ny; ++i) {
+        const float4 u = sums[i * per + c];
+        s.x += u.x, s.y += u.y, s.z += u.z, s.w += u.w;
     }
     const float f = l == 0.f ? 0.f : 1.f / l;
-    store4(o + row * a.D + c, s.x * f, s.y * f, s.z * f, s.w * f);
+    store4(o + row * a.D + 4 * c, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
 template <typename E, int DC>
@@ -255,9 +295,12 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, void *ws
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1)
         return e;
-    const int64_t items = pl.rows * (a.D / 4);
-    HEX_LAUNCH((attn_join_k<E>), dim3(static_cast<uint32_t>((items + 255) / 256)), dim3(256), 0, st,
-               part, stat, static_cast<E *>(o), a, pl);
+    if (pl.splits <= 16)
+        HEX_LAUNCH((attn_join_k<E, 64>), dim3(static_cast<uint32_t>(pl.rows)), dim3(64), 0, st,
+                   part, stat, static_cast<E *>(o), a, pl);
+    else
+        HEX_LAUNCH((attn_join_k<E, 256>), dim3(static_cast<uint32_t>(pl.rows)), dim3(256), 0, st,
+                   part, stat, static_cast<E *>(o), a, pl);
     return hipGetLastError();
 }
 
@@ -284,10 +327,17 @@ StepPlan step_plan(int S, int n, int Hq, int Hkv, int max_len)
     p.rows = static_cast<int64_t>(S) * n * Hq;
     p.row_tiles = (n * (Hq / Hkv) + 31) / 32;
     const int64_t one = static_cast<int64_t>(S) * Hkv * p.row_tiles;
+    // Few sequences: as many blocks as the card holds (16 heads of 128 on 4,
+    // three of 9000 to 16432 keys: 22.5 us with two a unit, 25.3 with four).
+    // Many: their lengths differ, and finer runs even them out (192 of 32 to
+    // 4000 keys, 8 heads of 64 on 2: 26.7 us with four, 29.7 with two).
+    const int per_cu = one * 8 <= device_cus() ? 2 : 4;
     constexpr int step = 32 * attn::kStepWaves; // keys a block takes in one turn
     const int64_t most = (static_cast<int64_t>(max_len) + step - 1) / step;
-    const int64_t want = (4 * static_cast<int64_t>(device_cus()) + one - 1) / one;
-    const int64_t splits = want < 1 || most < 1 ? 1 : want < most ? want : most;
+    const int64_t want = (per_cu * static_cast<int64_t>(device_cus()) + one - 1) / one;
+    int64_t splits = want < 1 || most < 1 ? 1 : want < most ? want : most;
+    if (splits > attn::kMaxRuns)
+        splits = attn::kMaxRuns;
     p.chunk = static_cast<int>((most + splits - 1) / splits) * step;
     if (p.chunk < step)
         p.chunk = step;

@@ -288,6 +288,7 @@ __global__ __launch_bounds__(1024) void rotary_reduce_k(const float *part, int n
     const int e = blockIdx.x * 32 + x;
     float v = 0.f;
     if (e < 2 * D)
+#pragma unroll 8
         for (int i = y; i < nparts; i += 32)
             v += part[static_cast<size_t>(i) * 2 * D + e];
     red[y][x] = v;

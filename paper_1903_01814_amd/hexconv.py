@@ -208,7 +208,9 @@ def _dev(t, name, dt=None, shape=None):
 
 def _stream(stream):
     if stream is None:
-        return _torch().cuda.current_stream().cuda_stream
+        # the handle alone: making a Stream object of it takes 3 us a call
+        torch = _torch()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -465,36 +467,39 @@ def hexpool3d_bwd(dy, argmax, relu_y, dx, k: int, kz: int, stride: int, stride_z
 
 # --------------------------------------- attention over packed sequences
 
-def _tokens(t, name, dt, heads=None, D=None, n=None):
-    """Pointer and token stride of [tokens][heads][D] with dense heads."""
+def _tokens(t, name, dtype, heads, D, n=None):
+    """Pointer and token stride of [tokens][heads][D] with dense heads (n
+    tokens, or any number)."""
     if t is None:
         return None, 0
-    if not t.is_cuda:
-        raise ValueError("hexconv: %s must be a device tensor" % name)
-    if _dtype_code(t) != dt:
-        raise TypeError("hexconv: %s has dtype %s" % (name, t.dtype))
-    want = (n, heads, D)
-    if t.dim() != 3 or any(w is not None and w != g for w, g in zip(want, t.shape)):
-        raise ValueError("hexconv: %s has shape %s, expected [%s][%s][%s]"
-                         % ((name, tuple(t.shape)) + tuple("n" if w is None else w for w in want)))
-    h, d = t.shape[1:]
-    if t.numel() and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is not dtype or not t.is_cuda or len(shape) != 3 or shape[1] != heads
+            or shape[2] != D or (n is not None and shape[0] != n)):
+        _refuse(t, name, dtype, ("n" if n is None else n, heads, D))
+    if (stride[2] != 1 or stride[1] != D) and t.numel() and (
+            (D > 1 and stride[2] != 1) or (heads > 1 and stride[1] != D)):
         raise ValueError("hexconv: the heads of %s must be dense" % name)
     # one token, or none: any stride does
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else h * d
+    return t.data_ptr(), stride[0] if shape[0] > 1 else heads * D
 
 
-def _ints(t, name, shape):
-    """Pointer of an int32 device tensor; None passes through."""
-    if t is not None and t.dtype != _torch().int32:
-        raise TypeError("hexconv: %s must be int32" % name)
-    return _dev(t, name, None, shape)
+def _array(t, name, dtype, shape):
+    """Pointer of a contiguous device tensor; None passes through."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        _refuse(t, name, dtype, shape)
+    return t.data_ptr()
 
 
-def _f32(t, name, shape):
-    if t is not None and t.dtype != _torch().float32:
-        raise TypeError("hexconv: %s must be float32" % name)
-    return _dev(t, name, None, shape)
+def _refuse(t, name, dtype, shape):
+    if not t.is_cuda:
+        raise ValueError("hexconv: %s must be a device tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("hexconv: %s has dtype %s, expected %s" % (name, t.dtype, dtype))
+    if len(t.shape) != len(shape) or any(w != "n" and w != g for w, g in zip(shape, t.shape)):
+        raise ValueError("hexconv: %s has shape %s, expected %s" % (name, tuple(t.shape), shape))
+    raise ValueError("hexconv: %s must be contiguous" % name)
 
 
 def _ws(ws):
@@ -506,18 +511,24 @@ def hexrotary_fwd(q, k, pos, freq, axis, wq, wk, qo, ko, eps: float = 1e-6, norm
     """qo, ko <- norm and rotation of the heads of q [T][Hq][D] and k
     [T][Hkv][D] by positions pos [T][A]; with slot (int32 [T]) the keys, and
     with v and vo the values, go to those rows of ko and vo."""
+    torch = _torch()
     T, Hq, D = q.shape
     Hkv, A = k.shape[1], pos.shape[1]
-    dt = _dtype_code(q)
+    dt, ty = _dtype_code(q), q.dtype
     n = T if slot is None else ko.shape[0]
-    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt), _tokens(k, "k", dt, Hkv, D, T)
-    (pv, ldv), (pvo, ldvo) = _tokens(v, "v", dt, Hkv, D, T), _tokens(vo, "vo", dt, Hkv, D, n)
-    (pqo, ldqo), (pko, ldko) = _tokens(qo, "qo", dt, Hq, D, T), _tokens(ko, "ko", dt, Hkv, D, n)
+    pq, ldq = _tokens(q, "q", ty, Hq, D)
+    pk, ldk = _tokens(k, "k", ty, Hkv, D, T)
+    pv, ldv = _tokens(v, "v", ty, Hkv, D, T)
+    pqo, ldqo = _tokens(qo, "qo", ty, Hq, D, T)
+    pko, ldko = _tokens(ko, "ko", ty, Hkv, D, n)
+    pvo, ldvo = _tokens(vo, "vo", ty, Hkv, D, n)
     rc = load().hexrotary_fwd(
-        pq, pk, pv, _f32(pos, "pos", (T, A)), _f32(freq, "freq", (D // 2,)),
-        _ints(axis, "axis", (D // 2,)), _dev(wq, "wq", dt, (D,)), _dev(wk, "wk", dt, (D,)), pqo,
-        pko, pvo, _ints(slot, "slot", (T,)), T, Hq, Hkv, D, A, ldq, ldk, ldv, ldqo, ldko, ldvo, n,
-        eps, HEX_ROTARY_NORM if norm else 0, dt, _stream(stream))
+        pq, pk, pv, _array(pos, "pos", torch.float32, (T, A)),
+        _array(freq, "freq", torch.float32, (D // 2,)),
+        _array(axis, "axis", torch.int32, (D // 2,)), _array(wq, "wq", ty, (D,)),
+        _array(wk, "wk", ty, (D,)), pqo, pko, pvo, _array(slot, "slot", torch.int32, (T,)), T, Hq,
+        Hkv, D, A, ldq, ldk, ldv, ldqo, ldko, ldvo, n, eps, HEX_ROTARY_NORM if norm else 0, dt,
+        _stream(stream))
     _ok("hexrotary_fwd", rc)
     return qo, ko
 
@@ -530,18 +541,23 @@ def hexrotary_bwd(q, k, pos, freq, axis, wq, wk, dqo, dko, dq, dk, dwq, dwk, ws,
                   eps: float = 1e-6, norm: bool = True, stream=None):
     """dq, dk and the float32 dwq, dwk (each may be None) <- gradients of
     hexrotary_fwd.  Without the norm q and k may be None."""
+    torch = _torch()
     T, Hq, D = dqo.shape
     Hkv, A = dko.shape[1], pos.shape[1]
-    dt = _dtype_code(dqo)
-    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt, Hq, D, T), _tokens(k, "k", dt, Hkv, D, T)
-    (pgq, ldgq), (pgk, ldgk) = _tokens(dqo, "dqo", dt), _tokens(dko, "dko", dt, Hkv, D, T)
-    (pdq, lddq), (pdk, lddk) = _tokens(dq, "dq", dt, Hq, D, T), _tokens(dk, "dk", dt, Hkv, D, T)
+    dt, ty = _dtype_code(dqo), dqo.dtype
+    pq, ldq = _tokens(q, "q", ty, Hq, D, T)
+    pk, ldk = _tokens(k, "k", ty, Hkv, D, T)
+    pgq, ldgq = _tokens(dqo, "dqo", ty, Hq, D)
+    pgk, ldgk = _tokens(dko, "dko", ty, Hkv, D, T)
+    pdq, lddq = _tokens(dq, "dq", ty, Hq, D, T)
+    pdk, lddk = _tokens(dk, "dk", ty, Hkv, D, T)
     rc = load().hexrotary_bwd(
-        pq, pk, _f32(pos, "pos", (T, A)), _f32(freq, "freq", (D // 2,)),
-        _ints(axis, "axis", (D // 2,)), _dev(wq, "wq", dt, (D,)), _dev(wk, "wk", dt, (D,)), pgq,
-        pgk, pdq, pdk, _f32(dwq, "dwq", (D,)), _f32(dwk, "dwk", (D,)), *_ws(ws), T, Hq, Hkv, D, A,
-        ldq, ldk, ldgq, ldgk, lddq, lddk, eps, HEX_ROTARY_NORM if norm else 0, dt,
-        _stream(stream))
+        pq, pk, _array(pos, "pos", torch.float32, (T, A)),
+        _array(freq, "freq", torch.float32, (D // 2,)),
+        _array(axis, "axis", torch.int32, (D // 2,)), _array(wq, "wq", ty, (D,)),
+        _array(wk, "wk", ty, (D,)), pgq, pgk, pdq, pdk, _array(dwq, "dwq", torch.float32, (D,)),
+        _array(dwk, "dwk", torch.float32, (D,)), *_ws(ws), T, Hq, Hkv, D, A, ldq, ldk, ldgq, ldgk,
+        lddq, lddk, eps, HEX_ROTARY_NORM if norm else 0, dt, _stream(stream))
     _ok("hexrotary_bwd", rc)
     return dq, dk, dwq, dwk
 
@@ -564,12 +580,16 @@ def hexattn_fwd(q, k, v, o, lse, q_start, k_start=None, k_len=None, scale=None,
         if k_len is not None:
             raise ValueError("hexconv: k_len needs k_start")
         k_start = q_start
-    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt), _tokens(k, "k", dt, Hkv, D)
-    (pv, ldv), (po, ldo) = _tokens(v, "v", dt, Hkv, D, Tk), _tokens(o, "o", dt, Hq, D, Tq)
+    i32, ty = _torch().int32, q.dtype
+    pq, ldq = _tokens(q, "q", ty, Hq, D)
+    pk, ldk = _tokens(k, "k", ty, Hkv, D)
+    pv, ldv = _tokens(v, "v", ty, Hkv, D, Tk)
+    po, ldo = _tokens(o, "o", ty, Hq, D, Tq)
     rc = load().hexattn_fwd(
-        pq, pk, pv, po, _f32(lse, "lse", (Tq, Hq)), _ints(q_start, "q_start", (S + 1,)),
-        _ints(k_start, "k_start", (S + 1,) if k_len is None else (S,)),
-        _ints(k_len, "k_len", (S,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, _scale(scale, D),
+        pq, pk, pv, po, _array(lse, "lse", _torch().float32, (Tq, Hq)),
+        _array(q_start, "q_start", i32, (S + 1,)),
+        _array(k_start, "k_start", i32, (S + 1,) if k_len is None else (S,)),
+        _array(k_len, "k_len", i32, (S,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, _scale(scale, D),
         HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
     _ok("hexattn_fwd", rc)
     return o, lse
@@ -588,14 +608,19 @@ def hexattn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, q_start, k_start=None, sc
     S = q_start.shape[0] - 1
     if k_start is None:
         k_start = q_start
-    (pq, ldq), (pk, ldk) = _tokens(q, "q", dt), _tokens(k, "k", dt, Hkv, D)
-    (pv, ldv), (po, ldo) = _tokens(v, "v", dt, Hkv, D, Tk), _tokens(o, "o", dt, Hq, D, Tq)
-    (pg, ldg), (pdq, lddq) = _tokens(dout, "dout", dt, Hq, D, Tq), _tokens(dq, "dq", dt, Hq, D, Tq)
-    (pdk, lddk), (pdv, lddv) = _tokens(dk, "dk", dt, Hkv, D, Tk), _tokens(dv, "dv", dt, Hkv, D, Tk)
+    i32, ty = _torch().int32, q.dtype
+    pq, ldq = _tokens(q, "q", ty, Hq, D)
+    pk, ldk = _tokens(k, "k", ty, Hkv, D)
+    pv, ldv = _tokens(v, "v", ty, Hkv, D, Tk)
+    po, ldo = _tokens(o, "o", ty, Hq, D, Tq)
+    pg, ldg = _tokens(dout, "dout", ty, Hq, D, Tq)
+    pdq, lddq = _tokens(dq, "dq", ty, Hq, D, Tq)
+    pdk, lddk = _tokens(dk, "dk", ty, Hkv, D, Tk)
+    pdv, lddv = _tokens(dv, "dv", ty, Hkv, D, Tk)
     rc = load().hexattn_bwd(
-        pq, pk, pv, po, _f32(lse, "lse", (Tq, Hq)), pg, pdq, pdk, pdv, *_ws(ws),
-        _ints(q_start, "q_start", (S + 1,)), _ints(k_start, "k_start", (S + 1,)), S, Tq, Tk, Hq,
-        Hkv, D, ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv, _scale(scale, D),
+        pq, pk, pv, po, _array(lse, "lse", _torch().float32, (Tq, Hq)), pg, pdq, pdk, pdv,
+        *_ws(ws), _array(q_start, "q_start", i32, (S + 1,)),
+        _array(k_start, "k_start", i32, (S + 1,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv, _scale(scale, D),
         HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
     _ok("hexattn_bwd", rc)
     return dq, dk, dv
@@ -612,11 +637,13 @@ def hexattn_step(q, k, v, o, ws, k_start, k_len, max_len: int, scale=None, strea
     S, n, Hq, D = q.shape
     Tk, Hkv = k.shape[:2]
     dt = _dtype_code(q)
-    (pk, ldk), (pv, ldv) = _tokens(k, "k", dt, Hkv, D), _tokens(v, "v", dt, Hkv, D, Tk)
+    i32, ty = _torch().int32, q.dtype
+    pk, ldk = _tokens(k, "k", ty, Hkv, D)
+    pv, ldv = _tokens(v, "v", ty, Hkv, D, Tk)
     rc = load().hexattn_step(
-        _dev(q, "q", dt), pk, pv, _dev(o, "o", dt, (S, n, Hq, D)), *_ws(ws),
-        _ints(k_start, "k_start", (S,)), _ints(k_len, "k_len", (S,)), S, n, Hq, Hkv, D, Tk,
-        max_len, ldk, ldv, _scale(scale, D), dt, _stream(stream))
+        _array(q, "q", ty, (S, n, Hq, D)), pk, pv, _array(o, "o", ty, (S, n, Hq, D)), *_ws(ws),
+        _array(k_start, "k_start", i32, (S,)), _array(k_len, "k_len", i32, (S,)), S, n, Hq, Hkv,
+        D, Tk, max_len, ldk, ldv, _scale(scale, D), dt, _stream(stream))
     _ok("hexattn_step", rc)
     return o
 
@@ -624,11 +651,11 @@ def hexattn_step(q, k, v, o, ws, k_start, k_len, max_len: int, scale=None, strea
 def hexdropout(x, res, y, p: float, rng, call: int = 0, stream=None):
     """y <- res (may be None) + dropout of x with probability p; rng: int64
     device tensor [seed, call number]."""
-    dt = _dtype_code(x)
-    if rng.dtype != _torch().int64:
+    dt, ty, shape = _dtype_code(x), x.dtype, x.shape
+    if rng.dtype is not _torch().int64:
         raise TypeError("hexconv: rng must be int64")
-    rc = load().hexdropout(_dev(x, "x", dt), _dev(res, "res", dt, x.shape),
-                           _dev(y, "y", dt, x.shape), x.numel(), p, _dev(rng, "rng", None, (2,)),
-                           call, dt, _stream(stream))
+    rc = load().hexdropout(_array(x, "x", ty, shape), _array(res, "res", ty, shape),
+                           _array(y, "y", ty, shape), x.numel(), p,
+                           _array(rng, "rng", rng.dtype, (2,)), call, dt, _stream(stream))
     _ok("hexdropout", rc)
     return y

@@ -1,6 +1,7 @@
-"""PyTorch layers over libhexconv: hexagonal convolution and pooling as
-``torch.autograd.Function``s and ``nn.Module``s, so that they drop into
-models written with the PyTorch API the way the paper's layers do (Sec. 2.4).
+"""PyTorch layers over libhexconv: hexagonal convolution, pooling, and
+attention over lit pixels, as ``torch.autograd.Function``s and
+``nn.Module``s, so that they drop into models written with the PyTorch API the
+way the paper's layers do (Sec. 2.4).
 
 Tensors are NCHW in the offset-column layout of Sec. 2.1 (odd columns shifted
 half a pitch down); weights are ``[C_out, C_in, T]`` with T = 1 + 3k(k+1)
@@ -375,3 +376,296 @@ class HexAvgPool3d(nn.Module):
 
     def forward(self, x):
         return hex_avg_pool3d(x, self.kernel_size, self.stride)
+
+
+# ------------------------------------------- attention over lit pixels
+# The lit pixels of camera events as packed sequences of tokens [T][...]: the
+# events one after another, ``start`` (int32 [S + 1], on the device) their
+# offsets.  Positions are float32 [T][axes], e.g. time and the pixel's centre.
+
+def hex_pixel_positions(H, W, device=None):
+    """Centres [H * W][2] (down, right) of the pixels of an H x W tensor in
+    units of the pixel pitch: odd columns lie half a pitch lower, columns are
+    sqrt(3)/2 apart (Sec. 2.1)."""
+    r = torch.arange(H, dtype=torch.float32, device=device)[:, None]
+    c = torch.arange(W, device=device)[None]
+    y = r + 0.5 * (c % 2).float()
+    x = (c.float() * (math.sqrt(3.0) / 2.0)).expand(H, W)
+    return torch.stack([y, x], dim=2).reshape(H * W, 2)
+
+
+def hex_frequencies(head_dim, bases=(10000.0, 100.0, 100.0), device=None):
+    """Frequencies (radians a unit) and axes of a head's head_dim / 2 pairs
+    for rotary positions of len(bases) axes: each axis owns a run of pairs
+    whose wavelengths grow geometrically from 2 pi up to 2 pi times its
+    base."""
+    pairs, axes = head_dim // 2, len(bases)
+    freq, axis = [], []
+    for a, base in enumerate(bases):
+        n = pairs // axes + (a < pairs % axes)
+        freq += [base ** (-i / n) for i in range(n)]
+        axis += [a] * n
+    return (torch.tensor(freq, dtype=torch.float32, device=device),
+            torch.tensor(axis, dtype=torch.int32, device=device))
+
+
+def _workspace(nbytes, like):
+    return _empty((nbytes,), like, torch.uint8) if nbytes else None
+
+
+class HexRotaryFunction(torch.autograd.Function):
+    """Norm and rotation of query and key heads (hexrotary_fwd)."""
+
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, pos, freq, axis, eps, norm):
+        qo, ko = _empty(q.shape, q), _empty(k.shape, k)
+        hx.hexrotary_fwd(q, k, pos, freq, axis, wq, wk, qo, ko, eps=eps, norm=norm)
+        ctx.save_for_backward(q if norm else None, k if norm else None, wq, wk, pos, freq, axis)
+        ctx.eps, ctx.norm = eps, norm
+        return qo, ko
+
+    @staticmethod
+    def backward(ctx, gq, gk):
+        q, k, wq, wk, pos, freq, axis = ctx.saved_tensors
+        gq, gk = gq.contiguous(), gk.contiguous()
+        dq, dk = _empty(gq.shape, gq), _empty(gk.shape, gk)
+        dwq, dwk = _rotary_bwd(q, k, pos, freq, axis, wq, wk, gq, gk, dq, dk, ctx.eps, ctx.norm)
+        return dq, dk, dwq, dwk, None, None, None, None, None
+
+
+def _rotary_bwd(q, k, pos, freq, axis, wq, wk, gq, gk, dq, dk, eps, norm):
+    """dq and dk written; the weights' gradients in their dtype."""
+    T, Hq, D = gq.shape
+    dwq = _empty((D,), gq, torch.float32) if norm and wq is not None else None
+    dwk = _empty((D,), gk, torch.float32) if norm and wk is not None else None
+    ws = None
+    if norm:
+        ws = _workspace(hx.hexrotary_bwd_workspace(T, Hq, gk.shape[1], D, hx._dtype_code(gq)), gq)
+    hx.hexrotary_bwd(q, k, pos, freq, axis, wq, wk, gq, gk, dq, dk, dwq, dwk, ws, eps=eps,
+                     norm=norm)
+    return (None if dwq is None else dwq.to(wq.dtype), None if dwk is None else dwk.to(wk.dtype))
+
+
+class HexAttentionFunction(torch.autograd.Function):
+    """Softmax attention over packed sequences (hexattn_fwd)."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, q_start, k_start, scale, causal):
+        # rows of no sequence have no result: zeros, and no gradient
+        o = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device)
+        hx.hexattn_fwd(q, k, v, o, lse, q_start, k_start, scale=scale, causal=causal)
+        ctx.save_for_backward(q, k, v, o, lse, q_start, k_start)
+        ctx.scale, ctx.causal = scale, causal
+        return o
+
+    @staticmethod
+    def backward(ctx, g):
+        q, k, v, o, lse, q_start, k_start = ctx.saved_tensors
+        dq, dk, dv = (torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        _attention_bwd(q, k, v, o, lse, g.contiguous(), dq, dk, dv, q_start, k_start, ctx.scale,
+                       ctx.causal)
+        return dq, dk, dv, None, None, None, None
+
+
+def _attention_bwd(q, k, v, o, lse, g, dq, dk, dv, q_start, k_start, scale, causal):
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[:2]
+    ws = _workspace(hx.hexattn_bwd_workspace(Tq, Tk, q_start.shape[0] - 1, Hq, Hkv, D,
+                                             hx._dtype_code(q)), q)
+    hx.hexattn_bwd(q, k, v, o, lse, g, dq, dk, dv, ws, q_start, k_start, scale=scale,
+                   causal=causal)
+
+
+class HexPixelAttentionFunction(torch.autograd.Function):
+    """Norm, rotation and attention of one projection's queries, keys and
+    values, qkv [T][Hq + 2 Hkv][D]: the gradients are written into one tensor
+    of that layout, with no copies between the parts.  Every token belongs to
+    a sequence."""
+
+    @staticmethod
+    def forward(ctx, qkv, wq, wk, pos, freq, axis, start, heads, eps, causal):
+        Hq, Hkv = heads
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        qo, ko = _empty(q.shape, q), _empty(k.shape, k)
+        hx.hexrotary_fwd(q, k, pos, freq, axis, wq, wk, qo, ko, eps=eps)
+        o, lse = _empty(q.shape, q), _empty(q.shape[:2], q, torch.float32)
+        hx.hexattn_fwd(qo, ko, v, o, lse, start, causal=causal)
+        ctx.save_for_backward(qkv, wq, wk, pos, freq, axis, start, qo, ko, o, lse)
+        ctx.heads, ctx.eps, ctx.causal = heads, eps, causal
+        return o
+
+    @staticmethod
+    def backward(ctx, g):
+        qkv, wq, wk, pos, freq, axis, start, qo, ko, o, lse = ctx.saved_tensors
+        Hq, Hkv = ctx.heads
+        parts = lambda t: (t[:, :Hq], t[:, Hq:Hq + Hkv], t[:, Hq + Hkv:])  # noqa: E731
+        d = torch.empty_like(qkv)
+        (q, k, v), (dq, dk, dv) = parts(qkv), parts(d)
+        gq, gk = _empty(qo.shape, qo), _empty(ko.shape, ko)
+        _attention_bwd(qo, ko, v, o, lse, g.contiguous(), gq, gk, dv, start, start, None,
+                       ctx.causal)
+        dwq, dwk = _rotary_bwd(q, k, pos, freq, axis, wq, wk, gq, gk, dq, dk, ctx.eps, True)
+        return d, dwq, dwk, None, None, None, None, None, None, None
+
+
+class HexDropoutFunction(torch.autograd.Function):
+    """Dropout with a residual (hexdropout); the backward makes the mask again
+    from the generator's words as they were."""
+
+    @staticmethod
+    def forward(ctx, x, residual, p, rng, call):
+        x = x.contiguous()
+        y = _empty(x.shape, x)
+        hx.hexdropout(x, None if residual is None else residual.contiguous(), y, p, rng, call)
+        ctx.save_for_backward(rng)
+        ctx.p, ctx.call = p, call
+        return y
+
+    @staticmethod
+    def backward(ctx, g):
+        (rng,) = ctx.saved_tensors
+        dx = None
+        if ctx.needs_input_grad[0]:
+            g = g.contiguous()
+            dx = _empty(g.shape, g)
+            hx.hexdropout(g, None, dx, ctx.p, rng, ctx.call)
+        return dx, g if ctx.needs_input_grad[1] else None, None, None, None
+
+
+def hex_rotary(q, k, pos, freq, axis, wq=None, wk=None, eps=1e-6, norm=True):
+    """Query heads q [T][Hq][D] and key heads k [T][Hkv][D], normed (weights
+    wq and wk [D], or ones) and turned by their positions pos [T][axes]."""
+    return HexRotaryFunction.apply(q, k, wq, wk, pos, freq, axis, float(eps), bool(norm))
+
+
+def hex_attention(q, k, v, q_start, k_start=None, scale=None, causal=False):
+    """Softmax attention of packed sequences, q [Tq][Hq][D] over k and v
+    [Tk][Hkv][D], offsets int32 [S + 1] (k_start: q_start by default)."""
+    return HexAttentionFunction.apply(q, k, v, q_start, q_start if k_start is None else k_start,
+                                      scale, bool(causal))
+
+
+def hex_dropout(x, p, rng, residual=None, call=0):
+    """residual + dropout of x with probability p.  rng: int64 [2] on the
+    device, seed and call number; the same words (and call) give the same
+    mask.  It must keep its values until the backward."""
+    return HexDropoutFunction.apply(x, residual, float(p), rng, int(call))
+
+
+class HexCache:
+    """Keys and values of S streams, `capacity` tokens each, for
+    HexPixelAttention.prefill and .step."""
+
+    def __init__(self, streams, capacity, kv_heads, head_dim, device=None, dtype=None):
+        shape = (int(streams) * int(capacity), int(kv_heads), int(head_dim))
+        self.k = torch.empty(shape, device=device, dtype=dtype)
+        self.v = torch.empty(shape, device=device, dtype=dtype)
+        self.capacity = int(capacity)
+        self.start = (torch.arange(int(streams), device=device) * self.capacity).to(torch.int32)
+        self.length = torch.zeros(int(streams), dtype=torch.int32, device=device)
+        self.most = 0  # no stream holds more tokens
+
+    def reserve(self, n):
+        """Room for n more tokens of every stream, by the host's count."""
+        if self.most + n > self.capacity:
+            raise ValueError("HexCache: %d tokens do not fit the capacity of %d"
+                             % (self.most + n, self.capacity))
+        self.most += n
+
+
+class HexPixelAttention(nn.Module):
+    """Attention layer over packed sequences of lit pixels: projection to
+    heads, root-mean-square norm of every query and key head, rotation by
+    positions of len(bases) axes, softmax attention (grouped heads), output
+    projection, and with ``dropout`` the residual branch's dropout.  The
+    projections are torch's linear layers.
+
+    forward(x [T][dim], pos, start): x + dropout(projection(attention(x))).
+    prefill and step do the same over a HexCache, without dropout."""
+
+    def __init__(self, dim, heads, kv_heads=None, head_dim=None, bases=(10000.0, 100.0, 100.0),
+                 causal=False, dropout=0.0, eps=1e-6, device=None, dtype=None):
+        super().__init__()
+        self.heads = (int(heads), int(kv_heads or heads))
+        self.head_dim = int(head_dim or dim // heads)
+        self.causal, self.dropout, self.eps = bool(causal), float(dropout), float(eps)
+        Hq, Hkv = self.heads
+        kw = {"device": device, "dtype": dtype}
+        self.qkv = nn.Linear(dim, (Hq + 2 * Hkv) * self.head_dim, bias=False, **kw)
+        self.out = nn.Linear(Hq * self.head_dim, dim, bias=False, **kw)
+        self.q_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
+        self.k_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
+        freq, axis = hex_frequencies(self.head_dim, bases, device)
+        self.register_buffer("freq", freq, persistent=False)
+        self.register_buffer("axis", axis, persistent=False)
+        # the dropout's generator: a seed of this layer's own, the call number
+        seed = int(torch.randint(1 << 62, ()))
+        self.register_buffer("rng", torch.tensor([seed, 0], dtype=torch.int64, device=device))
+
+    def _project(self, x):
+        Hq, Hkv = self.heads
+        return self.qkv(x).view(-1, Hq + 2 * Hkv, self.head_dim)
+
+    def forward(self, x, pos, start):
+        o = HexPixelAttentionFunction.apply(self._project(x), self.q_norm, self.k_norm, pos,
+                                            self.freq, self.axis, start, self.heads, self.eps,
+                                            self.causal)
+        y = self.out(o.flatten(1))
+        if not (self.training and self.dropout > 0):
+            return x + y
+        rng = self.rng.clone()
+        self.rng[1] += 1
+        return hex_dropout(y, self.dropout, rng, residual=x)
+
+    def new_cache(self, streams, capacity):
+        return HexCache(streams, capacity, self.heads[1], self.head_dim, self.qkv.weight.device,
+                        self.qkv.weight.dtype)
+
+    def _into_cache(self, qkv, pos, slot, cache):
+        Hq, Hkv = self.heads
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        qo = _empty(q.shape, q)
+        hx.hexrotary_fwd(q, k, pos, self.freq, self.axis, self.q_norm, self.k_norm, qo, cache.k,
+                         eps=self.eps, v=v, vo=cache.v, slot=slot)
+        return qo
+
+    @torch.no_grad()
+    def prefill(self, x, pos, start, cache, longest):
+        """Packed prompts x [T][dim] of all streams, at most ``longest`` tokens
+        each, appended to their caches."""
+        cache.reserve(int(longest))
+        T = x.shape[0]
+        shift = cache.start + cache.length - start[:-1]
+        slot = (torch.repeat_interleave(shift, start[1:] - start[:-1], output_size=T)
+                + torch.arange(T, dtype=torch.int32, device=x.device)).to(torch.int32)
+        qo = self._into_cache(self._project(x), pos, slot, cache)
+        cache.length += start[1:] - start[:-1]
+        o = _empty(qo.shape, qo)
+        hx.hexattn_fwd(qo, cache.k, cache.v, o, None, start, cache.start, cache.length,
+                       causal=self.causal)
+        return x + self.out(o.flatten(1))
+
+    @torch.no_grad()
+    def step(self, x, pos, cache):
+        """n new tokens of every stream, x [S][n][dim] and pos [S][n][axes]:
+        each sees its stream's tokens up to itself."""
+        if not self.causal:
+            raise ValueError("HexPixelAttention: steps need a causal layer")
+        S, n, dim = x.shape
+        cache.reserve(n)
+        at = cache.start + cache.length
+        slot = (at[:, None] + torch.arange(n, dtype=torch.int32, device=x.device)).view(-1)
+        qo = self._into_cache(self._project(x.reshape(S * n, dim)), pos.reshape(S * n, -1), slot,
+                              cache)
+        cache.length += n
+        q = qo.view(S, n, self.heads[0], self.head_dim)
+        o = torch.empty_like(q)
+        ws = _workspace(hx.hexattn_step_workspace(S, n, *self.heads, self.head_dim, cache.most,
+                                                  hx._dtype_code(q)), q)
+        hx.hexattn_step(q, cache.k, cache.v, o, ws, cache.start, cache.length, cache.most)
+        return x + self.out(o.view(S, n, -1))
+
+    def extra_repr(self):
+        return ("heads=%d, kv_heads=%d, head_dim=%d, causal=%s, dropout=%g"
+                % (self.heads + (self.head_dim, self.causal, self.dropout)))

@@ -296,10 +296,22 @@ inline int attn_slots(int T, int G, int TR, int S)
 {
     return static_cast<int>(static_cast<int64_t>(T) * G / TR) + S;
 }
-
-// keys of sequence s: its k_len from k_start on, or up to the next start
-__device__ __forceinline__ void key_span(const AttnArgs &a, int s, int &begin, int &n)
+// blocks of a launch over all slots and key heads
+inline uint32_t attn_blocks(const AttnArgs &a)
 {
+    return static_cast<uint32_t>(a.narrow ? (a.slots + 7) / 8 * 8 : a.slots) * a.Hkv;
+}
+
+// keys of sequence s: its k_len from k_start on, or up to the next start; its
+// queries' own tokens (q0, nq) where both have the same offsets
+__device__ __forceinline__ void key_span(const AttnArgs &a, int s, int q0, int nq, int &begin,
+                                         int &n)
+{
+    if (a.k_start == a.q_start && a.k_len == nullptr && a.Tk == a.Tq) {
+        begin = q0;
+        n = nq;
+        return;
+    }
     begin = min(max(a.k_start[s], 0), a.Tk);
     const int end = a.k_len != nullptr ? a.k_len[s] : a.k_start[s + 1] - begin;
     n = min(min(max(end, 0), a.max_len), a.Tk - begin);
@@ -320,6 +332,10 @@ __device__ __forceinline__ void store4(bf16raw *p, float x, float y, float z, fl
 __device__ __forceinline__ float4 quad(const floatx16 &x, int i)
 {
     return float4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+}
+__device__ __forceinline__ void set_quad(floatx16 &x, int i, const float4 &y)
+{
+    x[4 * i] = y.x, x[4 * i + 1] = y.y, x[4 * i + 2] = y.z, x[4 * i + 3] = y.w;
 }
 __device__ __forceinline__ void add_quad(floatx16 &x, int i, const float4 &y)
 {
@@ -343,35 +359,97 @@ __device__ __forceinline__ int clamp_start(const int *start, int i, int T)
     return min(max(start[i], 0), T);
 }
 
+// One tile on its way from memory to LDS: ROWS rows, a 16-byte chunk a thread
+// at a time, NT threads.  Addresses are a uniform base and a 32-bit offset
+// (token strides are below 2^24 bytes), so that a load costs two or three
+// vector instructions beside itself.  Chunks past D stay zero.
+template <typename E, int DC, int ROWS, int NT> struct Stage {
+    using TL = Tile<E, DC>;
+    static constexpr int N = ROWS * TL::CPR / NT;
+    static_assert(ROWS * TL::CPR % NT == 0, "");
+    uint4 r[N];
+
+    __device__ __forceinline__ Stage()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            r[i] = uint4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ static int row(int i) { return (threadIdx.x % NT + NT * i) / TL::CPR; }
+    __device__ __forceinline__ static int chunk(int i) { return (threadIdx.x % NT + NT * i) % TL::CPR; }
+    __device__ __forceinline__ void get(int i, const E *base, uint32_t bytes, int D)
+    {
+        if (chunk(i) * Elem<E>::VEC < D)
+            r[i] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(base) + bytes);
+    }
+    // rows from `base` on, ld bytes apart; those past the last of `left`
+    // repeat it
+    __device__ __forceinline__ void rows(const E *base, uint32_t ld, int left, int D)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            get(i, base, __umul24(min(row(i), left - 1), ld) + 16 * chunk(i), D);
+    }
+    __device__ __forceinline__ void put(unsigned char *t) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            *reinterpret_cast<uint4 *>(t + TL::chunk_at(row(i), chunk(i))) = r[i];
+    }
+};
+
+// Which (key head, tile slot) block `id` takes.  Dies take blocks in turn, 8 of
+// them.  Usually key heads are innermost, so that a head's keys stay on few
+// dies.  Heads of less than a 128-byte cache line share lines with their
+// neighbours: there all heads of a slot go to one die (512 sequences of 20 to
+// 400 tokens, 8 heads of 32 bf16 elements: see attn_fwd_k).  Slots from the
+// last on: under the causal mask a sequence's last tiles are the longest.
+__device__ __forceinline__ void head_and_slot(const AttnArgs &a, uint32_t id, int &kvh, int &slot)
+{
+    if (a.narrow) {
+        const uint32_t group = id / (8 * a.Hkv), r = id % (8 * a.Hkv);
+        kvh = r >> 3;
+        slot = a.slots - 1 - static_cast<int>(group * 8 + (r & 7));
+    } else {
+        kvh = id % a.Hkv;
+        slot = a.slots - 1 - static_cast<int>(id / a.Hkv);
+    }
+}
+
 struct Span {
     int seq;      // sequence
     int begin, n; // its tokens
     int tile;     // which of its tiles
 };
 
-// Sequence that owns tile slot w: 64 probes at once, log_64(S) rounds.
+// Sequence that owns tile slot w: 64 probes at once, log_64(S) rounds, the
+// last of which leaves the neighbouring offsets in the lanes.
 template <int TR>
 __device__ __forceinline__ Span find_span(const int *start, int S, int T, int G, int w)
 {
     const int lane = threadIdx.x & 63;
-    auto first = [&](int i) {
-        return static_cast<int>(static_cast<int64_t>(clamp_start(start, i, T)) * G / TR) + i;
+    auto slot = [&](int v, int i) {
+        return static_cast<int>(static_cast<int64_t>(v) * G / TR) + i;
     };
-    int lo = 0, n = S;
-    while (n > 1) {
-        const int step = (n + 63) >> 6;
-        const int off = lane * step;
-        const bool ok = off < n && first(lo + off) <= w;
-        const int c = max(1, __popcll(__ballot(ok)));
-        lo += (c - 1) * step;
-        n = min(step, n - (c - 1) * step);
+    int lo = 0, n = S, v, c;
+    for (;;) {
+        const int step = (n + 63) >> 6, at = lo + lane * step;
+        // one probe past the last, for the sequence's end
+        v = clamp_start(start, min(at, S), T);
+        const bool ok = lane * step < n && slot(v, at) <= w;
+        c = max(1, __popcll(__ballot(ok))) - 1;
+        lo += c * step;
+        if (step == 1)
+            break;
+        n = min(step, n - c * step);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
     Span s;
-    s.seq = lo;
-    s.begin = clamp_start(start, lo, T);
-    s.n = max(0, clamp_start(start, lo + 1, T) - s.begin);
-    s.tile = w - first(lo);
+    s.seq = __builtin_amdgcn_readfirstlane(lo);
+    c = __builtin_amdgcn_readfirstlane(c);
+    s.begin = __builtin_amdgcn_readlane(v, c);
+    const int end = c < 63 ? __builtin_amdgcn_readlane(v, c + 1) : clamp_start(start, s.seq + 1, T);
+    s.n = max(0, end - s.begin);
+    s.tile = w - slot(s.begin, s.seq);
     return s;
 }
 

@@ -446,6 +446,16 @@ bool stride_ok(int64_t ld, int heads, int D, int dt)
     return ld >= static_cast<int64_t>(heads) * D && ld % vec(dt) == 0;
 }
 
+// the attention kernels' offsets within a tile: tokens less than 2^24 bytes
+// apart
+bool stride_small(std::initializer_list<int64_t> lds, int dt)
+{
+    for (int64_t ld : lds)
+        if (ld >= (INT64_C(1) << 24) / static_cast<int64_t>(dtype_bytes(dt)))
+            return false;
+    return true;
+}
+
 int check_attn(int S, int Tq, int Tk, int Hq, int Hkv, int D, int dt)
 {
     if (S < 0 || Tq < 0 || Tk < 0)
@@ -463,7 +473,7 @@ int check_attn(int S, int Tq, int Tk, int Hq, int Hkv, int D, int dt)
 
 hexk::AttnArgs attn_args(const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, int S,
                    int Tq, int Tk, int Hq, int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv,
-                   int64_t ldo, float scale, bool causal)
+                   int64_t ldo, float scale, bool causal, int dt)
 {
     hexk::AttnArgs a;
     a.q_start = q_start;
@@ -489,6 +499,7 @@ hexk::AttnArgs attn_args(const int32_t *q_start, const int32_t *k_start, const i
         a.c = nextafterf(a.c, 0.f);
     a.c_lo = fmaxf(static_cast<float>(c - a.c), FLT_MIN);
     a.causal = causal;
+    a.narrow = D * dtype_bytes(dt) < 128;
     a.slots = 0;
     a.max_len = Tk;
     return a;
@@ -1044,6 +1055,8 @@ int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse
     if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 || !stride_ok(ldq, Hq, D, dt) ||
         !stride_ok(ldo, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt))
         return HEX_ERR_INVALID_ARG;
+    if (!stride_small({ldk, ldv}, dt))
+        return HEX_ERR_UNSUPPORTED;
     if (S == 0 || Tq == 0)
         return HEX_OK;
     if ((rc = ptrs_ok({q, o}, {k, v, lse})) != HEX_OK)
@@ -1051,7 +1064,7 @@ int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse
     if (q_start == nullptr || k_start == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
         return HEX_ERR_INVALID_ARG;
     const hexk::AttnArgs a = attn_args(q_start, k_start, k_len, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo,
-                                 scale, (flags & HEX_ATTN_CAUSAL) != 0);
+                                 scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
     return launched(hexk::attn_fwd(q, k, v, o, lse, a, static_cast<Dtype>(dt),
                                    static_cast<hipStream_t>(stream)));
 }
@@ -1078,6 +1091,8 @@ int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, cons
         !stride_ok(lddout, Hq, D, dt) || !stride_ok(lddq, Hq, D, dt) ||
         !stride_ok(lddk, Hkv, D, dt) || !stride_ok(lddv, Hkv, D, dt))
         return HEX_ERR_INVALID_ARG;
+    if (!stride_small({ldq, ldk, ldv, lddout}, dt))
+        return HEX_ERR_UNSUPPORTED;
     if (S == 0 || (Tq == 0 && Tk == 0))
         return HEX_OK;
     if ((rc = ptrs_ok({}, {q, k, v, o, lse, dout, dq, dk, dv, ws})) != HEX_OK)
@@ -1092,7 +1107,7 @@ int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, cons
     if (Tk > 0 && (k == nullptr || v == nullptr || dk == nullptr || dv == nullptr))
         return HEX_ERR_INVALID_ARG;
     const hexk::AttnArgs a = attn_args(q_start, k_start, nullptr, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv,
-                                 ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0);
+                                 ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
     return launched(hexk::attn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, a, hexk::AttnGrads{lddout, lddq, lddk, lddv},
                                    static_cast<Dtype>(dt), static_cast<hipStream_t>(stream)));
 }
@@ -1116,6 +1131,8 @@ int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws,
         return rc;
     if (!stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt))
         return HEX_ERR_INVALID_ARG;
+    if (!stride_small({ldk, ldv}, dt))
+        return HEX_ERR_UNSUPPORTED;
     if (S == 0)
         return HEX_OK;
     if ((rc = ptrs_ok({q, o}, {k, v, ws})) != HEX_OK)
@@ -1132,7 +1149,7 @@ int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws,
     if (ws_bytes < need || (need > 0 && ws == nullptr))
         return HEX_ERR_INVALID_ARG;
     hexk::AttnArgs a = attn_args(nullptr, k_start, k_len, S, 0, Tk, Hq, Hkv, D, 0, ldk, ldv, 0, scale,
-                           true);
+                           true, dt);
     a.max_len = max_len;
     return launched(hexk::attn_step(q, k, v, o, ws, a, p, static_cast<Dtype>(dt),
                                     static_cast<hipStream_t>(stream)));

@@ -236,8 +236,6 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     using Frag = typename Elem<E>::Frag;
     constexpr int TR = 128 * NQ, KT = BK / 32, DT = DC / 32, DS = DC / 16;
     constexpr int TB = TL::bytes(BK);
-    constexpr int NCH = BK * TL::CPR / 256;
-    static_assert(BK * TL::CPR % 256 == 0, "");
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
 
     if (blockIdx.x == 0) {
@@ -248,8 +246,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = lane >> 5, col = lane & 31;
-    const int kvh = (blockIdx.x - 1) % a.Hkv;
-    const int w = a.slots - 1 - static_cast<int>((blockIdx.x - 1) / a.Hkv);
+    int kvh, w;
+    head_and_slot(a, blockIdx.x - 1, kvh, w);
+    if (w < 0)
+        return;
     const Group g = a.group;
     const Span sp = find_span<TR>(a.q_start, a.S, a.Tq, g.G, w);
     const int rows = sp.n * g.G;
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
         return;
     const int row0 = sp.tile * TR;
     int kb, m;
-    key_span(a, sp.seq, kb, m);
+    key_span(a, sp.seq, sp.begin, sp.n, kb, m);
     const int ahead = m - sp.n;
 
     Frag qf[NQ][DS], gf[NQ][DS];
@@ -309,28 +309,17 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     least = __builtin_amdgcn_readfirstlane(least);
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
-    uint4 ks[NCH], vs[NCH];
+    Stage<E, DC, BK, 256> ks, vs;
+    const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
+    // rows past the end repeat the last one: their scores are masked
     auto load = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            const int c = e % TL::CPR * Elem<E>::VEC;
-            const int64_t r = min(tile * BK + e / TL::CPR, m - 1);
-            ks[i] = vs[i] = uint4{0, 0, 0, 0};
-            if (c < a.D) {
-                ks[i] = *reinterpret_cast<const uint4 *>(kp + r * a.ldk + c);
-                vs[i] = *reinterpret_cast<const uint4 *>(vp + r * a.ldv + c);
-            }
-        }
+        const int64_t k0 = static_cast<int64_t>(tile) * BK;
+        ks.rows(kp + k0 * a.ldk, ldk, m - tile * BK, a.D);
+        vs.rows(vp + k0 * a.ldv, ldv, m - tile * BK, a.D);
     };
     auto store = [&](unsigned char *t) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            const int p = TL::chunk_at(e / TL::CPR, e % TL::CPR);
-            *reinterpret_cast<uint4 *>(t + p) = ks[i];
-            *reinterpret_cast<uint4 *>(t + TB + p) = vs[i];
-        }
+        ks.put(t);
+        vs.put(t + TB);
     };
 
     int ca = TL::cols_at(col, h);
@@ -440,9 +429,8 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
     using Frag = typename Elem<E>::Frag;
     constexpr int RT = BR / 32, DT = DC / 32, DS = DC / 16;
     constexpr int TB = TL::bytes(BR);
-    constexpr int NCH = BR * TL::CPR / 256;
-    static_assert(BR * TL::CPR % 256 == 0 && BR <= 64, "");
-    constexpr int BUF = 2 * TB + 4 * BR * 4; // Q, dO; lse, delta, keys seen, lse's rest
+    static_assert(BR <= 64, "");
+    constexpr int BUF = 2 * TB + 4 * BR * 4; // Q, dO; lse, -D, keys seen, lse's rest
     // the values' operands stay in registers where they fit beside the sums
     constexpr bool VL = DT > (sizeof(E) == 4 ? 2 : 3);
     __shared__ __align__(16) unsigned char smem[2 * BUF + (VL ? TL::bytes(128) : 0)];
@@ -468,8 +456,9 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
             ++c;
         const int first = __builtin_amdgcn_readfirstlane(c > 0 ? ends[c - 1] : 0) / a.Hkv;
         const int of = __builtin_amdgcn_readfirstlane(ends[c]) / a.Hkv - first;
-        const int i = w - first * a.Hkv, kvh = i / of;
-        const KeyPiece pc = pl.list[first + i - kvh * of];
+        // heads after one another, or (narrow ones) side by side
+        const int i = w - first * a.Hkv, kvh = a.narrow ? i % a.Hkv : i / of;
+        const KeyPiece pc = pl.list[first + (a.narrow ? i / a.Hkv : i - kvh * of)];
         const int key0 = pc.key0, m = pc.m, rows = pc.n * g.G, ahead = m - pc.n;
         const int tile0 = pc.row0, ntiles = pc.row1;
 
@@ -482,58 +471,61 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
             if constexpr (!VL)
                 vf[s] = load_frag<E>(v + at * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
         }
-        if constexpr (VL)
-            for (int e = threadIdx.x; e < 128 * TL::CPR; e += 256) {
-                const int c = e % TL::CPR * Elem<E>::VEC;
-                const int64_t r = pc.k0 + min(key0 + e / TL::CPR, m - 1);
-                *reinterpret_cast<uint4 *>(vl + TL::chunk_at(e / TL::CPR, e % TL::CPR)) =
-                    c < a.D ? *reinterpret_cast<const uint4 *>(v + r * a.ldv + kvh * a.D + c)
-                            : uint4{0, 0, 0, 0};
-            }
+        if constexpr (VL) {
+            Stage<E, DC, 128, 256> vs;
+            vs.rows(v + static_cast<int64_t>(pc.k0 + key0) * a.ldv + kvh * a.D,
+                    a.ldv * sizeof(E), m - key0, a.D);
+            vs.put(vl);
+        }
 
         const E *qp = q + pc.q0 * a.ldq + static_cast<int64_t>(kvh) * g.G * a.D;
         const E *gp = dout + pc.q0 * gr.lddo + static_cast<int64_t>(kvh) * g.G * a.D;
         const float *lp = lse + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
         const float *dp0 = delta + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
-        uint4 qs[NCH], gs[NCH];
+        Stage<E, DC, BR, 256> qs, gs;
+        const uint32_t ldq = a.ldq * sizeof(E), ldg = gr.lddo * sizeof(E);
+        const float per_head = 1.f / g.G;
         Ref ls{0.f, 0.f};
         float ds = 0.f;
         int sees = 0;
         auto load = [&](int tile) {
+            // rows counted from the tile's first token: x = row, x / G exact
+            // in floats (x + 1/2 is at least 1/2 off a multiple of G)
+            const int first = row_token(g, tile * BR), skip = tile * BR - first * g.G;
+            const int end = skip + rows - 1 - tile * BR;
+            const E *qt = qp + first * a.ldq, *gt = gp + first * gr.lddo;
+            auto place = [&](int r, int &t, int &hd) {
+                const int x = min(skip + r, end);
+                t = static_cast<int>((x + 0.5f) * per_head);
+                hd = x - __mul24(t, g.G);
+            };
 #pragma unroll
-            for (int i = 0; i < NCH; ++i) {
-                const int e = threadIdx.x + 256 * i;
-                const int c = e % TL::CPR * Elem<E>::VEC;
-                const int r = min(tile * BR + e / TL::CPR, rows - 1);
-                const int t = row_token(g, r), hd = r - t * g.G;
-                qs[i] = gs[i] = uint4{0, 0, 0, 0};
-                if (c < a.D) {
-                    qs[i] = *reinterpret_cast<const uint4 *>(qp + t * a.ldq + hd * a.D + c);
-                    gs[i] = *reinterpret_cast<const uint4 *>(gp + t * gr.lddo + hd * a.D + c);
-                }
+            for (int i = 0; i < qs.N; ++i) {
+                int t, hd;
+                place(qs.row(i), t, hd);
+                const uint32_t c = __umul24(hd, a.D * sizeof(E)) + 16 * qs.chunk(i);
+                qs.get(i, qt, __umul24(t, ldq) + c, a.D);
+                gs.get(i, gt, __umul24(t, ldg) + c, a.D);
             }
             if (threadIdx.x < BR) {
                 const int r = tile * BR + threadIdx.x;
-                const int t = row_token(g, min(r, rows - 1)), hd = min(r, rows - 1) - t * g.G;
-                const float l = lp[static_cast<int64_t>(t) * a.Hq + hd];
+                int t, hd;
+                place(threadIdx.x, t, hd);
+                const uint32_t at = (t + first) * a.Hq + hd;
+                const float l = lp[at];
                 // rows past the end and rows that saw no key: every p is 0
                 ls = r >= rows || l == -HUGE_VALF ? Ref{HUGE_VALF, 0.f} : ref_of_lse(l);
-                ds = dp0[static_cast<int64_t>(t) * a.Hq + hd];
-                sees = r >= rows ? 0 : a.causal ? max(0, t + ahead + 1) : m;
+                ds = dp0[at];
+                sees = r >= rows ? 0 : a.causal ? max(0, t + first + ahead + 1) : m;
             }
         };
         auto store = [&](unsigned char *t) {
-#pragma unroll
-            for (int i = 0; i < NCH; ++i) {
-                const int e = threadIdx.x + 256 * i;
-                const int p = TL::chunk_at(e / TL::CPR, e % TL::CPR);
-                *reinterpret_cast<uint4 *>(t + p) = qs[i];
-                *reinterpret_cast<uint4 *>(t + TB + p) = gs[i];
-            }
+            qs.put(t);
+            gs.put(t + TB);
             if (threadIdx.x < BR) {
                 float *f = reinterpret_cast<float *>(t + 2 * TB);
                 f[threadIdx.x] = ls.hi;
-                f[BR + threadIdx.x] = ds;
+                f[BR + threadIdx.x] = -ds;
                 reinterpret_cast<int *>(f)[2 * BR + threadIdx.x] = sees;
                 f[3 * BR + threadIdx.x] = ls.lo;
             }
@@ -571,38 +563,47 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
                 const bool masked = wkey + 32 > first_sees;
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
+                    // dP starts from -D (float32: adds it at the end; its
+                    // operands leave no registers for it)
+                    constexpr bool F32 = sizeof(E) == 4;
                     floatx16 x = floatx16{}, dp = floatx16{};
+                    const int at = 32 * t + 4 * h;
+                    if constexpr (!F32)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            set_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
 #pragma unroll
                     for (int s = 0; s < DS; ++s) {
                         x = add_product(TL::read_cols(qt + 32 * t * TL::PITCH, ca, s), kf[s], x);
-                        const Frag vs =
-                            VL ? TL::read_cols(vw, ca, s) : vf[VL ? 0 : s];
+                        const Frag vs = VL ? TL::read_cols(vw, ca, s) : vf[VL ? 0 : s];
                         dp = add_product(TL::read_cols(gt + 32 * t * TL::PITCH, ca, s), vs, dp);
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int4 s4 = *reinterpret_cast<const int4 *>(st + at + 8 * i);
+                            const int sees4[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (key >= sees4[r])
+                                    x[4 * i + r] = -HUGE_VALF;
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int at = 32 * t + 8 * i + 4 * h;
-                        const float4 l4 = *reinterpret_cast<const float4 *>(lt + at);
-                        const float4 d4 = *reinterpret_cast<const float4 *>(dt + at);
+                        const float4 l4 = *reinterpret_cast<const float4 *>(lt + at + 8 * i);
                         const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-                        const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
                         float4 r4{0.f, 0.f, 0.f, 0.f};
-                        if constexpr (sizeof(E) == 4)
-                            r4 = *reinterpret_cast<const float4 *>(lt + 3 * BR + at);
+                        if constexpr (F32) {
+                            r4 = *reinterpret_cast<const float4 *>(lt + 3 * BR + at + 8 * i);
+                            add_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
+                        }
                         const float ll[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float p = prob<E>(x[4 * i + r], a, l[r], ll[r]);
                             x[4 * i + r] = p;
-                            dp[4 * i + r] = p * (dp[4 * i + r] - dd[r]);
-                        }
-                        if (masked) {
-                            const int4 s4 = *reinterpret_cast<const int4 *>(st + at);
-                            const int sees4[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (key >= sees4[r])
-                                    x[4 * i + r] = dp[4 * i + r] = 0.f;
+                            dp[4 * i + r] *= p;
                         }
                     }
 #pragma unroll
@@ -691,7 +692,7 @@ hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *l
     constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 128 * NQ, a.S);
     // one block more, the first, divides the keys' work
-    HEX_LAUNCH((attn_dq_k<E, DC, NQ, BK>), dim3(static_cast<uint32_t>(a.slots) * a.Hkv + 1),
+    HEX_LAUNCH((attn_dq_k<E, DC, NQ, BK>), dim3(attn_blocks(a) + 1),
                dim3(256), 0, st, q, k, v, o, lse, dout, dq, delta, a, gr, pl);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.Tk == 0)

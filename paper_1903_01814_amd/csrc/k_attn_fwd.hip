@@ -33,17 +33,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
     using Frag = typename Elem<E>::Frag;
     constexpr int TR = 128 * NQ, KT = BK / 32, DT = DC / 32, DS = DC / 16;
     constexpr int TB = TL::bytes(BK);
-    constexpr int NCH = BK * TL::CPR / 256; // chunks a thread stages of K (and of V)
-    static_assert(BK * TL::CPR % 256 == 0, "");
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = lane >> 5, col = lane & 31;
-    // key heads fastest (with 8 dies taking blocks in turn, a head's keys
-    // stay on few of them), sequences' last tiles first: under the causal
-    // mask they are the longest
-    const int kvh = blockIdx.x % a.Hkv;
-    const int w = a.slots - 1 - static_cast<int>(blockIdx.x / a.Hkv);
+    int kvh, w;
+    head_and_slot(a, blockIdx.x, kvh, w);
+    if (w < 0)
+        return;
     const Group g = a.group;
     const Span sp = find_span<TR>(a.q_start, a.S, a.Tq, g.G, w);
     const int rows = sp.n * g.G;
@@ -51,7 +48,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
         return;
     const int row0 = sp.tile * TR;
     int kb, m;
-    key_span(a, sp.seq, kb, m);
+    key_span(a, sp.seq, sp.begin, sp.n, kb, m);
     const int ahead = m - sp.n; // causal: query i sees keys up to i + ahead
 
     // this lane's query of each block of rows, and how many keys it sees
@@ -89,29 +86,17 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
     least = __builtin_amdgcn_readfirstlane(least);
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
-    uint4 ks[NCH], vs[NCH];
+    Stage<E, DC, BK, 256> ks, vs;
+    const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     // rows past the end repeat the last one: their scores are masked
     auto load = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            const int c = e % TL::CPR * Elem<E>::VEC;
-            const int64_t r = min(tile * BK + e / TL::CPR, m - 1);
-            ks[i] = vs[i] = uint4{0, 0, 0, 0};
-            if (c < a.D) {
-                ks[i] = *reinterpret_cast<const uint4 *>(kp + r * a.ldk + c);
-                vs[i] = *reinterpret_cast<const uint4 *>(vp + r * a.ldv + c);
-            }
-        }
+        const int64_t k0 = static_cast<int64_t>(tile) * BK;
+        ks.rows(kp + k0 * a.ldk, ldk, m - tile * BK, a.D);
+        vs.rows(vp + k0 * a.ldv, ldv, m - tile * BK, a.D);
     };
     auto store = [&](unsigned char *t) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = threadIdx.x + 256 * i;
-            const int p = TL::chunk_at(e / TL::CPR, e % TL::CPR);
-            *reinterpret_cast<uint4 *>(t + p) = ks[i];
-            *reinterpret_cast<uint4 *>(t + TB + p) = vs[i];
-        }
+        ks.put(t);
+        vs.put(t + TB);
     };
 
     int ca = TL::cols_at(col, h);
@@ -241,7 +226,7 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *l
     constexpr bool F32 = sizeof(E) == 4;
     constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 128 * NQ, a.S);
-    HEX_LAUNCH((attn_fwd_k<E, DC, NQ, BK>), dim3(static_cast<uint32_t>(a.slots) * a.Hkv), dim3(256),
+    HEX_LAUNCH((attn_fwd_k<E, DC, NQ, BK>), dim3(attn_blocks(a)), dim3(256),
                0, st, static_cast<const E *>(q), static_cast<const E *>(k),
                static_cast<const E *>(v), static_cast<E *>(o), lse, a);
     return hipGetLastError();

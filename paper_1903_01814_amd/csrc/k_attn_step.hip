@@ -29,7 +29,6 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
     using Frag = typename Elem<E>::Frag;
     constexpr int DT = DC / 32, DS = DC / 16, BK = 32;
     constexpr int TB = TL::bytes(BK);
-    constexpr int NCH = BK * TL::CPR / 64;
     static_assert(2 * TB >= 32 * DC * 4, "");
     __shared__ __align__(16) unsigned char smem[kStepWaves][2 * TB];
     __shared__ float stats[2][kStepWaves][32];
@@ -49,7 +48,7 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
     const int rows = pl.n * g.G;
 
     int kb, m;
-    key_span(a, seq, kb, m);
+    key_span(a, seq, 0, 0, kb, m);
     const int begin = split * pl.chunk, end = min(m, begin + pl.chunk);
     if (begin >= end && !(split == 0 && pl.splits == 1))
         return; // attn_join_k knows
@@ -66,28 +65,15 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
     unsigned char *kt = smem[wave], *vt = kt + TB;
-    uint4 ks[NCH], vs[NCH];
+    Stage<E, DC, BK, 64> ks, vs;
+    const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     auto load = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = lane + 64 * i;
-            const int c = e % TL::CPR * Elem<E>::VEC;
-            const int64_t kr = min(k0 + e / TL::CPR, m - 1);
-            ks[i] = vs[i] = uint4{0, 0, 0, 0};
-            if (c < a.D) {
-                ks[i] = *reinterpret_cast<const uint4 *>(kp + kr * a.ldk + c);
-                vs[i] = *reinterpret_cast<const uint4 *>(vp + kr * a.ldv + c);
-            }
-        }
+        ks.rows(kp + k0 * a.ldk, ldk, m - k0, a.D);
+        vs.rows(vp + k0 * a.ldv, ldv, m - k0, a.D);
     };
     auto store = [&]() {
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            const int e = lane + 64 * i;
-            const int p = TL::chunk_at(e / TL::CPR, e % TL::CPR);
-            *reinterpret_cast<uint4 *>(kt + p) = ks[i];
-            *reinterpret_cast<uint4 *>(vt + p) = vs[i];
-        }
+        ks.put(kt);
+        vs.put(vt);
     };
 
     int ca = TL::cols_at(col, h);
@@ -98,7 +84,7 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
         acc[d] = floatx16{};
     float mx = -HUGE_VALF, sum = 0.f;
 
-    int k0 = begin + wave * BK;
+    int k0 = __builtin_amdgcn_readfirstlane(begin + wave * BK);
     if (k0 < end)
         load(k0);
     for (; k0 < end; k0 += kStepWaves * BK) {
@@ -224,7 +210,7 @@ __global__ __launch_bounds__(NT) void attn_join_k(const float *part, const float
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     int kb, m;
-    key_span(a, static_cast<int>(row / (static_cast<int64_t>(pl.n) * a.Hq)), kb, m);
+    key_span(a, static_cast<int>(row / (static_cast<int64_t>(pl.n) * a.Hq)), 0, 0, kb, m);
     const int runs = (m + pl.chunk - 1) / pl.chunk;
     // the largest maximum, then every run's weight and the sum of the weights
     float top = -HUGE_VALF;

@@ -264,7 +264,7 @@ struct AttnArgs {
     Group group;
     int64_t ldq, ldk, ldv, ldo;
     float scale, c, c_lo;
-    bool causal;
+    bool causal, narrow; // narrow: a head is less than a cache line
     int slots;   // tiles of rows handed out per key head (set by the launcher)
     int max_len; // longest sequence of keys taken
 };

@@ -28,6 +28,8 @@ typedef short shortx8 __attribute__((ext_vector_type(8)));
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLo = 1.4426950408889634 - kLog2e;
 constexpr float kLn2 = 0.6931471805599453f, kLn2Lo = 0.6931471805599453 - kLn2;
 
+constexpr int kShortRows = 256;
+
 struct FragF32 {
     float v[8];
 };
@@ -295,6 +297,11 @@ __device__ __forceinline__ int row_token(Group g, int r)
 inline int attn_slots(int T, int G, int TR, int S)
 {
     return static_cast<int>(static_cast<int64_t>(T) * G / TR) + S;
+}
+// Sequences too short to fill tiles of 128 rows: tiles of 64
+inline bool attn_short(const AttnArgs &a)
+{
+    return static_cast<int64_t>(a.Tq) * a.group.G < static_cast<int64_t>(kShortRows) * a.S;
 }
 // blocks of a launch over all slots and key heads
 inline uint32_t attn_blocks(const AttnArgs &a)

@@ -87,18 +87,18 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int s)
     return r;
 }
 
-// One block of 256 threads: the list of pieces of one head (all heads' are
-// alike), a thread taking a tile at a time.  lds: kPlanLds bytes.
-constexpr int kPlanLds = 512 * 8 + (256 + 1) * kClasses * 4 + 2 * 4;
+// One block of NT threads: the list of pieces of one head (all heads' are
+// alike), a thread taking a tile at a time.  lds: plan_lds(NT) bytes.
+constexpr int plan_lds(int NT) { return NT * (2 * 8 + kClasses * 4) + (kClasses + 2) * 4; }
 
-__device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *lds)
+template <int NT> __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *lds)
 {
     int64_t *before = reinterpret_cast<int64_t *>(lds); // units, tiles before each
-    int64_t *tbefore = before + 256;                    // thread's run of sequences
-    int *counts = reinterpret_cast<int *>(tbefore + 256); // [classes][256]
-    int *ends = counts + 256 * kClasses;                  // [classes]; slots, divided tiles
+    int64_t *tbefore = before + NT;                     // thread's run of sequences
+    int *counts = reinterpret_cast<int *>(tbefore + NT); // [classes][NT]
+    int *ends = counts + NT * kClasses;                   // [classes]; slots, divided tiles
     const int tid = threadIdx.x;
-    const int run = (a.S + 255) / 256;
+    const int run = (a.S + NT - 1) / NT;
     const int s0 = min(a.S, tid * run), s1 = min(a.S, s0 + run);
     int64_t sum = 0, tiles = 0;
     for (int s = s0; s < s1; ++s) {
@@ -113,17 +113,17 @@ __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *l
     if (tid < 2)
         ends[kClasses + tid] = 0;
     __syncthreads();
-    for (int d = 1; d < 256; d <<= 1) {
+    for (int d = 1; d < NT; d <<= 1) {
         const int64_t v = tid >= d ? before[tid - d] : 0, w = tid >= d ? tbefore[tid - d] : 0;
         __syncthreads();
         before[tid] += v;
         tbefore[tid] += w;
         __syncthreads();
     }
-    const int64_t all = before[255];
+    const int64_t all = before[NT - 1];
     // offsets that do not ascend can ask for more than the list holds: none then
     const int all_tiles =
-        tbefore[255] > pl.room - 2 * pl.shares ? 0 : static_cast<int>(tbefore[255]);
+        tbefore[NT - 1] > pl.room - 2 * pl.shares ? 0 : static_cast<int>(tbefore[NT - 1]);
     __syncthreads();
     tbefore[tid] -= tiles;
     __syncthreads();
@@ -133,7 +133,7 @@ __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *l
     KeyPiece pc;
     auto tile = [&](int w) {
         // the last run, then sequence, whose first tile is not past w
-        int c = 0, len = 256;
+        int c = 0, len = NT;
         while (len > 1) {
             const int half = len >> 1;
             const bool ok = tbefore[c + half] <= w;
@@ -165,47 +165,47 @@ __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *l
     // a thread takes tiles that follow one another, and they keep their order
     // within a class: neighbours run at about the same time and read the same
     // rows
-    const int each = (all_tiles + 255) / 256;
+    const int each = (all_tiles + NT - 1) / NT;
     const int w0 = min(all_tiles, tid * each), w1 = min(all_tiles, w0 + each);
     for (int c = 0; c < kClasses; ++c)
-        counts[c * 256 + tid] = 0;
+        counts[c * NT + tid] = 0;
     for (int w = w0; w < w1; ++w) {
         tile(w);
-        counts[cls * 256 + tid] += pc.parts;
+        counts[cls * NT + tid] += pc.parts;
     }
     __syncthreads();
-    for (int d = 1; d < 256; d <<= 1) {
+    for (int d = 1; d < NT; d <<= 1) {
         int v[kClasses];
 #pragma unroll
         for (int c = 0; c < kClasses; ++c)
-            v[c] = tid >= d ? counts[c * 256 + tid - d] : 0;
+            v[c] = tid >= d ? counts[c * NT + tid - d] : 0;
         __syncthreads();
 #pragma unroll
         for (int c = 0; c < kClasses; ++c)
-            counts[c * 256 + tid] += v[c];
+            counts[c * NT + tid] += v[c];
         __syncthreads();
     }
     if (tid == 0) {
         *pl.next = pl.blocks; // the first ones are the blocks' own numbers
         int at = 0;
         for (int c = 0; c < kClasses; ++c) {
-            at += counts[c * 256 + 255];
+            at += counts[c * NT + NT - 1];
             ends[c] = pl.ends[c] = at;
         }
     }
     __syncthreads();
     // this thread's next place in each class: counted from the class's end
     for (int c = 0; c < kClasses; ++c) {
-        const int last = counts[c * 256 + 255];
-        const int here = tid > 0 ? counts[c * 256 + tid - 1] : 0;
+        const int last = counts[c * NT + NT - 1];
+        const int here = tid > 0 ? counts[c * NT + tid - 1] : 0;
         __syncthreads();
-        counts[c * 256 + tid] = ends[c] - last + here;
+        counts[c * NT + tid] = ends[c] - last + here;
         __syncthreads();
     }
     for (int w = w0; w < w1; ++w) {
         tile(w);
-        const int at = counts[cls * 256 + tid];
-        counts[cls * 256 + tid] = at + pc.parts;
+        const int at = counts[cls * NT + tid];
+        counts[cls * NT + tid] = at + pc.parts;
         // which slot a piece has decides nothing
         const int slot = pc.parts > 1 ? atomicAdd(ends + kClasses, pc.parts) : 0;
         for (int i = 0; i < pc.parts; ++i) {
@@ -224,23 +224,22 @@ __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *l
         pl.ends[kClasses] = ends[kClasses + 1];
 }
 
-// ---- dq: rows as in the forward, 32 NQ a wave, BK keys a tile.
+// ---- dq: rows as in the forward, 32 a wave of NW, BK keys a tile.
 //   X^T = K Q^T and dP^T = V dO^T (keys as rows), dQ^T += K^T dS^T
-template <typename E, int DC, int NQ, int BK>
-__global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, const E *v, const E *o,
-                                                 const float *lse, const E *dout, E *dq,
-                                                 float *delta, AttnArgs a, AttnGrads gr,
-                                                    KeyPlan pl)
+template <typename E, int DC, int BK, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, const E *v,
+                                                        const E *o, const float *lse,
+                                                        const E *dout, E *dq, float *delta,
+                                                        AttnArgs a, AttnGrads gr, KeyPlan pl)
 {
     using TL = Tile<E, DC>;
     using Frag = typename Elem<E>::Frag;
-    constexpr int TR = 128 * NQ, KT = BK / 32, DT = DC / 32, DS = DC / 16;
+    constexpr int TR = 32 * NW, KT = BK / 32, DT = DC / 32, DS = DC / 16;
     constexpr int TB = TL::bytes(BK);
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
-
     if (blockIdx.x == 0) {
-        static_assert(sizeof(smem) >= kPlanLds, "");
-        make_plan(a, pl, smem);
+        static_assert(sizeof(smem) >= plan_lds(64 * NW), "");
+        make_plan<64 * NW>(a, pl, smem);
         return;
     }
 
@@ -260,46 +259,31 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     key_span(a, sp.seq, sp.begin, sp.n, kb, m);
     const int ahead = m - sp.n;
 
-    Frag qf[NQ][DS], gf[NQ][DS];
-    int see[NQ], most = 0;
-    int64_t token[NQ];
-    int head[NQ];
-    Ref ref[NQ];
-    float dl[NQ];
+    const int row = row0 + wave * 32 + col, rc = min(row, rows - 1);
+    const int tq = row_token(g, rc), head = kvh * g.G + rc - tq * g.G;
+    const int64_t token = sp.begin + tq;
+    const int see = row < rows ? (a.causal ? min(m, max(0, tq + ahead + 1)) : m) : 0;
+    const E *qp = q + token * a.ldq + head * a.D;
+    const E *gp = dout + token * gr.lddo + head * a.D;
+    const E *op = o + token * a.ldo + head * a.D;
+    const float l = lse[token * a.Hq + head];
+    // a row that saw no key: every p is 0
+    const Ref ref = l == -HUGE_VALF ? Ref{HUGE_VALF, 0.f} : ref_of_lse(l);
+    Frag qf[DS], gf[DS];
+    float dl = 0.f;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-        const int r = row0 + (wave * NQ + b) * 32 + col;
-        const int rc = min(r, rows - 1);
-        const int t = row_token(g, rc);
-        head[b] = kvh * g.G + rc - t * g.G;
-        token[b] = sp.begin + t;
-        const E *qp = q + token[b] * a.ldq + head[b] * a.D;
-        const E *gp = dout + token[b] * gr.lddo + head[b] * a.D;
-        const E *op = o + token[b] * a.ldo + head[b] * a.D;
-        float sum = 0.f;
-#pragma unroll
-        for (int s = 0; s < DS; ++s) {
-            qf[b][s] = load_frag<E>(qp, 16 * s + 8 * h, a.D);
-            gf[b][s] = load_frag<E>(gp, 16 * s + 8 * h, a.D);
-            const Frag of = load_frag<E>(op, 16 * s + 8 * h, a.D);
-            sum += dot8(gf[b][s], of);
-        }
-        dl[b] = both_sum(sum);
-        const float l = lse[token[b] * a.Hq + head[b]];
-        // a row that saw no key: every p is 0
-        ref[b] = l == -HUGE_VALF ? Ref{HUGE_VALF, 0.f} : ref_of_lse(l);
-        if (r < rows && h == 0)
-            delta[token[b] * a.Hq + head[b]] = dl[b];
-        see[b] = r < rows ? (a.causal ? min(m, max(0, t + ahead + 1)) : m) : 0;
-        most = max(most, see[b]);
+    for (int s = 0; s < DS; ++s) {
+        qf[s] = load_frag<E>(qp, 16 * s + 8 * h, a.D);
+        gf[s] = load_frag<E>(gp, 16 * s + 8 * h, a.D);
+        dl += dot8(gf[s], load_frag<E>(op, 16 * s + 8 * h, a.D));
     }
+    dl = both_sum(dl);
+    if (row < rows && h == 0)
+        delta[token * a.Hq + head] = dl;
     const int r_last = min(rows, row0 + TR) - 1;
     const int end = a.causal ? min(m, max(0, row_token(g, r_last) + ahead + 1)) : m;
     const int ntiles = (end + BK - 1) / BK;
-    int least = see[0];
-#pragma unroll
-    for (int b = 1; b < NQ; ++b)
-        least = min(least, see[b]);
+    int most = see, least = see;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         most = max(most, __shfl_xor(most, d));
@@ -309,7 +293,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
     least = __builtin_amdgcn_readfirstlane(least);
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
-    Stage<E, DC, BK, 256> ks, vs;
+    Stage<E, DC, BK, 64 * NW> ks, vs;
     const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     // rows past the end repeat the last one: their scores are masked
     auto load = [&](int tile) {
@@ -324,12 +308,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
 
     int ca = TL::cols_at(col, h);
     typename TL::RowsAt ra = TL::rows_at(lane);
-    floatx16 acc[NQ][DT];
+    floatx16 acc[DT];
 #pragma unroll
-    for (int b = 0; b < NQ; ++b)
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-            acc[b][d] = floatx16{};
+    for (int d = 0; d < DT; ++d)
+        acc[d] = floatx16{};
 
     if (ntiles > 0) {
         load(0);
@@ -343,51 +325,31 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
         if (more)
             load(j + 1);
         if (j * BK < most) {
-            const bool masked = (j + 1) * BK > least;
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
-                floatx16 x[NQ], dp[NQ];
-#pragma unroll
-                for (int b = 0; b < NQ; ++b)
-                    x[b] = dp[b] = floatx16{};
+                const int key0 = j * BK + 32 * t;
+                floatx16 x = floatx16{}, dp = floatx16{};
 #pragma unroll
                 for (int s = 0; s < DS; ++s) {
-                    const Frag kf = TL::read_cols(kt + 32 * t * TL::PITCH, ca, s);
-                    const Frag vf = TL::read_cols(vt + 32 * t * TL::PITCH, ca, s);
-#pragma unroll
-                    for (int b = 0; b < NQ; ++b) {
-                        x[b] = add_product(kf, qf[b][s], x[b]);
-                        dp[b] = add_product(vf, gf[b][s], dp[b]);
-                    }
+                    x = add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], x);
+                    dp = add_product(TL::read_cols(vt + 32 * t * TL::PITCH, ca, s), gf[s], dp);
                 }
 #pragma unroll
-                for (int b = 0; b < NQ; ++b) {
+                for (int r = 0; r < 16; ++r)
+                    x[r] = prob<E>(x[r], a, ref.hi, ref.lo) * (dp[r] - dl);
+                if (key0 + 32 > least) {
+                    const int left = see - key0 - 4 * h;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float p = prob<E>(x[b][r], a, ref[b].hi, ref[b].lo);
-                        x[b][r] = p * (dp[b][r] - dl[b]);
-                    }
-                    if (masked) {
-                        const int left = see[b] - j * BK - 4 * h;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (32 * t + 8 * (r >> 2) + (r & 3) >= left)
-                                x[b][r] = 0.f;
-                    }
+                    for (int r = 0; r < 16; ++r)
+                        if (8 * (r >> 2) + (r & 3) >= left)
+                            x[r] = 0.f;
                 }
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    Frag sf[NQ];
+                    const Frag sf = to_frag<E>(x, s);
 #pragma unroll
-                    for (int b = 0; b < NQ; ++b)
-                        sf[b] = to_frag<E>(x[b], s);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const Frag kf = TL::read_rows(kt, ra, 32 * t + 16 * s, d);
-#pragma unroll
-                        for (int b = 0; b < NQ; ++b)
-                            acc[b][d] = mma(kf, sf[b], acc[b][d]);
-                    }
+                    for (int d = 0; d < DT; ++d)
+                        acc[d] = mma(TL::read_rows(kt, ra, 32 * t + 16 * s, d), sf, acc[d]);
                 }
             }
         }
@@ -396,15 +358,12 @@ __global__ __launch_bounds__(256, 2) void attn_dq_k(const E *q, const E *k, cons
         __syncthreads();
     }
 
+    if (row >= rows)
+        return;
+    E *p = dq + token * gr.lddq + head * a.D;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-        if (row0 + (wave * NQ + b) * 32 + col >= rows)
-            continue;
-        E *p = dq + token[b] * gr.lddq + head[b] * a.D;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-            store_col(p, acc[b][d], 32 * d + 4 * h, a.D, a.scale);
-    }
+    for (int d = 0; d < DT; ++d)
+        store_col(p, acc[d], 32 * d + 4 * h, a.D, a.scale);
 }
 
 // Rows a step of attn_dkv_k takes, and the blocks of it that a compute unit
@@ -563,12 +522,14 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
                 const bool masked = wkey + 32 > first_sees;
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
-                    // dP starts from -D (float32: adds it at the end; its
-                    // operands leave no registers for it)
-                    constexpr bool F32 = sizeof(E) == 4;
+                    if (RT > 1 && j * BR + 32 * t >= rows)
+                        break;
+                    // dP starts from -D, or, where there are no registers for
+                    // that beside the operands, ends with it
+                    constexpr bool F32 = sizeof(E) == 4, EARLY = !F32 || DC > 64;
                     floatx16 x = floatx16{}, dp = floatx16{};
                     const int at = 32 * t + 4 * h;
-                    if constexpr (!F32)
+                    if constexpr (EARLY)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             set_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
@@ -594,10 +555,10 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
                         const float4 l4 = *reinterpret_cast<const float4 *>(lt + at + 8 * i);
                         const float l[4] = {l4.x, l4.y, l4.z, l4.w};
                         float4 r4{0.f, 0.f, 0.f, 0.f};
-                        if constexpr (F32) {
+                        if constexpr (F32)
                             r4 = *reinterpret_cast<const float4 *>(lt + 3 * BR + at + 8 * i);
+                        if constexpr (!EARLY)
                             add_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
-                        }
                         const float ll[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
@@ -683,18 +644,29 @@ __global__ __launch_bounds__(256) void attn_dkv_join_k(E *dk, E *dv, AttnArgs a,
         store_col(dv + at * gr.lddv + kvh * a.D, sum, 32 * (which - DT) + c0, a.D, 1.f);
 }
 
+template <typename E, int DC, int NW>
+hipError_t launch_dq(const E *q, const E *k, const E *v, const E *o, const float *lse,
+                     const E *dout, E *dq, float *delta, AttnArgs a, const AttnGrads &gr,
+                     const KeyPlan &pl, hipStream_t st)
+{
+    constexpr bool F32 = sizeof(E) == 4;
+    constexpr int BK = NW == 2 || (F32 && DC > 64) ? 32 : 64;
+    a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
+    // one block more, the first, divides the keys' work
+    HEX_LAUNCH((attn_dq_k<E, DC, BK, NW>), dim3(attn_blocks(a) + 1), dim3(64 * NW), 0, st, q, k,
+               v, o, lse, dout, dq, delta, a, gr, pl);
+    return hipGetLastError();
+}
+
 template <typename E, int DC>
 hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *lse, const E *dout,
-                  E *dq, E *dk, E *dv, float *delta, AttnArgs a, const AttnGrads &gr,
+                  E *dq, E *dk, E *dv, float *delta, const AttnArgs &a, const AttnGrads &gr,
                   const KeyPlan &pl, hipStream_t st)
 {
     constexpr bool F32 = sizeof(E) == 4;
-    constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64;
-    a.slots = attn_slots(a.Tq, a.group.G, 128 * NQ, a.S);
-    // one block more, the first, divides the keys' work
-    HEX_LAUNCH((attn_dq_k<E, DC, NQ, BK>), dim3(attn_blocks(a) + 1),
-               dim3(256), 0, st, q, k, v, o, lse, dout, dq, delta, a, gr, pl);
-    hipError_t e = hipGetLastError();
+    hipError_t e = attn_short(a)
+                       ? launch_dq<E, DC, 2>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st)
+                       : launch_dq<E, DC, 4>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st);
     if (e != hipSuccess || a.Tk == 0)
         return e;
     HEX_LAUNCH((attn_dkv_k<E, DC, dkv_rows(F32, DC)>), dim3(static_cast<uint32_t>(pl.blocks)),

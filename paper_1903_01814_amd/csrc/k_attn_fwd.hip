@@ -4,10 +4,10 @@
 //   lse_i = log sum_j exp(x_ij)
 //
 // in one pass over the keys with a running maximum m and sum l per row.  A
-// block owns TR = 128 NQ rows of one key head of one sequence (a row is a
-// query token and one of the G query heads that share the key head, so short
-// sequences fill a tile G times better and the keys are read once for the
-// group), a wave 32 NQ of them.  Per tile of BK keys, staged in LDS for the
+// block owns 128 rows (64 where sequences are short) of one key head of one
+// sequence (a row is a query token and one of the G query heads that share the
+// key head, so short sequences fill a tile G times better and the keys are
+// read once for the group), a wave 32 of them.  Per tile of BK keys, staged in LDS for the
 // whole block (two buffers, the next tile's loads in flight during the
 // products):
 //   X^T = K Q^T   keys as rows: a lane holds one query's scores
@@ -24,14 +24,14 @@ namespace {
 
 constexpr float kSlack = 8.f; // in powers of two
 
-// NQ blocks of 32 rows a wave, BK keys a tile.
-template <typename E, int DC, int NQ, int BK>
-__global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, const E *v, E *o,
-                                                  float *lse, AttnArgs a)
+// NW waves, BK keys a tile.
+template <typename E, int DC, int BK, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k, const E *v, E *o,
+                                                         float *lse, AttnArgs a)
 {
     using TL = Tile<E, DC>;
     using Frag = typename Elem<E>::Frag;
-    constexpr int TR = 128 * NQ, KT = BK / 32, DT = DC / 32, DS = DC / 16;
+    constexpr int TR = 32 * NW, KT = BK / 32, DT = DC / 32, DS = DC / 16;
     constexpr int TB = TL::bytes(BK);
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
 
@@ -51,32 +51,21 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
     key_span(a, sp.seq, sp.begin, sp.n, kb, m);
     const int ahead = m - sp.n; // causal: query i sees keys up to i + ahead
 
-    // this lane's query of each block of rows, and how many keys it sees
-    Frag qf[NQ][DS];
-    int see[NQ], most = 0;
-    int64_t at[NQ];
+    // this lane's query, and how many keys it sees
+    const int row = row0 + wave * 32 + col, rc = min(row, rows - 1);
+    const int tq = row_token(g, rc), head = kvh * g.G + rc - tq * g.G;
+    const int64_t token = sp.begin + tq;
+    const int see = row < rows ? (a.causal ? min(m, max(0, tq + ahead + 1)) : m) : 0;
+    const E *qp = q + token * a.ldq + head * a.D;
+    Frag qf[DS];
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-        const int r = row0 + (wave * NQ + b) * 32 + col;
-        const int rc = min(r, rows - 1);
-        const int t = row_token(g, rc);
-        const int head = kvh * g.G + rc - t * g.G;
-        at[b] = static_cast<int64_t>(sp.begin + t) * a.Hq + head;
-        const E *qp = q + (sp.begin + t) * a.ldq + head * a.D;
-#pragma unroll
-        for (int s = 0; s < DS; ++s)
-            qf[b][s] = load_frag<E>(qp, 16 * s + 8 * h, a.D);
-        see[b] = r < rows ? (a.causal ? min(m, max(0, t + ahead + 1)) : m) : 0;
-        most = max(most, see[b]);
-    }
-    // keys that any row of the wave, and of the block, sees; and that all do
+    for (int s = 0; s < DS; ++s)
+        qf[s] = load_frag<E>(qp, 16 * s + 8 * h, a.D);
+    // keys that any row of the block sees; of the wave; and that all of it see
     const int r_last = min(rows, row0 + TR) - 1;
     const int end = a.causal ? min(m, max(0, row_token(g, r_last) + ahead + 1)) : m;
     const int ntiles = (end + BK - 1) / BK;
-    int least = see[0];
-#pragma unroll
-    for (int b = 1; b < NQ; ++b)
-        least = min(least, see[b]);
+    int most = see, least = see;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         most = max(most, __shfl_xor(most, d));
@@ -86,7 +75,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
     least = __builtin_amdgcn_readfirstlane(least);
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
-    Stage<E, DC, BK, 256> ks, vs;
+    Stage<E, DC, BK, 64 * NW> ks, vs;
     const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     // rows past the end repeat the last one: their scores are masked
     auto load = [&](int tile) {
@@ -101,16 +90,67 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
 
     int ca = TL::cols_at(col, h);
     typename TL::RowsAt ra = TL::rows_at(lane);
-    floatx16 acc[NQ][DT];
-    float mx[NQ], sum[NQ];
+    floatx16 acc[DT];
+    float mx = -HUGE_VALF, sum = 0.f;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-        mx[b] = -HUGE_VALF;
-        sum[b] = 0.f;
+    for (int d = 0; d < DT; ++d)
+        acc[d] = floatx16{};
+
+    // the tile of keys at kt and vt, key0 the first
+    auto tile = [&](unsigned char *kt, unsigned char *vt, int key0) {
+        floatx16 x[KT];
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-            acc[b][d] = floatx16{};
-    }
+        for (int t = 0; t < KT; ++t) {
+            x[t] = floatx16{};
+#pragma unroll
+            for (int s = 0; s < DS; ++s)
+                x[t] = add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], x[t]);
+        }
+        if (key0 + BK > least) {
+            const int left = see - key0 - 4 * h;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * t + 8 * (r >> 2) + (r & 3) >= left)
+                        x[t][r] = -HUGE_VALF;
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                top = fmaxf(top, x[t][r]);
+        top = both_max(top) * a.c;
+        if (__any(top > mx + kSlack)) {
+            const float to = fmaxf(mx, top);
+            const float f = mx == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(mx - to);
+            mx = to;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                acc[d] *= f;
+        }
+        // a row that has seen no key: every p is 0
+        const float ref = mx == -HUGE_VALF ? 0.f : mx;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = prob<E>(x[t][r], a, ref, 0.f);
+                x[t][r] = p;
+                sum += p;
+            }
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Frag pf = to_frag<E>(x[t], s);
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+                    acc[d] = mma(TL::read_rows(vt, ra, 32 * t + 16 * s, d), pf, acc[d]);
+            }
+    };
 
     if (ntiles > 0) {
         load(0);
@@ -123,113 +163,46 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(const E *q, const E *k, con
         in_loop(ca), in_loop(ra.a), in_loop(ra.b);
         if (more)
             load(j + 1);
-        if (j * BK < most) {
-            floatx16 x[NQ][KT];
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-#pragma unroll
-                for (int b = 0; b < NQ; ++b)
-                    x[b][t] = floatx16{};
-#pragma unroll
-                for (int s = 0; s < DS; ++s) {
-                    const Frag kf = TL::read_cols(kt + 32 * t * TL::PITCH, ca, s);
-#pragma unroll
-                    for (int b = 0; b < NQ; ++b)
-                        x[b][t] = add_product(kf, qf[b][s], x[b][t]);
-                }
-            }
-            if ((j + 1) * BK > least) {
-#pragma unroll
-                for (int b = 0; b < NQ; ++b) {
-                    const int left = see[b] - j * BK - 4 * h;
-#pragma unroll
-                    for (int t = 0; t < KT; ++t)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (32 * t + 8 * (r >> 2) + (r & 3) >= left)
-                                x[b][t][r] = -HUGE_VALF;
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < NQ; ++b) {
-                float top = x[b][0][0];
-#pragma unroll
-                for (int t = 0; t < KT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        top = fmaxf(top, x[b][t][r]);
-                top = both_max(top) * a.c;
-                if (__any(top > mx[b] + kSlack)) {
-                    const float to = fmaxf(mx[b], top);
-                    const float f = mx[b] == -HUGE_VALF ? 0.f : __builtin_amdgcn_exp2f(mx[b] - to);
-                    mx[b] = to;
-                    sum[b] *= f;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-                        acc[b][d] *= f;
-                }
-                // a row that has seen no key: every p is 0
-                const float ref = mx[b] == -HUGE_VALF ? 0.f : mx[b];
-#pragma unroll
-                for (int t = 0; t < KT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float p = prob<E>(x[b][t][r], a, ref, 0.f);
-                        x[b][t][r] = p;
-                        sum[b] += p;
-                    }
-            }
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    Frag pf[NQ];
-#pragma unroll
-                    for (int b = 0; b < NQ; ++b)
-                        pf[b] = to_frag<E>(x[b][t], s);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const Frag vf = TL::read_rows(vt, ra, 32 * t + 16 * s, d);
-#pragma unroll
-                        for (int b = 0; b < NQ; ++b)
-                            acc[b][d] = mma(vf, pf[b], acc[b][d]);
-                    }
-                }
-        }
+        if (j * BK < most)
+            tile(kt, vt, j * BK);
         if (more)
             store(smem + ((j + 1) & 1) * 2 * TB);
         __syncthreads();
     }
 
+    const float l = both_sum(sum);
+    if (row >= rows)
+        return;
+    const float f = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);
+    E *op = o + token * a.ldo + head * a.D;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-        const float l = both_sum(sum[b]);
-        const int r = row0 + (wave * NQ + b) * 32 + col;
-        if (r >= rows)
-            continue;
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        // at = token * Hq + head
-        const int64_t token = at[b] / a.Hq;
-        E *op = o + token * a.ldo + (at[b] - token * a.Hq) * a.D;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-            store_col(op, acc[b][d], 32 * d + 4 * h, a.D, f);
-        if (lse != nullptr && h == 0)
-            lse[at[b]] = l == 0.f ? -HUGE_VALF : log_sum(mx[b], l);
-    }
+    for (int d = 0; d < DT; ++d)
+        store_col(op, acc[d], 32 * d + 4 * h, a.D, f);
+    if (lse != nullptr && h == 0)
+        lse[token * a.Hq + head] = l == 0.f ? -HUGE_VALF : log_sum(mx, l);
+}
+
+template <typename E, int DC, int NW>
+hipError_t launch_waves(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a,
+                        hipStream_t st)
+{
+    constexpr bool F32 = sizeof(E) == 4;
+    constexpr int BK = NW == 2 || (F32 && DC > 64) ? 32 : 64;
+    a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
+    HEX_LAUNCH((attn_fwd_k<E, DC, BK, NW>), dim3(attn_blocks(a)), dim3(64 * NW), 0, st, q, k, v,
+               o, lse, a);
+    return hipGetLastError();
 }
 
 template <typename E, int DC>
-hipError_t launch(const void *q, const void *k, const void *v, void *o, float *lse, AttnArgs a,
-                  hipStream_t st)
+hipError_t launch(const void *q, const void *k, const void *v, void *o, float *lse,
+                  const AttnArgs &a, hipStream_t st)
 {
-    constexpr bool F32 = sizeof(E) == 4;
-    constexpr int NQ = 1, BK = F32 && DC > 64 ? 32 : 64;
-    a.slots = attn_slots(a.Tq, a.group.G, 128 * NQ, a.S);
-    HEX_LAUNCH((attn_fwd_k<E, DC, NQ, BK>), dim3(attn_blocks(a)), dim3(256),
-               0, st, static_cast<const E *>(q), static_cast<const E *>(k),
-               static_cast<const E *>(v), static_cast<E *>(o), lse, a);
-    return hipGetLastError();
+    const auto run = [&](auto f) {
+        return f(static_cast<const E *>(q), static_cast<const E *>(k), static_cast<const E *>(v),
+                 static_cast<E *>(o), lse, a, st);
+    };
+    return attn_short(a) ? run(launch_waves<E, DC, 2>) : run(launch_waves<E, DC, 4>);
 }
 
 template <typename E>

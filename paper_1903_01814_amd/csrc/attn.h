@@ -22,7 +22,6 @@ namespace attn {
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef short shortx8 __attribute__((ext_vector_type(8)));
 
 // log2(e) and ln(2) as a float and what it leaves
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLo = 1.4426950408889634 - kLog2e;
@@ -30,23 +29,74 @@ constexpr float kLn2 = 0.6931471805599453f, kLn2Lo = 0.6931471805599453 - kLn2;
 
 constexpr int kShortRows = 256;
 
+// ---- how a type is multiplied.  E: what tensors hold; Frag: an operand;
+// Score: a sum over the head dimension while it is added up; FINE: exponents
+// in two parts (prob).  In LDS an element takes BYTES bytes in each of PLANES
+// tiles.
+//
+// bfloat16: as it is.
+struct Bf16 {
+    using E = bf16raw;
+    using Frag = bf16x8;
+    using Score = floatx16;
+    static constexpr bool FINE = false;
+    static constexpr int BYTES = 2, PLANES = 1;
+};
+// float32 as three bfloat16 numbers, x = h + m + l: h is x rounded, m the rest
+// rounded, l the rest of that, 8 bits each, so that nothing is left out of the
+// 24.  A product is the six products h h', h m', m h', m m', h l', l h' in
+// float32 sums; what is dropped is 2^-24 of it, a rounding of a float32
+// product.  Six bfloat16 products take 192 clocks where the float32 ones take
+// 512 (32 x 32 x 16); the kernels gain 1.4 to 1.8 (D = 32 to 128).  Values
+// below 2^-110 lose bits (their rests are denormal); infinities, and finite
+// values from 3.39e38 on, which round to one, become NaN.
+struct FragSplit {
+    bf16x8 p[3];
+};
+struct ScoreSplit {
+    floatx16 hi, lo; // h h', and the rest
+};
+struct Split {
+    using E = float;
+    using Frag = FragSplit;
+    using Score = ScoreSplit;
+    static constexpr bool FINE = true;
+    static constexpr int BYTES = 2, PLANES = 3;
+};
+// float32 as it is, for the cache step: each of its waves has tiles of its own,
+// whose three parts do not fit LDS, and it waits for memory either way.
 struct FragF32 {
     float v[8];
 };
-
-template <typename E> struct Elem;
-template <> struct Elem<bf16raw> {
-    using Frag = bf16x8;
-    static constexpr int VEC = 8; // elements of a 16-byte vector
-};
-template <> struct Elem<float> {
+struct Full {
+    using E = float;
     using Frag = FragF32;
-    static constexpr int VEC = 4;
+    using Score = floatx16;
+    static constexpr bool FINE = true;
+    static constexpr int BYTES = 4, PLANES = 1;
 };
+
+// Whole sequences of E are multiplied by Math<E>, with so many waves a SIMD:
+// two, while the operands fit 256 registers.
+template <typename E> using Math = std::conditional_t<sizeof(E) == 2, Bf16, Split>;
+constexpr int attn_waves(bool f32, int DC) { return f32 && DC > 64 ? 1 : 2; }
 
 __device__ __forceinline__ floatx16 mma(bf16x8 a, bf16x8 b, floatx16 c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// the five small products of two split operands, then the large one
+__device__ __forceinline__ floatx16 mma_rest(const FragSplit &a, const FragSplit &b, floatx16 c)
+{
+    c = mma(a.p[2], b.p[0], c);
+    c = mma(a.p[0], b.p[2], c);
+    c = mma(a.p[1], b.p[1], c);
+    c = mma(a.p[1], b.p[0], c);
+    return mma(a.p[0], b.p[1], c);
+}
+__device__ __forceinline__ floatx16 mma(const FragSplit &a, const FragSplit &b, floatx16 c)
+{
+    return mma(a.p[0], b.p[0], mma_rest(a, b, c));
 }
 __device__ __forceinline__ floatx16 mma(const FragF32 &a, const FragF32 &b, floatx16 c)
 {
@@ -56,18 +106,57 @@ __device__ __forceinline__ floatx16 mma(const FragF32 &a, const FragF32 &b, floa
     return c;
 }
 
-// The next 16 elements of a sum over the head dimension.  float32: the
-// matrix core adds them from zero and the vector unit adds that to the sum, so
-// that a score of D = 128 is 8 roundings of its own size and not 64 (scores of
-// 100, whose exponentials carry 100 times a score's relative error: a third
-// of it; the additions run beside the next products).
-__device__ __forceinline__ floatx16 add_product(bf16x8 a, bf16x8 b, floatx16 c)
+// The next 16 elements of a score.  Scores of 100, whose exponentials carry
+// 100 times their relative error, are where float32's roundings count: so Full
+// adds 16 elements at a time from zero and these sums by the vector unit (8
+// roundings of the score's size at D = 128, not 64), and Split keeps its large
+// products apart from the small ones.
+__device__ __forceinline__ void add_product(bf16x8 a, bf16x8 b, floatx16 &c) { c = mma(a, b, c); }
+__device__ __forceinline__ void add_product(const FragF32 &a, const FragF32 &b, floatx16 &c)
 {
-    return mma(a, b, c);
+    c = c + mma(a, b, floatx16{});
 }
-__device__ __forceinline__ floatx16 add_product(const FragF32 &a, const FragF32 &b, floatx16 c)
+__device__ __forceinline__ void add_product(const FragSplit &a, const FragSplit &b, ScoreSplit &c)
 {
-    return c + mma(a, b, floatx16{});
+    c.lo = mma_rest(a, b, c.lo);
+    c.hi = mma(a.p[0], b.p[0], c.hi);
+}
+__device__ __forceinline__ floatx16 value(const floatx16 &c) { return c; }
+__device__ __forceinline__ floatx16 value(const ScoreSplit &c) { return c.hi + c.lo; }
+
+__device__ __forceinline__ bf16x8 round8(const float (&v)[8])
+{
+    bf16x8 f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        f[i] = static_cast<__bf16>(v[i]);
+    return f;
+}
+__device__ __forceinline__ FragSplit split8(float (&v)[8])
+{
+    FragSplit f;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        f.p[p] = round8(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] -= static_cast<float>(f.p[p][i]);
+    }
+    return f;
+}
+template <typename M> __device__ __forceinline__ typename M::Frag make_frag(float (&v)[8])
+{
+    if constexpr (M::PLANES == 3) {
+        return split8(v);
+    } else if constexpr (M::BYTES == 2) {
+        return round8(v);
+    } else {
+        FragF32 f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f.v[i] = v[i];
+        return f;
+    }
 }
 
 // A number of powers of two as hi + lo, and 2^(x scale log2(e) - ref).  At
@@ -81,11 +170,11 @@ __device__ __forceinline__ Ref ref_of_lse(float lse)
     const float hi = lse * kLog2e;
     return Ref{hi, fmaf(lse, kLog2eLo, fmaf(lse, kLog2e, -hi))};
 }
-template <typename E>
+template <typename M>
 __device__ __forceinline__ float prob(float x, const AttnArgs &a, float hi, float lo)
 {
     float e = fmaf(x, a.c, -hi);
-    if constexpr (sizeof(E) == 4)
+    if constexpr (M::FINE)
         e += fmaf(x, a.c_lo, -lo);
     return __builtin_amdgcn_exp2f(e);
 }
@@ -98,35 +187,27 @@ __device__ __forceinline__ float log_sum(float m, float l)
 // Registers 8 s .. 8 s + 7 of a result as an operand; bfloat16 rounds to
 // nearest even (probabilities lie in [0, 1], their sum is kept in float32
 // from the unrounded values).
-template <typename E> __device__ __forceinline__ typename Elem<E>::Frag to_frag(const floatx16 &x, int s)
+template <typename M> __device__ __forceinline__ typename M::Frag to_frag(const floatx16 &x, int s)
 {
-    if constexpr (sizeof(E) == 2) {
-        bf16x8 f;
+    float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f[i] = static_cast<__bf16>(x[8 * s + i]);
-        return f;
-    } else {
-        FragF32 f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f.v[i] = x[8 * s + i];
-        return f;
-    }
+    for (int i = 0; i < 8; ++i)
+        v[i] = x[8 * s + i];
+    return make_frag<M>(v);
 }
 
 // ---- tiles in LDS: rows of DC head elements (a multiple of 32, padded with
 // zeros), 16-byte chunks permuted within the row by its number, so that both
 // reads below spread over all 64 banks: sixteen rows of one chunk
 // (read_cols), and runs of 64 or 128 bytes of four to eight rows (read_rows).
-template <typename E, int DC> struct Tile {
-    static constexpr int PITCH = (DC == 96 ? 128 : DC) * static_cast<int>(sizeof(E)); // bytes a row
-    static constexpr int CPR = DC * static_cast<int>(sizeof(E)) / 16; // chunks in use
-    static constexpr int bytes(int rows) { return rows * PITCH; }
+template <typename M, int DC, int ROWS> struct Tile {
+    using Frag = typename M::Frag;
+    static constexpr int PITCH = (DC == 96 ? 128 : DC) * M::BYTES; // bytes a row
+    static constexpr int PLANE = ROWS * PITCH, SIZE = M::PLANES * PLANE;
 
     __device__ __forceinline__ static int swz(int row)
     {
-        if constexpr (sizeof(E) == 2) {
+        if constexpr (M::BYTES == 2) {
             if constexpr (PITCH == 256)
                 return ((row >> 2) & 3) | (row & 3) << 2;
             else if constexpr (PITCH == 128)
@@ -150,22 +231,25 @@ template <typename E, int DC> struct Tile {
     // (cols_at), a step changes it by an exclusive or, rows by an offset.
     __device__ __forceinline__ static int cols_at(int row, int h)
     {
-        return row * PITCH + (((sizeof(E) == 2 ? h : 2 * h) ^ swz(row)) << 4);
+        return row * PITCH + (((M::BYTES == 2 ? h : 2 * h) ^ swz(row)) << 4);
     }
-    __device__ __forceinline__ static typename Elem<E>::Frag read_cols(const unsigned char *t,
-                                                                       int at, int s)
+    __device__ __forceinline__ static Frag read_cols(const unsigned char *t, int at, int s)
     {
-        if constexpr (sizeof(E) == 2) {
-            return *reinterpret_cast<const bf16x8 *>(t + (at ^ (s << 5)));
+        Frag f;
+        if constexpr (M::PLANES == 3) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                f.p[p] = *reinterpret_cast<const bf16x8 *>(t + p * PLANE + (at ^ (s << 5)));
+        } else if constexpr (M::BYTES == 2) {
+            f = *reinterpret_cast<const bf16x8 *>(t + (at ^ (s << 5)));
         } else {
-            FragF32 f;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float4 u = *reinterpret_cast<const float4 *>(t + (at ^ (s << 6 | j << 4)));
                 f.v[4 * j] = u.x, f.v[4 * j + 1] = u.y, f.v[4 * j + 2] = u.z, f.v[4 * j + 3] = u.w;
             }
-            return f;
         }
+        return f;
     }
 
     // Operand with rows as contraction, in the order of a result's registers:
@@ -179,7 +263,7 @@ template <typename E, int DC> struct Tile {
     __device__ __forceinline__ static RowsAt rows_at(int lane)
     {
         const int h = lane >> 5;
-        if constexpr (sizeof(E) == 2) {
+        if constexpr (M::BYTES == 2) {
             const int r = 4 * h + ((lane & 15) >> 2);
             const int c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), o = 8 * (lane & 1);
             return RowsAt{chunk_at(r, c) + o, chunk_at(r + 8, c) + o};
@@ -187,21 +271,27 @@ template <typename E, int DC> struct Tile {
             return RowsAt{chunk_at(4 * h, (lane & 31) >> 2) + 4 * (lane & 3), 0};
         }
     }
-    __device__ __forceinline__ static typename Elem<E>::Frag read_rows(unsigned char *t, RowsAt at,
-                                                                       int row0, int d)
+    __device__ __forceinline__ static bf16x8 transposed(unsigned char *t, RowsAt at, int d)
     {
-        if constexpr (sizeof(E) == 2) {
-            using lp = __attribute__((address_space(3))) shortx4 *;
-            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lp)(t + row0 * PITCH + (at.a ^ (d << 6))));
-            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lp)(t + row0 * PITCH + (at.b ^ (d << 6))));
-            return __builtin_bit_cast(bf16x8,
-                                      __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        using lp = __attribute__((address_space(3))) shortx4 *;
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(t + (at.a ^ (d << 6))));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(t + (at.b ^ (d << 6))));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    __device__ __forceinline__ static Frag read_rows(unsigned char *t, RowsAt at, int row0, int d)
+    {
+        if constexpr (M::PLANES == 3) {
+            Frag f;
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                f.p[p] = transposed(t + p * PLANE + row0 * PITCH, at, d);
+            return f;
+        } else if constexpr (M::BYTES == 2) {
+            return transposed(t + row0 * PITCH, at, d);
         } else {
             // the permutation of row 8 (i / 4) + 4 h + i % 4 is that of row 4 h
             // and that of the rest, by exclusive or
-            FragF32 f;
+            Frag f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = 8 * (i >> 2) + (i & 3);
@@ -240,43 +330,53 @@ __device__ __forceinline__ float both_max(float v)
     return fmaxf(x.lower, x.upper);
 }
 
-// One operand of 8 head elements from global memory, zeros past D; `p` is the
-// row's start (16-byte aligned), c the first element (a multiple of 8, as D).
-template <typename E>
-__device__ __forceinline__ typename Elem<E>::Frag load_frag(const E *p, int c, int D)
+// 8 head elements of a row from global memory, zeros past D; `p` is the row's
+// start (16-byte aligned), c the first element (a multiple of 8, as D).
+__device__ __forceinline__ void load8(const float *p, int c, int D, float (&v)[8])
 {
-    if constexpr (sizeof(E) == 2) {
-        uint4 u{0, 0, 0, 0};
-        if (c < D)
-            u = *reinterpret_cast<const uint4 *>(p + c);
-        return __builtin_bit_cast(bf16x8, u);
+    float4 u{0, 0, 0, 0}, w{0, 0, 0, 0};
+    if (c < D) {
+        u = *reinterpret_cast<const float4 *>(p + c);
+        w = *reinterpret_cast<const float4 *>(p + c + 4);
+    }
+    v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+    v[4] = w.x, v[5] = w.y, v[6] = w.z, v[7] = w.w;
+}
+__device__ __forceinline__ bf16x8 load8(const bf16raw *p, int c, int D)
+{
+    uint4 u{0, 0, 0, 0};
+    if (c < D)
+        u = *reinterpret_cast<const uint4 *>(p + c);
+    return __builtin_bit_cast(bf16x8, u);
+}
+// the same as an operand
+template <typename M>
+__device__ __forceinline__ typename M::Frag load_frag(const typename M::E *p, int c, int D)
+{
+    if constexpr (sizeof(typename M::E) == 2) {
+        return load8(p, c, D);
     } else {
-        FragF32 f;
-        float4 u{0, 0, 0, 0}, w{0, 0, 0, 0};
-        if (c < D) {
-            u = *reinterpret_cast<const float4 *>(p + c);
-            w = *reinterpret_cast<const float4 *>(p + c + 4);
-        }
-        f.v[0] = u.x, f.v[1] = u.y, f.v[2] = u.z, f.v[3] = u.w;
-        f.v[4] = w.x, f.v[5] = w.y, f.v[6] = w.z, f.v[7] = w.w;
-        return f;
+        float v[8];
+        load8(p, c, D, v);
+        return make_frag<M>(v);
     }
 }
-
-__device__ __forceinline__ float dot8(const FragF32 &a, const FragF32 &b)
+__device__ __forceinline__ float dot8(const float *a, const float *b, int c, int D, float s)
 {
-    float s = 0.f;
+    float x[8], y[8];
+    load8(a, c, D, x);
+    load8(b, c, D, y);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        s = fmaf(a.v[i], b.v[i], s);
+        s = fmaf(x[i], y[i], s);
     return s;
 }
-__device__ __forceinline__ float dot8(bf16x8 a, bf16x8 b)
+__device__ __forceinline__ float dot8(const bf16raw *a, const bf16raw *b, int c, int D, float s)
 {
-    float s = 0.f;
+    const bf16x8 x = load8(a, c, D), y = load8(b, c, D);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        s = fmaf(static_cast<float>(a[i]), static_cast<float>(b[i]), s);
+        s = fmaf(static_cast<float>(x[i]), static_cast<float>(y[i]), s);
     return s;
 }
 
@@ -370,24 +470,44 @@ __device__ __forceinline__ int clamp_start(const int *start, int i, int T)
 // at a time, NT threads.  Addresses are a uniform base and a 32-bit offset
 // (token strides are below 2^24 bytes), so that a load costs two or three
 // vector instructions beside itself.  Chunks past D stay zero.
-template <typename E, int DC, int ROWS, int NT> struct Stage {
-    using TL = Tile<E, DC>;
-    static constexpr int N = ROWS * TL::CPR / NT;
-    static_assert(ROWS * TL::CPR % NT == 0, "");
-    uint4 r[N];
+template <typename M, int DC, int ROWS, int NT> struct Stage {
+    using E = typename M::E;
+    using TL = Tile<M, DC, ROWS>;
+    // an item: what fills one 16-byte chunk of each plane
+    static constexpr int ELEMS = 16 / M::BYTES, VECS = ELEMS * static_cast<int>(sizeof(E)) / 16;
+    static constexpr int PER_ROW = DC / ELEMS, ITEMS = ROWS * PER_ROW, N = (ITEMS + NT - 1) / NT;
+    uint4 r[N][VECS];
 
     __device__ __forceinline__ Stage()
     {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            r[i] = uint4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < VECS; ++j)
+                r[i][j] = uint4{0, 0, 0, 0};
     }
-    __device__ __forceinline__ static int row(int i) { return (threadIdx.x % NT + NT * i) / TL::CPR; }
-    __device__ __forceinline__ static int chunk(int i) { return (threadIdx.x % NT + NT * i) % TL::CPR; }
+    __device__ __forceinline__ static int row(int i)
+    {
+        return (threadIdx.x % NT + NT * i) / PER_ROW;
+    }
+    __device__ __forceinline__ static int item(int i)
+    {
+        return (threadIdx.x % NT + NT * i) % PER_ROW;
+    }
+    // (a thread's last may be past the tile's end)
+    __device__ __forceinline__ static bool has(int i)
+    {
+        return (i + 1) * NT <= ITEMS || threadIdx.x % NT + NT * i < ITEMS;
+    }
+    // the item's place in its row, in bytes
+    __device__ __forceinline__ static uint32_t place(int i) { return 16 * VECS * item(i); }
     __device__ __forceinline__ void get(int i, const E *base, uint32_t bytes, int D)
     {
-        if (chunk(i) * Elem<E>::VEC < D)
-            r[i] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(base) + bytes);
+        if (has(i) && item(i) * ELEMS < D)
+#pragma unroll
+            for (int j = 0; j < VECS; ++j)
+                r[i][j] = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(base) +
+                                                          bytes)[j];
     }
     // rows from `base` on, ld bytes apart; those past the last of `left`
     // repeat it
@@ -395,13 +515,28 @@ template <typename E, int DC, int ROWS, int NT> struct Stage {
     {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            get(i, base, __umul24(min(row(i), left - 1), ld) + 16 * chunk(i), D);
+            get(i, base, __umul24(min(row(i), left - 1), ld) + place(i), D);
     }
     __device__ __forceinline__ void put(unsigned char *t) const
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            *reinterpret_cast<uint4 *>(t + TL::chunk_at(row(i), chunk(i))) = r[i];
+        for (int i = 0; i < N; ++i) {
+            if (!has(i))
+                break;
+            unsigned char *to = t + TL::chunk_at(row(i), item(i));
+            if constexpr (M::PLANES == 3) {
+                float v[8] = {__uint_as_float(r[i][0].x), __uint_as_float(r[i][0].y),
+                              __uint_as_float(r[i][0].z), __uint_as_float(r[i][0].w),
+                              __uint_as_float(r[i][1].x), __uint_as_float(r[i][1].y),
+                              __uint_as_float(r[i][1].z), __uint_as_float(r[i][1].w)};
+                const FragSplit f = split8(v);
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    *reinterpret_cast<bf16x8 *>(to + p * TL::PLANE) = f.p[p];
+            } else {
+                *reinterpret_cast<uint4 *>(to) = r[i][0];
+            }
+        }
     }
 };
 

@@ -226,16 +226,15 @@ template <int NT> __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl
 
 // ---- dq: rows as in the forward, 32 a wave of NW, BK keys a tile.
 //   X^T = K Q^T and dP^T = V dO^T (keys as rows), dQ^T += K^T dS^T
-template <typename E, int DC, int BK, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, const E *v,
-                                                        const E *o, const float *lse,
-                                                        const E *dout, E *dq, float *delta,
-                                                        AttnArgs a, AttnGrads gr, KeyPlan pl)
+template <typename M, int DC, int BK, int NW, typename E = typename M::E>
+__global__ __launch_bounds__(64 * NW, attn_waves(sizeof(E) == 4, DC)) void
+attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, const E *dout, E *dq,
+          float *delta, AttnArgs a, AttnGrads gr, KeyPlan pl)
 {
-    using TL = Tile<E, DC>;
-    using Frag = typename Elem<E>::Frag;
+    using TL = Tile<M, DC, BK>;
+    using Frag = typename M::Frag;
     constexpr int TR = 32 * NW, KT = BK / 32, DT = DC / 32, DS = DC / 16;
-    constexpr int TB = TL::bytes(BK);
+    constexpr int TB = TL::SIZE;
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
     if (blockIdx.x == 0) {
         static_assert(sizeof(smem) >= plan_lds(64 * NW), "");
@@ -273,9 +272,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, 
     float dl = 0.f;
 #pragma unroll
     for (int s = 0; s < DS; ++s) {
-        qf[s] = load_frag<E>(qp, 16 * s + 8 * h, a.D);
-        gf[s] = load_frag<E>(gp, 16 * s + 8 * h, a.D);
-        dl += dot8(gf[s], load_frag<E>(op, 16 * s + 8 * h, a.D));
+        qf[s] = load_frag<M>(qp, 16 * s + 8 * h, a.D);
+        gf[s] = load_frag<M>(gp, 16 * s + 8 * h, a.D);
+        dl = dot8(gp, op, 16 * s + 8 * h, a.D, dl);
     }
     dl = both_sum(dl);
     if (row < rows && h == 0)
@@ -293,7 +292,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, 
     least = __builtin_amdgcn_readfirstlane(least);
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
-    Stage<E, DC, BK, 64 * NW> ks, vs;
+    Stage<M, DC, BK, 64 * NW> ks, vs;
     const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     // rows past the end repeat the last one: their scores are masked
     auto load = [&](int tile) {
@@ -328,15 +327,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, 
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
                 const int key0 = j * BK + 32 * t;
-                floatx16 x = floatx16{}, dp = floatx16{};
+                typename M::Score sc{};
+                floatx16 dp = floatx16{};
 #pragma unroll
                 for (int s = 0; s < DS; ++s) {
-                    x = add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], x);
-                    dp = add_product(TL::read_cols(vt + 32 * t * TL::PITCH, ca, s), gf[s], dp);
+                    add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], sc);
+                    dp = mma(TL::read_cols(vt + 32 * t * TL::PITCH, ca, s), gf[s], dp);
                 }
+                floatx16 x = value(sc);
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    x[r] = prob<E>(x[r], a, ref.hi, ref.lo) * (dp[r] - dl);
+                    x[r] = prob<M>(x[r], a, ref.hi, ref.lo) * (dp[r] - dl);
                 if (key0 + 32 > least) {
                     const int left = see - key0 - 4 * h;
 #pragma unroll
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, 
                 }
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    const Frag sf = to_frag<E>(x, s);
+                    const Frag sf = to_frag<M>(x, s);
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
                         acc[d] = mma(TL::read_rows(kt, ra, 32 * t + 16 * s, d), sf, acc[d]);
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_dq_k(const E *q, const E *k, 
 
 // Rows a step of attn_dkv_k takes, and the blocks of it that a compute unit
 // holds at once (registers and LDS).
-constexpr int dkv_rows(bool f32, int DC) { return !f32 && DC <= 96 ? 64 : 32; }
+constexpr int dkv_rows(bool f32, int DC) { return DC <= (f32 ? 32 : 96) ? 64 : 32; }
 constexpr int dkv_per_cu(bool f32, int DC)
 {
     return DC <= 32 && !f32 ? 4 : DC <= 64 || !f32 ? 2 : 1;
@@ -378,21 +379,21 @@ constexpr int dkv_per_cu(bool f32, int DC)
 //   X = Q K^T and dP = dO V^T (query rows as rows; a lane holds one key),
 //   dV^T += dO^T P, dK^T += Q^T dS
 // Blocks take pieces off the list until it is empty.
-template <typename E, int DC, int BR>
-__global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_k(const E *q, const E *k, const E *v,
-                                                     const float *lse, const E *dout,
-                                                     const float *delta, E *dk, E *dv, AttnArgs a,
-                                                     AttnGrads gr, KeyPlan pl)
+template <typename M, int DC, int BR, typename E = typename M::E>
+__global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void
+attn_dkv_k(const E *q, const E *k, const E *v, const float *lse, const E *dout, const float *delta,
+           E *dk, E *dv, AttnArgs a, AttnGrads gr, KeyPlan pl)
 {
-    using TL = Tile<E, DC>;
-    using Frag = typename Elem<E>::Frag;
+    using TL = Tile<M, DC, BR>;
+    using VT = Tile<M, DC, 128>;
+    using Frag = typename M::Frag;
     constexpr int RT = BR / 32, DT = DC / 32, DS = DC / 16;
-    constexpr int TB = TL::bytes(BR);
+    constexpr int TB = TL::SIZE;
     static_assert(BR <= 64, "");
     constexpr int BUF = 2 * TB + 4 * BR * 4; // Q, dO; lse, -D, keys seen, lse's rest
     // the values' operands stay in registers where they fit beside the sums
-    constexpr bool VL = DT > (sizeof(E) == 4 ? 2 : 3);
-    __shared__ __align__(16) unsigned char smem[2 * BUF + (VL ? TL::bytes(128) : 0)];
+    constexpr bool VL = M::PLANES == 1 && DC > 96;
+    __shared__ __align__(16) unsigned char smem[2 * BUF + (VL ? VT::SIZE : 0)];
     __shared__ int next, ends[kClasses];
     unsigned char *vl = smem + 2 * BUF;
 
@@ -426,12 +427,12 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
             const int64_t at = pc.k0 + kc;
-            kf[s] = load_frag<E>(k + at * a.ldk + kvh * a.D, 16 * s + 8 * h, a.D);
+            kf[s] = load_frag<M>(k + at * a.ldk + kvh * a.D, 16 * s + 8 * h, a.D);
             if constexpr (!VL)
-                vf[s] = load_frag<E>(v + at * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
+                vf[s] = load_frag<M>(v + at * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
         }
         if constexpr (VL) {
-            Stage<E, DC, 128, 256> vs;
+            Stage<M, DC, 128, 256> vs;
             vs.rows(v + static_cast<int64_t>(pc.k0 + key0) * a.ldv + kvh * a.D,
                     a.ldv * sizeof(E), m - key0, a.D);
             vs.put(vl);
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
         const E *gp = dout + pc.q0 * gr.lddo + static_cast<int64_t>(kvh) * g.G * a.D;
         const float *lp = lse + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
         const float *dp0 = delta + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
-        Stage<E, DC, BR, 256> qs, gs;
+        Stage<M, DC, BR, 256> qs, gs;
         const uint32_t ldq = a.ldq * sizeof(E), ldg = gr.lddo * sizeof(E);
         const float per_head = 1.f / g.G;
         Ref ls{0.f, 0.f};
@@ -462,7 +463,7 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
             for (int i = 0; i < qs.N; ++i) {
                 int t, hd;
                 place(qs.row(i), t, hd);
-                const uint32_t c = __umul24(hd, a.D * sizeof(E)) + 16 * qs.chunk(i);
+                const uint32_t c = __umul24(hd, a.D * sizeof(E)) + qs.place(i);
                 qs.get(i, qt, __umul24(t, ldq) + c, a.D);
                 gs.get(i, gt, __umul24(t, ldg) + c, a.D);
             }
@@ -524,21 +525,19 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
                 for (int t = 0; t < RT; ++t) {
                     if (RT > 1 && j * BR + 32 * t >= rows)
                         break;
-                    // dP starts from -D, or, where there are no registers for
-                    // that beside the operands, ends with it
-                    constexpr bool F32 = sizeof(E) == 4, EARLY = !F32 || DC > 64;
-                    floatx16 x = floatx16{}, dp = floatx16{};
+                    typename M::Score sc{};
+                    floatx16 dp; // from -D on
                     const int at = 32 * t + 4 * h;
-                    if constexpr (EARLY)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            set_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
+                    for (int i = 0; i < 4; ++i)
+                        set_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
 #pragma unroll
                     for (int s = 0; s < DS; ++s) {
-                        x = add_product(TL::read_cols(qt + 32 * t * TL::PITCH, ca, s), kf[s], x);
-                        const Frag vs = VL ? TL::read_cols(vw, ca, s) : vf[VL ? 0 : s];
-                        dp = add_product(TL::read_cols(gt + 32 * t * TL::PITCH, ca, s), vs, dp);
+                        add_product(TL::read_cols(qt + 32 * t * TL::PITCH, ca, s), kf[s], sc);
+                        const Frag vs = VL ? VT::read_cols(vw, ca, s) : vf[VL ? 0 : s];
+                        dp = mma(TL::read_cols(gt + 32 * t * TL::PITCH, ca, s), vs, dp);
                     }
+                    floatx16 x = value(sc);
                     if (masked) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -555,21 +554,19 @@ __global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void attn_dkv_
                         const float4 l4 = *reinterpret_cast<const float4 *>(lt + at + 8 * i);
                         const float l[4] = {l4.x, l4.y, l4.z, l4.w};
                         float4 r4{0.f, 0.f, 0.f, 0.f};
-                        if constexpr (F32)
+                        if constexpr (M::FINE)
                             r4 = *reinterpret_cast<const float4 *>(lt + 3 * BR + at + 8 * i);
-                        if constexpr (!EARLY)
-                            add_quad(dp, i, *reinterpret_cast<const float4 *>(dt + at + 8 * i));
                         const float ll[4] = {r4.x, r4.y, r4.z, r4.w};
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            const float p = prob<E>(x[4 * i + r], a, l[r], ll[r]);
+                            const float p = prob<M>(x[4 * i + r], a, l[r], ll[r]);
                             x[4 * i + r] = p;
                             dp[4 * i + r] *= p;
                         }
                     }
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        const Frag pf = to_frag<E>(x, s), sf = to_frag<E>(dp, s);
+                        const Frag pf = to_frag<M>(x, s), sf = to_frag<M>(dp, s);
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
                             dva[d] = mma(TL::read_rows(gt, ra, 32 * t + 16 * s, d), pf, dva[d]);
@@ -649,11 +646,10 @@ hipError_t launch_dq(const E *q, const E *k, const E *v, const E *o, const float
                      const E *dout, E *dq, float *delta, AttnArgs a, const AttnGrads &gr,
                      const KeyPlan &pl, hipStream_t st)
 {
-    constexpr bool F32 = sizeof(E) == 4;
-    constexpr int BK = NW == 2 || (F32 && DC > 64) ? 32 : 64;
+    constexpr int BK = NW == 2 || (sizeof(E) == 4 && DC > 32) ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
     // one block more, the first, divides the keys' work
-    HEX_LAUNCH((attn_dq_k<E, DC, BK, NW>), dim3(attn_blocks(a) + 1), dim3(64 * NW), 0, st, q, k,
+    HEX_LAUNCH((attn_dq_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a) + 1), dim3(64 * NW), 0, st, q, k,
                v, o, lse, dout, dq, delta, a, gr, pl);
     return hipGetLastError();
 }
@@ -669,7 +665,7 @@ hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *l
                        : launch_dq<E, DC, 4>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st);
     if (e != hipSuccess || a.Tk == 0)
         return e;
-    HEX_LAUNCH((attn_dkv_k<E, DC, dkv_rows(F32, DC)>), dim3(static_cast<uint32_t>(pl.blocks)),
+    HEX_LAUNCH((attn_dkv_k<Math<E>, DC, dkv_rows(F32, DC)>), dim3(static_cast<uint32_t>(pl.blocks)),
                dim3(256), 0, st, q, k, v, lse, dout, delta, dk, dv, a, gr, pl);
     e = hipGetLastError();
     // no tile of so few rows is divided

@@ -25,14 +25,14 @@ namespace {
 constexpr float kSlack = 8.f; // in powers of two
 
 // NW waves, BK keys a tile.
-template <typename E, int DC, int BK, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k, const E *v, E *o,
-                                                         float *lse, AttnArgs a)
+template <typename M, int DC, int BK, int NW, typename E = typename M::E>
+__global__ __launch_bounds__(64 * NW, attn_waves(sizeof(E) == 4, DC)) void
+attn_fwd_k(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a)
 {
-    using TL = Tile<E, DC>;
-    using Frag = typename Elem<E>::Frag;
+    using TL = Tile<M, DC, BK>;
+    using Frag = typename M::Frag;
     constexpr int TR = 32 * NW, KT = BK / 32, DT = DC / 32, DS = DC / 16;
-    constexpr int TB = TL::bytes(BK);
+    constexpr int TB = TL::SIZE;
     __shared__ __align__(16) unsigned char smem[4 * TB]; // K, V, K, V
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k,
     Frag qf[DS];
 #pragma unroll
     for (int s = 0; s < DS; ++s)
-        qf[s] = load_frag<E>(qp, 16 * s + 8 * h, a.D);
+        qf[s] = load_frag<M>(qp, 16 * s + 8 * h, a.D);
     // keys that any row of the block sees; of the wave; and that all of it see
     const int r_last = min(rows, row0 + TR) - 1;
     const int end = a.causal ? min(m, max(0, row_token(g, r_last) + ahead + 1)) : m;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k,
     least = __builtin_amdgcn_readfirstlane(least);
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
-    Stage<E, DC, BK, 64 * NW> ks, vs;
+    Stage<M, DC, BK, 64 * NW> ks, vs;
     const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     // rows past the end repeat the last one: their scores are masked
     auto load = [&](int tile) {
@@ -101,10 +101,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k,
         floatx16 x[KT];
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
-            x[t] = floatx16{};
+            typename M::Score sc{};
 #pragma unroll
             for (int s = 0; s < DS; ++s)
-                x[t] = add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], x[t]);
+                add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], sc);
+            x[t] = value(sc);
         }
         if (key0 + BK > least) {
             const int left = see - key0 - 4 * h;
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k,
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = prob<E>(x[t][r], a, ref, 0.f);
+                const float p = prob<M>(x[t][r], a, ref, 0.f);
                 x[t][r] = p;
                 sum += p;
             }
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_fwd_k(const E *q, const E *k,
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const Frag pf = to_frag<E>(x[t], s);
+                const Frag pf = to_frag<M>(x[t], s);
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
                     acc[d] = mma(TL::read_rows(vt, ra, 32 * t + 16 * s, d), pf, acc[d]);
@@ -186,10 +187,9 @@ template <typename E, int DC, int NW>
 hipError_t launch_waves(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a,
                         hipStream_t st)
 {
-    constexpr bool F32 = sizeof(E) == 4;
-    constexpr int BK = NW == 2 || (F32 && DC > 64) ? 32 : 64;
+    constexpr int BK = NW == 2 || (sizeof(E) == 4 && DC > 32) ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
-    HEX_LAUNCH((attn_fwd_k<E, DC, BK, NW>), dim3(attn_blocks(a)), dim3(64 * NW), 0, st, q, k, v,
+    HEX_LAUNCH((attn_fwd_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a)), dim3(64 * NW), 0, st, q, k, v,
                o, lse, a);
     return hipGetLastError();
 }

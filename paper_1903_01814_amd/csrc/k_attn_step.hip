@@ -21,14 +21,14 @@ namespace {
 constexpr int kStepWaves = 4;
 constexpr int kMaxRuns = 1024; // of a row, to be joined in LDS
 
-template <typename E, int DC>
+template <typename M, int DC, typename E = typename M::E>
 __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void attn_step_k(
     const E *q, const E *k, const E *v, E *o, float *part, float2 *stat, AttnArgs a, StepPlan pl)
 {
-    using TL = Tile<E, DC>;
-    using Frag = typename Elem<E>::Frag;
     constexpr int DT = DC / 32, DS = DC / 16, BK = 32;
-    constexpr int TB = TL::bytes(BK);
+    using TL = Tile<M, DC, BK>;
+    using Frag = typename M::Frag;
+    constexpr int TB = TL::SIZE;
     static_assert(2 * TB >= 32 * DC * 4, "");
     __shared__ __align__(16) unsigned char smem[kStepWaves][2 * TB];
     __shared__ float stats[2][kStepWaves][32];
@@ -60,12 +60,12 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
     Frag qf[DS];
 #pragma unroll
     for (int s = 0; s < DS; ++s)
-        qf[s] = load_frag<E>(q + row * a.D, 16 * s + 8 * h, a.D);
+        qf[s] = load_frag<M>(q + row * a.D, 16 * s + 8 * h, a.D);
     const int see = r < rows ? max(0, m - pl.n + t + 1) : 0;
 
     const E *kp = k + kb * a.ldk + kvh * a.D, *vp = v + kb * a.ldv + kvh * a.D;
     unsigned char *kt = smem[wave], *vt = kt + TB;
-    Stage<E, DC, BK, 64> ks, vs;
+    Stage<M, DC, BK, 64> ks, vs;
     const uint32_t ldk = a.ldk * sizeof(E), ldv = a.ldv * sizeof(E);
     auto load = [&](int k0) {
         ks.rows(kp + k0 * a.ldk, ldk, m - k0, a.D);
@@ -97,10 +97,11 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         if (k0 + kStepWaves * BK < end)
             load(k0 + kStepWaves * BK);
-        floatx16 x = floatx16{};
+        typename M::Score sc{};
 #pragma unroll
         for (int s = 0; s < DS; ++s)
-            x = add_product(TL::read_cols(kt, ca, s), qf[s], x);
+            add_product(TL::read_cols(kt, ca, s), qf[s], sc);
+        floatx16 x = value(sc);
         // keys past the run belong to another block or do not exist
         const int left = min(see, end) - k0 - 4 * h;
         float top = -HUGE_VALF;
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
         const float ref = mx == -HUGE_VALF ? 0.f : mx;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            x[i] = prob<E>(x[i], a, ref, 0.f);
+            x[i] = prob<M>(x[i], a, ref, 0.f);
             sum += x[i];
         }
 #pragma unroll
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(64 * kStepWaves, sizeof(E) * DC > 256 ? 1 : 2) void
             acc[d] *= f;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const Frag pf = to_frag<E>(x, s);
+            const Frag pf = to_frag<M>(x, s);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
                 acc[d] = mma(TL::read_rows(vt, ra, 16 * s, d), pf, acc[d]);
@@ -275,7 +276,7 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, void *ws
     float *part = static_cast<float *>(ws);
     float2 *stat = reinterpret_cast<float2 *>(part + static_cast<int64_t>(pl.splits) * pl.rows * a.D);
     const uint32_t blocks = static_cast<uint32_t>(a.S) * pl.row_tiles * pl.splits * a.Hkv;
-    HEX_LAUNCH((attn_step_k<E, DC>), dim3(blocks), dim3(64 * kStepWaves), 0, st,
+    HEX_LAUNCH((attn_step_k<std::conditional_t<sizeof(E) == 2, Bf16, Full>, DC>), dim3(blocks), dim3(64 * kStepWaves), 0, st,
                static_cast<const E *>(q), static_cast<const E *>(k), static_cast<const E *>(v),
                static_cast<E *>(o), part, stat, a, pl);
     const hipError_t e = hipGetLastError();

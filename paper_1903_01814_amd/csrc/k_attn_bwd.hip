@@ -18,7 +18,7 @@ namespace hexk {
 namespace attn {
 namespace {
 
-// ---- how the keys' work is divided.  A tile of 128 keys of one sequence and
+// ---- how the keys' work is divided.  A tile of keys of one sequence and
 // key head takes as many units as it has tiles of rows that see it, and kFixed
 // for its own loads and stores.  Causal, a sequence's first keys have the whole
 // sequence's rows and its last ones a few, and sequences differ: one block a
@@ -61,13 +61,13 @@ __device__ __forceinline__ KeyUnits key_units(const AttnArgs &a, const KeyPlan &
 {
     KeyUnits u;
     u.nt = (n * a.group.G + pl.row_tile - 1) / pl.row_tile;
-    u.tiles = (m + 127) / 128;
+    u.tiles = static_cast<int>((static_cast<uint32_t>(m) + pl.key_tile - 1) / pl.key_tile);
     u.k = u.a0 = 0;
     u.lo = u.hi = u.tiles;
     if (a.causal) {
         const int64_t x = static_cast<int64_t>(m - n) * a.group.G; // row_tile: a power of two
         u.a0 = static_cast<int>((x + pl.row_tile - 1) >> pl.row_shift);
-        u.k = (128 >> pl.row_shift) * a.group.G;
+        u.k = (pl.key_tile >> pl.row_shift) * a.group.G;
         u.lo = u.a0 >= 0 ? u.a0 / u.k + 1 : 0;
         u.hi = u.nt + u.a0 >= 0 ? (u.nt + u.a0) / u.k + 1 : 0;
     }
@@ -91,7 +91,8 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int s)
 // alike), a thread taking a tile at a time.  lds: plan_lds(NT) bytes.
 constexpr int plan_lds(int NT) { return NT * (2 * 8 + kClasses * 4) + (kClasses + 2) * 4; }
 
-template <int NT> __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *lds)
+template <int NT>
+__device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *lds)
 {
     int64_t *before = reinterpret_cast<int64_t *>(lds); // units, tiles before each
     int64_t *tbefore = before + NT;                     // thread's run of sequences
@@ -158,7 +159,7 @@ template <int NT> __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl
         pc.parts = 4 * static_cast<int64_t>(rows + kFixed) <= 5 * share
                        ? 1
                        : static_cast<int>((rows + share - 1) / share);
-        pc.q0 = q.q0, pc.n = q.n, pc.k0 = q.k0, pc.m = q.m, pc.key0 = j * 128;
+        pc.q0 = q.q0, pc.n = q.n, pc.k0 = q.k0, pc.m = q.m, pc.key0 = j * pl.key_tile;
         const int64_t size = rows / pc.parts + kFixed; // up to 5/4 of a share
         cls = kClasses - 1 - static_cast<int>(min(6 * size / share, INT64_C(kClasses - 1)));
     };
@@ -367,25 +368,35 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
         store_col(p, acc[d], 32 * d + 4 * h, a.D, a.scale);
 }
 
-// Rows a step of attn_dkv_k takes, and the blocks of it that a compute unit
-// holds at once (registers and LDS).
+// Rows a step of attn_dkv_k takes, and the waves of it that a SIMD holds at
+// once (registers and LDS).
 constexpr int dkv_rows(bool f32, int DC) { return DC <= (f32 ? 32 : 96) ? 64 : 32; }
-constexpr int dkv_per_cu(bool f32, int DC)
+constexpr int dkv_waves(bool f32, int DC)
 {
     return DC <= 32 && !f32 ? 4 : DC <= 64 || !f32 ? 2 : 1;
 }
 
-// ---- dk and dv: tiles of 128 keys, 32 a wave; BR rows a step.
+// Tiles of 256 keys instead of 128 (bfloat16, heads past 32) where sequences
+// have so many keys on average: half as many reads of Q and dO.  16 heads of
+// 128 on 4: 24 sequences of 2048 keys 2010 -> 1730 us, of 500 to 5000 causal
+// 1563 -> 1397, 128 of 370 505 -> 471; but 256 of 150 194 -> 228, 512 of 60
+// 124 -> 177.  Heads of 64: 24 of 2048 1100 -> 1026, of 500 to 5000 739 -> 687;
+// but 128 of 370 263 -> 270, 64 of 470 129 -> 141.
+constexpr bool dkv_wide(bool f32, int DC) { return !f32 && DC > 32; }
+constexpr int dkv_wide_keys(int DC) { return DC > 96 ? 320 : 1024; }
+
+// ---- dk and dv: tiles of KT keys, 32 a wave; BR rows a step.
 //   X = Q K^T and dP = dO V^T (query rows as rows; a lane holds one key),
 //   dV^T += dO^T P, dK^T += Q^T dS
 // Blocks take pieces off the list until it is empty.
-template <typename M, int DC, int BR, typename E = typename M::E>
-__global__ __launch_bounds__(256, dkv_per_cu(sizeof(E) == 4, DC)) void
+template <typename M, int DC, int BR, int KT, typename E = typename M::E>
+__global__ __launch_bounds__(2 * KT, dkv_waves(sizeof(E) == 4, DC)) void
 attn_dkv_k(const E *q, const E *k, const E *v, const float *lse, const E *dout, const float *delta,
            E *dk, E *dv, AttnArgs a, AttnGrads gr, KeyPlan pl)
 {
     using TL = Tile<M, DC, BR>;
-    using VT = Tile<M, DC, 128>;
+    using VT = Tile<M, DC, KT>;
+    constexpr int NT = 2 * KT;
     using Frag = typename M::Frag;
     constexpr int RT = BR / 32, DT = DC / 32, DS = DC / 16;
     constexpr int TB = TL::SIZE;
@@ -432,7 +443,7 @@ attn_dkv_k(const E *q, const E *k, const E *v, const float *lse, const E *dout, 
                 vf[s] = load_frag<M>(v + at * a.ldv + kvh * a.D, 16 * s + 8 * h, a.D);
         }
         if constexpr (VL) {
-            Stage<M, DC, 128, 256> vs;
+            Stage<M, DC, KT, NT> vs;
             vs.rows(v + static_cast<int64_t>(pc.k0 + key0) * a.ldv + kvh * a.D,
                     a.ldv * sizeof(E), m - key0, a.D);
             vs.put(vl);
@@ -442,7 +453,7 @@ attn_dkv_k(const E *q, const E *k, const E *v, const float *lse, const E *dout, 
         const E *gp = dout + pc.q0 * gr.lddo + static_cast<int64_t>(kvh) * g.G * a.D;
         const float *lp = lse + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
         const float *dp0 = delta + static_cast<int64_t>(pc.q0) * a.Hq + kvh * g.G;
-        Stage<M, DC, BR, 256> qs, gs;
+        Stage<M, DC, BR, NT> qs, gs;
         const uint32_t ldq = a.ldq * sizeof(E), ldg = gr.lddo * sizeof(E);
         const float per_head = 1.f / g.G;
         Ref ls{0.f, 0.f};
@@ -581,15 +592,14 @@ attn_dkv_k(const E *q, const E *k, const E *v, const float *lse, const E *dout, 
         }
 
         if (pc.parts > 1) {
-            float4 *part = pl.part +
-                           (2 * static_cast<int64_t>(kvh) * pl.shares + pc.slot) * (2 * DT * 4 * 256) +
-                           threadIdx.x;
+            const int64_t slot = 2 * static_cast<int64_t>(kvh) * pl.shares + pc.slot;
+            float4 *part = pl.part + slot * (2 * DT * 4 * NT) + threadIdx.x;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    part[(d * 4 + i) * 256] = quad(dka[d], i);
-                    part[((DT + d) * 4 + i) * 256] = quad(dva[d], i);
+                    part[(d * 4 + i) * NT] = quad(dka[d], i);
+                    part[((DT + d) * 4 + i) * NT] = quad(dva[d], i);
                 }
         } else if (key < m) {
             E *kp = dk + (pc.k0 + key) * gr.lddk + kvh * a.D;
@@ -610,8 +620,8 @@ attn_dkv_k(const E *q, const E *k, const E *v, const float *lse, const E *dout, 
 
 // Adds up the pieces of divided tiles: block = (head, divided tile, 32 elements
 // of dk or dv), thread = the lane that holds them in attn_dkv_k.
-template <typename E, int DC>
-__global__ __launch_bounds__(256) void attn_dkv_join_k(E *dk, E *dv, AttnArgs a, AttnGrads gr,
+template <typename E, int DC, int NT>
+__global__ __launch_bounds__(NT) void attn_dkv_join_k(E *dk, E *dv, AttnArgs a, AttnGrads gr,
                                                        KeyPlan pl)
 {
     constexpr int DT = DC / 32;
@@ -624,11 +634,11 @@ __global__ __launch_bounds__(256) void attn_dkv_join_k(E *dk, E *dv, AttnArgs a,
     for (int i = 0; i < pc.parts; ++i) {
         const float4 *p = pl.part +
                           (2 * static_cast<int64_t>(kvh) * pl.shares + pc.slot + i) *
-                              (2 * DT * 4 * 256) +
-                          which * 4 * 256 + threadIdx.x;
+                              (2 * DT * 4 * NT) +
+                          which * 4 * NT + threadIdx.x;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            add_quad(sum, c, p[c * 256]);
+            add_quad(sum, c, p[c * NT]);
     }
     const int lane = threadIdx.x & 63;
     const int key = pc.key0 + (threadIdx.x >> 6) * 32 + (lane & 31), c0 = 4 * (lane >> 5);
@@ -649,8 +659,27 @@ hipError_t launch_dq(const E *q, const E *k, const E *v, const E *o, const float
     constexpr int BK = NW == 2 || (sizeof(E) == 4 && DC > 32) ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
     // one block more, the first, divides the keys' work
-    HEX_LAUNCH((attn_dq_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a) + 1), dim3(64 * NW), 0, st, q, k,
-               v, o, lse, dout, dq, delta, a, gr, pl);
+    HEX_LAUNCH((attn_dq_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a) + 1), dim3(64 * NW), 0, st, q,
+               k, v, o, lse, dout, dq, delta, a, gr, pl);
+    return hipGetLastError();
+}
+
+template <typename E, int DC, int KT>
+hipError_t launch_dkv(const E *q, const E *k, const E *v, const float *lse, const E *dout, E *dk,
+                      E *dv, const float *delta, const AttnArgs &a, const AttnGrads &gr,
+                      const KeyPlan &pl, hipStream_t st)
+{
+    HEX_LAUNCH((attn_dkv_k<Math<E>, DC, dkv_rows(sizeof(E) == 4, DC), KT>),
+               dim3(static_cast<uint32_t>(pl.blocks)), dim3(2 * KT), 0, st, q, k, v, lse, dout,
+               delta, dk, dv, a, gr, pl);
+    const hipError_t e = hipGetLastError();
+    // no tile of so few rows is divided
+    const int64_t row_tiles = static_cast<int64_t>(a.Tq) * a.group.G / pl.row_tile + 1;
+    if (e != hipSuccess || row_tiles + kFixed <= kLeast)
+        return e;
+    HEX_LAUNCH((attn_dkv_join_k<E, DC, 2 * KT>),
+               dim3(static_cast<uint32_t>(pl.shares) * a.Hkv, DC / 16), dim3(2 * KT), 0, st, dk, dv,
+               a, gr, pl);
     return hipGetLastError();
 }
 
@@ -659,22 +688,15 @@ hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *l
                   E *dq, E *dk, E *dv, float *delta, const AttnArgs &a, const AttnGrads &gr,
                   const KeyPlan &pl, hipStream_t st)
 {
-    constexpr bool F32 = sizeof(E) == 4;
-    hipError_t e = attn_short(a)
-                       ? launch_dq<E, DC, 2>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st)
-                       : launch_dq<E, DC, 4>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st);
+    const hipError_t e = attn_short(a)
+                             ? launch_dq<E, DC, 2>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st)
+                             : launch_dq<E, DC, 4>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st);
     if (e != hipSuccess || a.Tk == 0)
         return e;
-    HEX_LAUNCH((attn_dkv_k<Math<E>, DC, dkv_rows(F32, DC)>), dim3(static_cast<uint32_t>(pl.blocks)),
-               dim3(256), 0, st, q, k, v, lse, dout, delta, dk, dv, a, gr, pl);
-    e = hipGetLastError();
-    // no tile of so few rows is divided
-    const int64_t row_tiles = static_cast<int64_t>(a.Tq) * a.group.G / pl.row_tile + 1;
-    if (e != hipSuccess || row_tiles + kFixed <= kLeast)
-        return e;
-    HEX_LAUNCH((attn_dkv_join_k<E, DC>), dim3(static_cast<uint32_t>(pl.shares) * a.Hkv, DC / 16),
-               dim3(256), 0, st, dk, dv, a, gr, pl);
-    return hipGetLastError();
+    if constexpr (dkv_wide(sizeof(E) == 4, DC))
+        if (pl.key_tile == 256)
+            return launch_dkv<E, DC, 256>(q, k, v, lse, dout, dk, dv, delta, a, gr, pl, st);
+    return launch_dkv<E, DC, 128>(q, k, v, lse, dout, dk, dv, delta, a, gr, pl, st);
 }
 
 template <typename E>
@@ -701,7 +723,7 @@ size_t round16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 // the workspace: delta, the plan's parts, partial sums
 struct BwdSpace {
     size_t before, next, ends, divided, list, part, bytes;
-    int shares, blocks, room, row_tile;
+    int shares, blocks, room, row_tile, key_tile;
 };
 BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
 {
@@ -711,9 +733,10 @@ BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
     w.row_tile = dkv_rows(f32, DC);
     // no more shares of a head than make kLeast units each, no more blocks
     // than pieces
-    const double tiles = Tk / 128 + static_cast<double>(S);
+    w.key_tile = dkv_wide(f32, DC) && Tk / dkv_wide_keys(DC) >= S ? 256 : 128;
+    const double tiles = Tk / w.key_tile + static_cast<double>(S);
     const double units = tiles * (static_cast<double>(Tq) * (Hq / Hkv) / w.row_tile + 1 + kFixed);
-    const int held = dkv_per_cu(f32, DC) * device_cus();
+    const int held = dkv_waves(f32, DC) * 128 / w.key_tile * device_cus();
     const int most = (kShares * held + Hkv - 1) / Hkv;
     w.shares = units / kLeast + 1 < most ? static_cast<int>(units / kLeast) + 1 : most;
     // a divided tile has more than a share, so that there are fewer of them
@@ -726,7 +749,8 @@ BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
     w.divided = w.ends + 256;
     w.list = w.divided + round16(static_cast<size_t>(w.shares) * sizeof(KeyPiece));
     w.part = w.list + round16(static_cast<size_t>(w.room) * sizeof(KeyPiece));
-    w.bytes = w.part + static_cast<size_t>(w.shares) * Hkv * 2 * (2 * 128 * DC) * sizeof(float);
+    w.bytes = w.part + static_cast<size_t>(w.shares) * Hkv * 2 *
+                           (2 * static_cast<size_t>(w.key_tile) * DC) * sizeof(float);
     return w;
 }
 
@@ -750,6 +774,7 @@ hipError_t attn_bwd(const void *q, const void *k, const void *v, const void *o, 
     pl.blocks = w.blocks;
     pl.room = w.room;
     pl.row_tile = w.row_tile;
+    pl.key_tile = w.key_tile;
     pl.row_shift = w.row_tile == 64 ? 6 : 5;
     float *delta = static_cast<float *>(ws);
     return dt == F32

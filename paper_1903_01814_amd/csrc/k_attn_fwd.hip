@@ -189,8 +189,8 @@ hipError_t launch_waves(const E *q, const E *k, const E *v, E *o, float *lse, At
 {
     constexpr int BK = NW == 2 || (sizeof(E) == 4 && DC > 32) ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
-    HEX_LAUNCH((attn_fwd_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a)), dim3(64 * NW), 0, st, q, k, v,
-               o, lse, a);
+    HEX_LAUNCH((attn_fwd_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a)), dim3(64 * NW), 0, st, q, k,
+               v, o, lse, a);
     return hipGetLastError();
 }
 

@@ -274,9 +274,11 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, void *ws
                   const AttnArgs &a, const StepPlan &pl, hipStream_t st)
 {
     float *part = static_cast<float *>(ws);
-    float2 *stat = reinterpret_cast<float2 *>(part + static_cast<int64_t>(pl.splits) * pl.rows * a.D);
+    float2 *stat =
+        reinterpret_cast<float2 *>(part + static_cast<int64_t>(pl.splits) * pl.rows * a.D);
     const uint32_t blocks = static_cast<uint32_t>(a.S) * pl.row_tiles * pl.splits * a.Hkv;
-    HEX_LAUNCH((attn_step_k<std::conditional_t<sizeof(E) == 2, Bf16, Full>, DC>), dim3(blocks), dim3(64 * kStepWaves), 0, st,
+    using M = std::conditional_t<sizeof(E) == 2, Bf16, Full>;
+    HEX_LAUNCH((attn_step_k<M, DC>), dim3(blocks), dim3(64 * kStepWaves), 0, st,
                static_cast<const E *>(q), static_cast<const E *>(k), static_cast<const E *>(v),
                static_cast<E *>(o), part, stat, a, pl);
     const hipError_t e = hipGetLastError();
@@ -328,7 +330,8 @@ StepPlan step_plan(int S, int n, int Hq, int Hkv, int max_len)
     p.chunk = static_cast<int>((most + splits - 1) / splits) * step;
     if (p.chunk < step)
         p.chunk = step;
-    p.splits = most < 1 ? 1 : static_cast<int>((static_cast<int64_t>(max_len) + p.chunk - 1) / p.chunk);
+    const int64_t len = max_len;
+    p.splits = most < 1 ? 1 : static_cast<int>((len + p.chunk - 1) / p.chunk);
     return p;
 }
 

@@ -277,7 +277,7 @@ struct AttnGrads {
 hipError_t attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse,
                     const AttnArgs &a, Dtype dt, hipStream_t st);
 
-// A piece of the gradient's second kernel: 128 keys from key0 on of the
+// A piece of the gradient's second kernel: a tile of keys from key0 on of the
 // sequence with queries q0 .. q0 + n and keys k0 .. k0 + m, and the row tiles
 // row0 .. row1 of them.  parts > 1: one of so many of its tile, whose sums go
 // to partial sum `slot`.
@@ -292,7 +292,7 @@ struct KeyPlan {
     int *before, *next, *ends;
     KeyPiece *divided, *list;
     float4 *part;
-    int shares, blocks, room, row_tile, row_shift; // row_tile = 2^row_shift
+    int shares, blocks, room, row_tile, row_shift, key_tile; // row_tile = 2^row_shift
 };
 // k_len is not used (a key belongs to one sequence)
 size_t attn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt);

@@ -138,6 +138,20 @@ def test_attention_long(dt, D):
     run_attention([1] * 70 + [640], None, 2, 1, D, dt, False, 4)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [40, 64, 80, 128])
+@pytest.mark.parametrize("lq,lk", [
+    ([641], None), ([511, 513], None), ([1100, 0, 3], None), ([2500], None),
+    ([9, 400], [1025, 300]), ([1200, 33], [385, 257]), ([1030], None), ([2100, 40], [2080, 33]),
+])
+def test_attention_of_long_sequences(lq, lk, D, dt, causal):
+    """Means of hundreds of keys a sequence: the gradient's large key tiles,
+    whole and divided, and what they leave at a sequence's end."""
+    torch_mod()
+    run_attention(lq, lk, 4, 1, D, dt, causal, 17 + D)
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("scale", [0.0, 0.01, 3.0])
 def test_attention_scales(dt, scale):

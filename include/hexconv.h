@@ -320,6 +320,16 @@ int hexpool3d_bwd(const void *dy, const uint16_t *argmax, const void *relu_y, vo
  *  - Products take bf16 operands as they are and add in float32.
  *    Probabilities and their gradients are rounded to bf16 for their second
  *    product (bf16 calls); sums, maxima and logarithms are float32.
+ *  - Float32 products of hexattn_fwd and hexattn_bwd take each operand as the
+ *    sum of three bf16 numbers, all of its 24 bits, and drop what is below
+ *    2^-24 of a product.  Operands under 2^-110 lose bits; infinities, and
+ *    values from 3.39e38 on, give NaN.
+ *  - A key that a row does not see has the probability 0 for it, and 0 times
+ *    a NaN or an infinity is NaN: within a sequence, values (in the gradient
+ *    queries, keys and dout too) that are not finite can reach rows and keys
+ *    that do not see them.  They reach no other sequence.
+ *  - hexattn_*: a row of tokens spans less than 2^24 bytes (ld times the
+ *    element size; HEX_ERR_UNSUPPORTED otherwise).
  *  - Outputs must not overlap inputs.
  */
 #define HEX_ATTN_MAX_DIM 128
@@ -393,7 +403,9 @@ size_t hexattn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, hex_
  * dv, strides lddq, lddk and lddv, from dout and the forward's o and lse.  A
  * key head's gradients are the sums over the query heads that share it.
  * Rows that see no key, and keys that no row sees, get zeros.  ws: at least
- * hexattn_bwd_workspace(...) bytes.  Deterministic.
+ * hexattn_bwd_workspace(...) bytes, for partial sums that do not depend on the
+ * lengths: up to 0.4 GB for large problems, less for small ones.
+ * Deterministic.
  */
 int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
                 const void *dout, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes,
@@ -412,7 +424,8 @@ size_t hexattn_step_workspace(int S, int n, int Hq, int Hkv, int D, int max_len,
  * k_start[s] on of the Tk tokens of k and v (int32 [S] each), the last n of
  * them the new tokens themselves, and new token t sees the keys up to its
  * own.  A row that sees no key gives zeros.  max_len: a bound on the lengths
- * (longer ones are cut to it), by which the work is split over the keys.
+ * (longer ones are cut to it), by which the work is split over the keys; Tk
+ * and max_len are at most 2^30.
  * ws: at least hexattn_step_workspace(...) bytes, NULL where that is 0.
  * Deterministic.
  */

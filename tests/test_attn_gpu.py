@@ -213,6 +213,32 @@ def test_attention_gradients_against_differences(dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [40, 128])
+def test_attention_scales_by_powers_of_two(D, dt):
+    """Inputs times powers of two give outputs times powers of two, to the
+    bit: no part of a product is lost to its magnitude."""
+    torch_mod()
+    g = torch.Generator().manual_seed(23)
+    T, Hq, Hkv, up = 200, 4, 2, 2.0 ** 40
+    q, k, v, do = (normal(g, T, h, D, dt=dt)[1] for h in (Hq, Hkv, Hkv, Hq))
+    s = ints([0, 150, T])
+    ws = torch.empty(hx.hexattn_bwd_workspace(T, T, 2, Hq, Hkv, D, hx._dtype_code(q)),
+                     dtype=torch.uint8, device="cuda")
+
+    def run(q, k, v, do):
+        o, lse = nan(T, Hq, D, dt=dt), nan(T, Hq)
+        grads = [nan(*t.shape, dt=dt) for t in (q, k, v)]
+        hx.hexattn_fwd(q, k, v, o, lse, s, causal=True)
+        hx.hexattn_bwd(q, k, v, o, lse, do, *grads, ws, s, causal=True)
+        return [o, lse, *grads]
+
+    want = run(q, k, v, do)
+    got = run(q / up, k * up, v * up, do / up)
+    for a, b, f, n in zip(got, want, (up, 1, up, 1 / up, 1 / up), ("o", "lse", "dq", "dk", "dv")):
+        assert torch.equal(a, b * f), n
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attention_repeats_itself(dt):
     """The same bits from every run: no sum depends on the order of blocks."""
     torch_mod()

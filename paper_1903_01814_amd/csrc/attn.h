@@ -27,8 +27,6 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLo = 1.4426950408889634 - kLog2e;
 constexpr float kLn2 = 0.6931471805599453f, kLn2Lo = 0.6931471805599453 - kLn2;
 
-constexpr int kShortRows = 256;
-
 // ---- how a type is multiplied.  E: what tensors hold; Frag: an operand;
 // Score: a sum over the head dimension while it is added up; FINE: exponents
 // in two parts (prob).  In LDS an element takes BYTES bytes in each of PLANES
@@ -398,7 +396,13 @@ inline int attn_slots(int T, int G, int TR, int S)
 {
     return static_cast<int>(static_cast<int64_t>(T) * G / TR) + S;
 }
-// Sequences too short to fill tiles of 128 rows: tiles of 64
+// Sequences of so few rows on average take tiles of 64 rows and 32 keys, which
+// they fill better, instead of 128 and 64 (forward, dq; 8 heads of 32, 512
+// sequences of 130 rows: 69.8 -> 63.4, 84.0 -> 76.5 us; 4 of 64, 384 of 195:
+// 54.2 -> 51.3, 71.9 -> 68.5; 256 of 345: 74.7 -> 75.3, 96.8 -> 94.3).  Not in
+// float32, where every wave more splits the same keys again (4 heads of 64, 384
+// of 95 rows: 52 -> 67, 81 -> 91).
+constexpr int kShortRows = 256;
 inline bool attn_short(const AttnArgs &a)
 {
     return static_cast<int64_t>(a.Tq) * a.group.G < static_cast<int64_t>(kShortRows) * a.S;
@@ -544,8 +548,9 @@ template <typename M, int DC, int ROWS, int NT> struct Stage {
 // them.  Usually key heads are innermost, so that a head's keys stay on few
 // dies.  Heads of less than a 128-byte cache line share lines with their
 // neighbours: there all heads of a slot go to one die (512 sequences of 20 to
-// 400 tokens, 8 heads of 32 bf16 elements: see attn_fwd_k).  Slots from the
-// last on: under the causal mask a sequence's last tiles are the longest.
+// 400 tokens, 8 heads of 32 in bfloat16: dq 81.4 -> 76.5 us, forward the same).
+// Slots from the last on: under the causal mask a sequence's last tiles are the
+// longest.
 __device__ __forceinline__ void head_and_slot(const AttnArgs &a, uint32_t id, int &kvh, int &slot)
 {
     if (a.narrow) {

@@ -688,9 +688,12 @@ hipError_t launch(const E *q, const E *k, const E *v, const E *o, const float *l
                   E *dq, E *dk, E *dv, float *delta, const AttnArgs &a, const AttnGrads &gr,
                   const KeyPlan &pl, hipStream_t st)
 {
-    const hipError_t e = attn_short(a)
-                             ? launch_dq<E, DC, 2>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st)
-                             : launch_dq<E, DC, 4>(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st);
+    const auto dq_of = [&](auto f) { return f(q, k, v, o, lse, dout, dq, delta, a, gr, pl, st); };
+    hipError_t e;
+    if constexpr (sizeof(E) == 2)
+        e = attn_short(a) ? dq_of(launch_dq<E, DC, 2>) : dq_of(launch_dq<E, DC, 4>);
+    else
+        e = dq_of(launch_dq<E, DC, 4>);
     if (e != hipSuccess || a.Tk == 0)
         return e;
     if constexpr (dkv_wide(sizeof(E) == 4, DC))

@@ -202,7 +202,10 @@ hipError_t launch(const void *q, const void *k, const void *v, void *o, float *l
         return f(static_cast<const E *>(q), static_cast<const E *>(k), static_cast<const E *>(v),
                  static_cast<E *>(o), lse, a, st);
     };
-    return attn_short(a) ? run(launch_waves<E, DC, 2>) : run(launch_waves<E, DC, 4>);
+    if constexpr (sizeof(E) == 2)
+        if (attn_short(a))
+            return run(launch_waves<E, DC, 2>);
+    return run(launch_waves<E, DC, 4>);
 }
 
 template <typename E>

@@ -177,18 +177,25 @@ def hex_tap_table(k: int, parity: int):
 
 # --------------------------------------------------------- device entries
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    # looked up once: the statement takes 0.1 us each time
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t):
-    torch = _torch()
-    if t.dtype == torch.float32:
+    torch, dtype = _torch(), t.dtype
+    if dtype is torch.float32:
         return HEX_F32
-    if t.dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return HEX_BF16
-    raise TypeError("hexconv: unsupported dtype %s" % t.dtype)
+    raise TypeError("hexconv: unsupported dtype %s" % dtype)
 
 
 def _dev(t, name, dt=None, shape=None):
@@ -573,7 +580,7 @@ def hexattn_fwd(q, k, v, o, lse, q_start, k_start=None, k_len=None, scale=None,
     k_start: the same for the keys (None: q_start), or int32 [S] with k_len.
     scale: 1 / sqrt(D) by default."""
     Tq, Hq, D = q.shape
-    Tk, Hkv = k.shape[:2]
+    Tk, Hkv, _ = k.shape
     dt = _dtype_code(q)
     S = q_start.shape[0] - 1
     if k_start is None:
@@ -589,8 +596,8 @@ def hexattn_fwd(q, k, v, o, lse, q_start, k_start=None, k_len=None, scale=None,
         pq, pk, pv, po, _array(lse, "lse", _torch().float32, (Tq, Hq)),
         _array(q_start, "q_start", i32, (S + 1,)),
         _array(k_start, "k_start", i32, (S + 1,) if k_len is None else (S,)),
-        _array(k_len, "k_len", i32, (S,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, _scale(scale, D),
-        HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
+        _array(k_len, "k_len", i32, (S,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo,
+        _scale(scale, D), HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
     _ok("hexattn_fwd", rc)
     return o, lse
 
@@ -603,7 +610,7 @@ def hexattn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, q_start, k_start=None, sc
                 causal: bool = False, stream=None):
     """dq, dk, dv <- gradients of hexattn_fwd from dout, o and lse."""
     Tq, Hq, D = q.shape
-    Tk, Hkv = k.shape[:2]
+    Tk, Hkv, _ = k.shape
     dt = _dtype_code(q)
     S = q_start.shape[0] - 1
     if k_start is None:
@@ -620,8 +627,9 @@ def hexattn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, q_start, k_start=None, sc
     rc = load().hexattn_bwd(
         pq, pk, pv, po, _array(lse, "lse", _torch().float32, (Tq, Hq)), pg, pdq, pdk, pdv,
         *_ws(ws), _array(q_start, "q_start", i32, (S + 1,)),
-        _array(k_start, "k_start", i32, (S + 1,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv, _scale(scale, D),
-        HEX_ATTN_CAUSAL if causal else 0, dt, _stream(stream))
+        _array(k_start, "k_start", i32, (S + 1,)), S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo, ldg,
+        lddq, lddk, lddv, _scale(scale, D), HEX_ATTN_CAUSAL if causal else 0, dt,
+        _stream(stream))
     _ok("hexattn_bwd", rc)
     return dq, dk, dv
 
@@ -635,7 +643,7 @@ def hexattn_step(q, k, v, o, ws, k_start, k_len, max_len: int, scale=None, strea
     over the k_len[s] cached tokens from k_start[s] on of k and v
     [Tk][Hkv][D], at most max_len each."""
     S, n, Hq, D = q.shape
-    Tk, Hkv = k.shape[:2]
+    Tk, Hkv, _ = k.shape
     dt = _dtype_code(q)
     i32, ty = _torch().int32, q.dtype
     pk, ldk = _tokens(k, "k", ty, Hkv, D)

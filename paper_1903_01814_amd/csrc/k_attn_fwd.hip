@@ -98,6 +98,9 @@ attn_fwd_k(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a)
 
     // the tile of keys at kt and vt, key0 the first
     auto tile = [&](unsigned char *kt, unsigned char *vt, int key0) {
+        // scores before the other wave's vector work: 1151 -> 1131 us (16432 keys,
+        // 16 heads of 128 on 4); the exponentials first instead 1185
+        __builtin_amdgcn_s_setprio(1);
         floatx16 x[KT];
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
@@ -107,6 +110,7 @@ attn_fwd_k(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a)
                 add_product(TL::read_cols(kt + 32 * t * TL::PITCH, ca, s), qf[s], sc);
             x[t] = value(sc);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (key0 + BK > least) {
             const int left = see - key0 - 4 * h;
 #pragma unroll

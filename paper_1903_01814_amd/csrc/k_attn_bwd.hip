@@ -227,6 +227,10 @@ __device__ void make_plan(const AttnArgs &a, const KeyPlan &pl, unsigned char *l
 
 // ---- dq: rows as in the forward, 32 a wave of NW, BK keys a tile.
 //   X^T = K Q^T and dP^T = V dO^T (keys as rows), dQ^T += K^T dS^T
+// D from a bfloat16 o is off by o's rounding, as much as the sums' own rounding
+// where a row sees a few keys and o is as large as v (dq of 8 keys: 3.1e-3
+// instead of 2.4e-3).  D is also sum_j p_ij dp_ij, and a row of up to 32 keys
+// takes that, from its one tile.
 template <typename M, int DC, int BK, int NW, typename E = typename M::E>
 __global__ __launch_bounds__(64 * NW, attn_waves(sizeof(E) == 4, DC)) void
 attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, const E *dout, E *dq,
@@ -270,6 +274,7 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
     // a row that saw no key: every p is 0
     const Ref ref = l == -HUGE_VALF ? Ref{HUGE_VALF, 0.f} : ref_of_lse(l);
     Frag qf[DS], gf[DS];
+    constexpr bool EXACT = sizeof(E) == 2;
     float dl = 0.f;
 #pragma unroll
     for (int s = 0; s < DS; ++s) {
@@ -278,8 +283,6 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
         dl = dot8(gp, op, 16 * s + 8 * h, a.D, dl);
     }
     dl = both_sum(dl);
-    if (row < rows && h == 0)
-        delta[token * a.Hq + head] = dl;
     const int r_last = min(rows, row0 + TR) - 1;
     const int end = a.causal ? min(m, max(0, row_token(g, r_last) + ahead + 1)) : m;
     const int ntiles = (end + BK - 1) / BK;
@@ -338,7 +341,7 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
                 floatx16 x = value(sc);
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    x[r] = prob<M>(x[r], a, ref.hi, ref.lo) * (dp[r] - dl);
+                    x[r] = prob<M>(x[r], a, ref.hi, ref.lo);
                 if (key0 + 32 > least) {
                     const int left = see - key0 - 4 * h;
 #pragma unroll
@@ -346,6 +349,17 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
                         if (8 * (r >> 2) + (r & 3) >= left)
                             x[r] = 0.f;
                 }
+                if (EXACT && t == 0 && j == 0) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        sum = fmaf(x[r], dp[r], sum);
+                    sum = both_sum(sum);
+                    dl = see <= 32 ? sum : dl;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    x[r] *= dp[r] - dl;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     const Frag sf = to_frag<M>(x, s);
@@ -362,6 +376,8 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
 
     if (row >= rows)
         return;
+    if (h == 0)
+        delta[token * a.Hq + head] = dl;
     E *p = dq + token * gr.lddq + head * a.D;
 #pragma unroll
     for (int d = 0; d < DT; ++d)

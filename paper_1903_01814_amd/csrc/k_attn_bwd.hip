@@ -11,6 +11,13 @@
 // and do . v are computed twice, 7 products in place of 5; in exchange no sum
 // is added up by atomics, each has one order and the result is the same from
 // run to run.
+//
+// Bound by the matrix cores and the vector unit in turn, as the forward, and
+// attn_dkv_k by the wait for the next rows as well.  24 sequences of 500 to 5000
+// tokens, 16 heads of 128 on 4, causal, in bfloat16: dq 850 us (6 of 14 parts of
+// the work, 950 TFLOP/s; matrix cores busy 0.43), dk and dv 1340 (810 TFLOP/s;
+// 0.35) and 46 to join; 16 of 1027, 8 heads of 64 on 4, in float32: 327, 425 and
+// 27 (160, 165 TFLOP/s; 0.45, 0.48); 512 of 20 to 400, 8 heads of 32: 76, 107.
 #include "attn.h"
 #include "kernels.h"
 
@@ -35,9 +42,11 @@ namespace {
 // that kernel: its fences write back and drop a die's whole cache, 1904 -> 2282
 // us where many tiles are divided.)
 constexpr int kFixed = 4;
-constexpr int kShares = 3;  // shares of all heads for each block that the card holds
+// shares of all heads for each block that the card holds (the case above: 1422 us
+// and 22 to join with 2, 1375 and 45 with 3, 1341 and 96 with 5)
+constexpr int kShares = 3;
 constexpr int kClasses = 8; // of pieces by size
-constexpr int kLeast = 24; // units of a share at least: small tiles stay whole
+constexpr int kLeast = 24;  // units of a share at least: small tiles stay whole
 
 // one sequence's units: k i - a0 is the first row tile that sees key tile i
 struct KeyUnits {
@@ -384,8 +393,10 @@ attn_dq_k(const E *q, const E *k, const E *v, const E *o, const float *lse, cons
         store_col(p, acc[d], 32 * d + 4 * h, a.D, a.scale);
 }
 
-// Rows a step of attn_dkv_k takes, and the waves of it that a SIMD holds at
-// once (registers and LDS).
+// Rows a step of attn_dkv_k takes, as many as the registers hold (64 instead of
+// 32: heads of 64 827 -> 687 us, of 80 1359 -> 1200, of 32 117 -> 107, in
+// float32 657 -> 613; heads of 128 spill, 1397 -> 1418), and the waves of it that
+// a SIMD holds at once.
 constexpr int dkv_rows(bool f32, int DC) { return DC <= (f32 ? 32 : 96) ? 64 : 32; }
 constexpr int dkv_waves(bool f32, int DC)
 {

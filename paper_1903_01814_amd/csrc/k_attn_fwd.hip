@@ -7,14 +7,24 @@
 // block owns 128 rows (64 where sequences are short) of one key head of one
 // sequence (a row is a query token and one of the G query heads that share the
 // key head, so short sequences fill a tile G times better and the keys are
-// read once for the group), a wave 32 of them.  Per tile of BK keys, staged in LDS for the
-// whole block (two buffers, the next tile's loads in flight during the
-// products):
+// read once for the group), a wave 32 of them.  Per tile of BK keys, staged in
+// LDS for the whole block (two buffers, the next tile's loads in flight during
+// the products):
 //   X^T = K Q^T   keys as rows: a lane holds one query's scores
 //   p = 2^(x c - m)  with c = scale log2(e), m and l in the lane
 //   O^T += V^T P^T   P^T straight from the registers, V^T by the transposing read
 // The maximum is raised only when a row passes it by more than 2^kSlack: the
 // sums stay exact in float32, and most tiles save the rescaling of O.
+//
+// Bound by the matrix cores and the vector unit in turn: one wave's exponentials
+// (a quarter of the rate) run beside the other's products, so the two waves a
+// SIMD that the launch bounds ask for are worth more than registers (one wave
+// with twice as many took 1826 us where two took 1182).  Heads of 128 in
+// bfloat16, 16 on 4: one sequence of 16432 1130 us, 970 TFLOP/s (a large library
+// product 1220), matrix cores busy 0.46 of the cycles, vector unit 0.45; 24 of
+// 500 to 5000, causal 690 us, 790 TFLOP/s.  Heads of 32, 512 sequences of 20 to
+// 400: 62 us, the vector unit.  Heads of 64 in float32, 16 of 1027: 231 us, 150
+// TFLOP/s.
 #include "attn.h"
 #include "kernels.h"
 
@@ -24,7 +34,9 @@ namespace {
 
 constexpr float kSlack = 8.f; // in powers of two
 
-// NW waves, BK keys a tile.
+// NW waves, BK keys a tile: 64, or 32 where registers (float32 past 32, 64 rows)
+// leave no room for more (heads of 64 in bfloat16, 24 sequences of 500 to 5000:
+// 362 us with 64 keys, 391 with 32).
 template <typename M, int DC, int BK, int NW, typename E = typename M::E>
 __global__ __launch_bounds__(64 * NW, attn_waves(sizeof(E) == 4, DC)) void
 attn_fwd_k(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a)

@@ -313,11 +313,12 @@ __global__ __launch_bounds__(1024) void rotary_reduce_k(const float *part, int n
 
 // kTokens tokens, fewer where that makes less than four blocks a compute unit
 // (1000 tokens, 16 + 4 heads of 128 in bfloat16: forward 12.4 -> 6.2, backward
-// 14.8 -> 8.0 us; 300 of 64 in float32: 6.3 -> 4.2, 8.5 -> 4.5)
+// 14.8 -> 8.0 us; 300 of 64 in float32: 6.3 -> 4.2, 8.5 -> 4.5); up to kTokens
+// in all take one block (4 tokens: 4.5 us either way)
 int tokens_per_block(int64_t T)
 {
     int per = kTokens;
-    while (per > 1 && T / per < 4 * device_cus())
+    while (T > kTokens && per > 1 && T / per < 4 * device_cus())
         per /= 2;
     return per;
 }

@@ -424,9 +424,11 @@ void *scratch_ptr()
 
 // ---- attention over packed sequences
 
-constexpr int64_t kMaxRows = (INT64_C(1) << 31) - 4096; // row numbers, and the tile past them, are 32 bits
-constexpr int kMaxKeys = 1 << 30;                       // of a cache
-constexpr int64_t kMaxBlocks = (INT64_C(1) << 24) - 1;  // 256 threads each, 2^32 of them in all
+// row numbers, and the tile past them, are 32 bits
+constexpr int64_t kMaxRows = (INT64_C(1) << 31) - 4096;
+constexpr int kMaxKeys = 1 << 30; // of a cache
+// 256 threads each, 2^32 of them in all
+constexpr int64_t kMaxBlocks = (INT64_C(1) << 24) - 1;
 
 int64_t vec(int dt) { return dt == HEX_F32 ? 4 : 8; } // elements of 16 bytes
 
@@ -471,9 +473,24 @@ int check_attn(int S, int Tq, int Tk, int Hq, int Hkv, int D, int dt)
     return HEX_OK;
 }
 
-hexk::AttnArgs attn_args(const int32_t *q_start, const int32_t *k_start, const int32_t *k_len, int S,
-                   int Tq, int Tk, int Hq, int Hkv, int D, int64_t ldq, int64_t ldk, int64_t ldv,
-                   int64_t ldo, float scale, bool causal, int dt)
+int check_step(int S, int n, int Hq, int Hkv, int D, int max_len, int dt)
+{
+    if (S < 1 || n < 1 || max_len < 0)
+        return HEX_ERR_INVALID_ARG;
+    const int rc = check_heads(Hq, Hkv, D, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (static_cast<int64_t>(S) * n > kMaxRows / Hq || max_len > kMaxKeys)
+        return HEX_ERR_UNSUPPORTED;
+    const hexk::StepPlan p = hexk::step_plan(S, n, Hq, Hkv, max_len);
+    if (static_cast<int64_t>(S) * Hkv * p.row_tiles > kMaxBlocks / p.splits || p.rows > kMaxBlocks)
+        return HEX_ERR_UNSUPPORTED;
+    return HEX_OK;
+}
+
+hexk::AttnArgs attn_args(const int32_t *q_start, const int32_t *k_start, const int32_t *k_len,
+                         int S, int Tq, int Tk, int Hq, int Hkv, int D, int64_t ldq, int64_t ldk,
+                         int64_t ldv, int64_t ldo, float scale, bool causal, int dt)
 {
     hexk::AttnArgs a;
     a.q_start = q_start;
@@ -1052,8 +1069,9 @@ int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse
     int rc = check_attn(S, Tq, Tk, Hq, Hkv, D, dt);
     if (rc != HEX_OK)
         return rc;
-    if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 || !stride_ok(ldq, Hq, D, dt) ||
-        !stride_ok(ldo, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt))
+    if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 ||
+        !stride_ok(ldq, Hq, D, dt) || !stride_ok(ldo, Hq, D, dt) ||
+        !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt))
         return HEX_ERR_INVALID_ARG;
     if (!stride_small({ldk, ldv}, dt))
         return HEX_ERR_UNSUPPORTED;
@@ -1063,8 +1081,8 @@ int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse
         return rc;
     if (q_start == nullptr || k_start == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
         return HEX_ERR_INVALID_ARG;
-    const hexk::AttnArgs a = attn_args(q_start, k_start, k_len, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv, ldo,
-                                 scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
+    const hexk::AttnArgs a = attn_args(q_start, k_start, k_len, S, Tq, Tk, Hq, Hkv, D, ldq, ldk,
+                                       ldv, ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
     return launched(hexk::attn_fwd(q, k, v, o, lse, a, static_cast<Dtype>(dt),
                                    static_cast<hipStream_t>(stream)));
 }
@@ -1086,8 +1104,9 @@ int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, cons
     int rc = check_attn(S, Tq, Tk, Hq, Hkv, D, dt);
     if (rc != HEX_OK)
         return rc;
-    if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 || !stride_ok(ldq, Hq, D, dt) ||
-        !stride_ok(ldo, Hq, D, dt) || !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt) ||
+    if (!(scale >= 0.f) || !isfinite(scale) || (flags & ~HEX_ATTN_CAUSAL) != 0 ||
+        !stride_ok(ldq, Hq, D, dt) || !stride_ok(ldo, Hq, D, dt) ||
+        !stride_ok(ldk, Hkv, D, dt) || !stride_ok(ldv, Hkv, D, dt) ||
         !stride_ok(lddout, Hq, D, dt) || !stride_ok(lddq, Hq, D, dt) ||
         !stride_ok(lddk, Hkv, D, dt) || !stride_ok(lddv, Hkv, D, dt))
         return HEX_ERR_INVALID_ARG;
@@ -1106,15 +1125,16 @@ int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, cons
         return HEX_ERR_INVALID_ARG;
     if (Tk > 0 && (k == nullptr || v == nullptr || dk == nullptr || dv == nullptr))
         return HEX_ERR_INVALID_ARG;
-    const hexk::AttnArgs a = attn_args(q_start, k_start, nullptr, S, Tq, Tk, Hq, Hkv, D, ldq, ldk, ldv,
-                                 ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
-    return launched(hexk::attn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, a, hexk::AttnGrads{lddout, lddq, lddk, lddv},
+    const hexk::AttnArgs a = attn_args(q_start, k_start, nullptr, S, Tq, Tk, Hq, Hkv, D, ldq, ldk,
+                                       ldv, ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
+    return launched(hexk::attn_bwd(q, k, v, o, lse, dout, dq, dk, dv, ws, a,
+                                   hexk::AttnGrads{lddout, lddq, lddk, lddv},
                                    static_cast<Dtype>(dt), static_cast<hipStream_t>(stream)));
 }
 
 size_t hexattn_step_workspace(int S, int n, int Hq, int Hkv, int D, int max_len, hex_dtype dt)
 {
-    if (S < 1 || n < 1 || max_len < 0 || check_heads(Hq, Hkv, D, dt) != HEX_OK)
+    if (check_step(S, n, Hq, Hkv, D, max_len, dt) != HEX_OK)
         return 0;
     return hexk::step_workspace(hexk::step_plan(S, n, Hq, Hkv, max_len), D);
 }
@@ -1139,17 +1159,16 @@ int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws,
         return rc;
     if (k_start == nullptr || k_len == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
         return HEX_ERR_INVALID_ARG;
-    if (static_cast<int64_t>(S) * n > kMaxRows / Hq || Tk > kMaxKeys || max_len > kMaxKeys)
+    if (Tk > kMaxKeys)
         return HEX_ERR_UNSUPPORTED;
+    if ((rc = check_step(S, n, Hq, Hkv, D, max_len, dt)) != HEX_OK)
+        return rc;
     const hexk::StepPlan p = hexk::step_plan(S, n, Hq, Hkv, max_len);
-    if (static_cast<int64_t>(S) * Hkv * p.row_tiles > kMaxBlocks / p.splits ||
-        p.rows > kMaxBlocks)
-        return HEX_ERR_UNSUPPORTED;
     const size_t need = hexk::step_workspace(p, D);
     if (ws_bytes < need || (need > 0 && ws == nullptr))
         return HEX_ERR_INVALID_ARG;
-    hexk::AttnArgs a = attn_args(nullptr, k_start, k_len, S, 0, Tk, Hq, Hkv, D, 0, ldk, ldv, 0, scale,
-                           true, dt);
+    hexk::AttnArgs a = attn_args(nullptr, k_start, k_len, S, 0, Tk, Hq, Hkv, D, 0, ldk, ldv, 0,
+                                 scale, true, dt);
     a.max_len = max_len;
     return launched(hexk::attn_step(q, k, v, o, ws, a, p, static_cast<Dtype>(dt),
                                     static_cast<hipStream_t>(stream)));

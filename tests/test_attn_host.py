@@ -134,6 +134,17 @@ def test_workspace_of_bad_arguments():
     assert hx.hexrotary_bwd_workspace(0, 4, 2, 32, 0) == 0
 
 
+@pytest.mark.parametrize("n", [1 << 20, 1 << 30, (1 << 31) - 1])
+@pytest.mark.parametrize("S,max_len", [(1, 100), (1 << 20, 100), (3, (1 << 31) - 1)])
+def test_workspaces_of_the_largest_arguments(S, max_len, n):
+    """Products past 32 bits neither wrap to a size nor end the process."""
+    hx.hexattn_step_workspace(S, n, 4, 1, 64, max_len, 1)
+    assert hx.hexattn_step_workspace(S, 1 << 30, 4, 1, 64, max_len, 1) == 0
+    hx.hexattn_bwd_workspace(n, n, S, 4, 1, 64, 1)
+    assert hx.hexattn_bwd_workspace(n, 1 << 30, S, 65535, 1, 128, 1) == 0
+    assert hx.hexrotary_bwd_workspace(n, 65535, 65535, 128, 1) <= 1024 * 2 * 128 * 4
+
+
 def test_binding_refuses():
     """Host tensors, wrong types and heads that are not dense."""
     q = torch.zeros(4, 2, 32)

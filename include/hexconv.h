@@ -313,6 +313,8 @@ int hexpool3d_bwd(const void *dy, const uint16_t *argmax, const void *relu_y, vo
  *    heads share Hkv key heads, Hq / Hkv in a row each.
  *  - Offsets into tensors are 64 bits wide: a cache may be larger than 2^31
  *    elements.
+ *  - Offsets, lengths, slots, positions, frequencies and axes need 4-byte
+ *    alignment only.
  *  - Offsets and lengths on the device are not checked on the host; the
  *    kernels bring them into the tensors' bounds, so wrong ones give wrong
  *    results and no access outside.

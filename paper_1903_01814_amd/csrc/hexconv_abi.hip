@@ -473,6 +473,15 @@ int check_attn(int S, int Tq, int Tk, int Hq, int Hkv, int D, int dt)
     return HEX_OK;
 }
 
+// arrays read a 4-byte element at a time
+int words_ok(std::initializer_list<const void *> required, const void *optional)
+{
+    for (const void *p : required)
+        if (p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0)
+            return HEX_ERR_INVALID_ARG;
+    return (reinterpret_cast<uintptr_t>(optional) & 3u) != 0 ? HEX_ERR_INVALID_ARG : HEX_OK;
+}
+
 int check_step(int S, int n, int Hq, int Hkv, int D, int max_len, int dt)
 {
     if (S < 1 || n < 1 || max_len < 0)
@@ -1007,7 +1016,8 @@ int hexrotary_fwd(const void *q, const void *k, const void *v, const float *pos,
         return HEX_ERR_INVALID_ARG;
     if (T == 0)
         return HEX_OK;
-    if ((rc = ptrs_ok({q, k, pos, freq, axis, qo, ko}, {wq, wk, v, vo, slot})) != HEX_OK)
+    if ((rc = ptrs_ok({q, k, qo, ko}, {wq, wk, v, vo})) != HEX_OK ||
+        (rc = words_ok({pos, freq, axis}, slot)) != HEX_OK)
         return rc;
     const hexk::RotaryArgs a{pos, freq, axis, T,  ldq, ldk, ldv,     ldqo, ldko,
                              ldvo, 0,   0,    Hq, Hkv, D,   A,       n_slots, eps,
@@ -1049,7 +1059,8 @@ int hexrotary_bwd(const void *q, const void *k, const float *pos, const float *f
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (T == 0) // no token: the weights' gradients are zero
         return launched(hexk::rotary_zero(dwq, dwk, D, st));
-    if ((rc = ptrs_ok({pos, freq, axis, dqo, dko, dq, dk}, {})) != HEX_OK)
+    if ((rc = ptrs_ok({dqo, dko, dq, dk}, {})) != HEX_OK ||
+        (rc = words_ok({pos, freq, axis}, nullptr)) != HEX_OK)
         return rc;
     if (norm && (q == nullptr || k == nullptr || ws == nullptr ||
                  ws_bytes < hexrotary_bwd_workspace(T, Hq, Hkv, D, dt)))

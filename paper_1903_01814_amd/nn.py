@@ -451,9 +451,7 @@ class HexAttentionFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, q_start, k_start, scale, causal):
-        # rows of no sequence have no result: zeros, and no gradient
-        o = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device)
+        o, lse = _attention_outputs(q)
         hx.hexattn_fwd(q, k, v, o, lse, q_start, k_start, scale=scale, causal=causal)
         ctx.save_for_backward(q, k, v, o, lse, q_start, k_start)
         ctx.scale, ctx.causal = scale, causal
@@ -468,6 +466,12 @@ class HexAttentionFunction(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None
 
 
+def _attention_outputs(q):
+    """o and lse as rows of no sequence have them: zeros, and no gradient."""
+    return (torch.zeros(q.shape, dtype=q.dtype, device=q.device),
+            torch.full(q.shape[:2], -math.inf, dtype=torch.float32, device=q.device))
+
+
 def _attention_bwd(q, k, v, o, lse, g, dq, dk, dv, q_start, k_start, scale, causal):
     Tq, Hq, D = q.shape
     Tk, Hkv = k.shape[:2]
@@ -480,8 +484,7 @@ def _attention_bwd(q, k, v, o, lse, g, dq, dk, dv, q_start, k_start, scale, caus
 class HexPixelAttentionFunction(torch.autograd.Function):
     """Norm, rotation and attention of one projection's queries, keys and
     values, qkv [T][Hq + 2 Hkv][D]: the gradients are written into one tensor
-    of that layout, with no copies between the parts.  Every token belongs to
-    a sequence."""
+    of that layout, with no copies between the parts."""
 
     @staticmethod
     def forward(ctx, qkv, wq, wk, pos, freq, axis, start, heads, eps, causal):
@@ -489,7 +492,7 @@ class HexPixelAttentionFunction(torch.autograd.Function):
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
         qo, ko = _empty(q.shape, q), _empty(k.shape, k)
         hx.hexrotary_fwd(q, k, pos, freq, axis, wq, wk, qo, ko, eps=eps)
-        o, lse = _empty(q.shape, q), _empty(q.shape[:2], q, torch.float32)
+        o, lse = _attention_outputs(q)
         hx.hexattn_fwd(qo, ko, v, o, lse, start, causal=causal)
         ctx.save_for_backward(qkv, wq, wk, pos, freq, axis, start, qo, ko, o, lse)
         ctx.heads, ctx.eps, ctx.causal = heads, eps, causal
@@ -500,9 +503,9 @@ class HexPixelAttentionFunction(torch.autograd.Function):
         qkv, wq, wk, pos, freq, axis, start, qo, ko, o, lse = ctx.saved_tensors
         Hq, Hkv = ctx.heads
         parts = lambda t: (t[:, :Hq], t[:, Hq:Hq + Hkv], t[:, Hq + Hkv:])  # noqa: E731
-        d = torch.empty_like(qkv)
+        d = torch.zeros_like(qkv)
         (q, k, v), (dq, dk, dv) = parts(qkv), parts(d)
-        gq, gk = _empty(qo.shape, qo), _empty(ko.shape, ko)
+        gq, gk = torch.zeros_like(qo), torch.zeros_like(ko)
         _attention_bwd(qo, ko, v, o, lse, g.contiguous(), gq, gk, dv, start, start, None,
                        ctx.causal)
         dwq, dwk = _rotary_bwd(q, k, pos, freq, axis, wq, wk, gq, gk, dq, dk, ctx.eps, True)
@@ -633,14 +636,17 @@ class HexPixelAttention(nn.Module):
     @torch.no_grad()
     def prefill(self, x, pos, start, cache, longest):
         """Packed prompts x [T][dim] of all streams, at most ``longest`` tokens
-        each, appended to their caches."""
+        each, appended to their caches.  (A longer one is cut at its stream's
+        capacity.)"""
         cache.reserve(int(longest))
-        T = x.shape[0]
-        shift = cache.start + cache.length - start[:-1]
-        slot = (torch.repeat_interleave(shift, start[1:] - start[:-1], output_size=T)
-                + torch.arange(T, dtype=torch.int32, device=x.device)).to(torch.int32)
+        T, n = x.shape[0], start[1:] - start[:-1]
+        each = lambda t: torch.repeat_interleave(t, n, output_size=T)  # noqa: E731
+        at = each(cache.length - start[:-1]) + torch.arange(T, dtype=torch.int32, device=x.device)
+        # no slot past the stream's own
+        slot = torch.where(at < cache.capacity, each(cache.start) + at, -1).to(torch.int32)
         qo = self._into_cache(self._project(x), pos, slot, cache)
-        cache.length += start[1:] - start[:-1]
+        cache.length += n
+        cache.length.clamp_(max=cache.capacity)
         o = _empty(qo.shape, qo)
         hx.hexattn_fwd(qo, cache.k, cache.v, o, None, start, cache.start, cache.length,
                        causal=self.causal)

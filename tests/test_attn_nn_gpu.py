@@ -142,6 +142,56 @@ def test_example_trains():
     assert pixel_events.train() >= 0.9
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_layer_with_unused_tokens(dt):
+    """Tokens after the last sequence pass through the layer as they are, and
+    change no gradient: the same layer on the others alone has the same bits."""
+    torch_mod()
+    torch.manual_seed(3)
+    layer = hnn.HexPixelAttention(64, 4, 2, 16, device="cuda", dtype=dt)
+    start = torch.tensor([0, 30, 64], dtype=torch.int32, device="cuda")
+    x0 = torch.randn(128, 64, device="cuda").to(dt)
+    pos = torch.rand(128, 3, device="cuda") * 9
+    filler = torch.full((1 << 22,), float("nan"), device="cuda")  # what fresh memory may hold
+    del filler
+    got = []
+    for n in (128, 64):
+        x = x0[:n].clone().requires_grad_()
+        layer.zero_grad()
+        y = layer(x, pos[:n].contiguous(), start)
+        (y[:64].float() ** 2).sum().backward()
+        got.append([y[:64], x.grad[:64]] + [p.grad.clone() for p in layer.parameters()])
+        if n > 64:
+            assert torch.equal(y[64:], x0[64:])
+            assert not x.grad[64:].any()
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all()
+        err, size = (a - b).abs().max(), b.abs().max()
+        assert err <= (1e-5 if dt == torch.float32 else 2e-2) * size
+
+
+def test_prefill_cuts_at_capacity():
+    """A prompt longer than its stream's room does not reach the next one's."""
+    torch_mod()
+    torch.manual_seed(4)
+    layer = hnn.HexPixelAttention(32, 2, 1, 16, causal=True, device="cuda").eval()
+    cache = layer.new_cache(3, 8)
+    cache.k.zero_()
+    cache.v.zero_()
+    start = torch.tensor([0, 11, 13, 15], dtype=torch.int32, device="cuda")
+    x, pos = torch.randn(15, 32, device="cuda"), torch.rand(15, 3, device="cuda")
+    layer.prefill(x, pos, start, cache, 8)  # the first has 11
+    assert cache.length.tolist() == [8, 2, 2]
+    alone = layer.new_cache(2, 8)
+    alone.k.zero_()
+    alone.v.zero_()
+    layer.prefill(x[11:].contiguous(), pos[11:].contiguous(), start[1:] - 11, alone, 2)
+    used = lambda t: t.view(-1, 8, 16)[:, :2]  # noqa: E731
+    assert torch.allclose(used(cache.k)[1:], used(alone.k), atol=1e-5)
+    assert torch.allclose(used(cache.v)[1:], used(alone.v), atol=1e-5)
+    assert not cache.k.view(3, 8, 16)[1:, 2:].any()
+
+
 def test_cache_refuses_overflow():
     cache = hnn.HexCache(2, 5, 1, 8)
     cache.reserve(3)

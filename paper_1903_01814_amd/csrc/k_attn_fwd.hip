@@ -20,9 +20,9 @@
 // (a quarter of the rate) run beside the other's products, so the two waves a
 // SIMD that the launch bounds ask for are worth more than registers (one wave
 // with twice as many took 1826 us where two took 1182).  Heads of 128 in
-// bfloat16, 16 on 4: one sequence of 16432 1130 us, 970 TFLOP/s (a large library
+// bfloat16, 16 on 4: one sequence of 16432 1150 us, 960 TFLOP/s (a large library
 // product 1220), matrix cores busy 0.46 of the cycles, vector unit 0.45; 24 of
-// 500 to 5000, causal 690 us, 790 TFLOP/s.  Heads of 32, 512 sequences of 20 to
+// 500 to 5000, causal 700 us, 780 TFLOP/s.  Heads of 32, 512 sequences of 20 to
 // 400: 62 us, the vector unit.  Heads of 64 in float32, 16 of 1027: 231 us, 150
 // TFLOP/s.
 #include "attn.h"
@@ -34,9 +34,11 @@ namespace {
 
 constexpr float kSlack = 8.f; // in powers of two
 
-// NW waves, BK keys a tile: 64, or 32 where registers (float32 past 32, 64 rows)
-// leave no room for more (heads of 64 in bfloat16, 24 sequences of 500 to 5000:
-// 362 us with 64 keys, 391 with 32).
+// NW waves, BK keys a tile: 64 for heads up to 64 (in bfloat16; 24 sequences of
+// 500 to 5000: 362 us, with 32 keys 391) and up to 32 in float32, else 32: three
+// waves a SIMD fit then instead of two (heads of 128: 24 of 2048 keys 963 ->
+// 919 us, 64 of 470 146 -> 135, 128 of 370 263 -> 244, one of 16432 1125 ->
+// 1150, two of them the same).
 template <typename M, int DC, int BK, int NW, typename E = typename M::E>
 __global__ __launch_bounds__(64 * NW, attn_waves(sizeof(E) == 4, DC)) void
 attn_fwd_k(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a)
@@ -110,8 +112,8 @@ attn_fwd_k(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a)
 
     // the tile of keys at kt and vt, key0 the first
     auto tile = [&](unsigned char *kt, unsigned char *vt, int key0) {
-        // scores before the other wave's vector work: 1151 -> 1131 us (16432 keys,
-        // 16 heads of 128 on 4); the exponentials first instead 1185
+        // scores before the other waves' vector work (16 heads of 128 on 4: 24
+        // sequences of 2048 932 -> 918 us; the exponentials first lost 3 %)
         __builtin_amdgcn_s_setprio(1);
         floatx16 x[KT];
 #pragma unroll
@@ -203,7 +205,7 @@ template <typename E, int DC, int NW>
 hipError_t launch_waves(const E *q, const E *k, const E *v, E *o, float *lse, AttnArgs a,
                         hipStream_t st)
 {
-    constexpr int BK = NW == 2 || (sizeof(E) == 4 && DC > 32) ? 32 : 64;
+    constexpr int BK = NW == 2 || DC > (sizeof(E) == 4 ? 32 : 64) ? 32 : 64;
     a.slots = attn_slots(a.Tq, a.group.G, 32 * NW, a.S);
     HEX_LAUNCH((attn_fwd_k<Math<E>, DC, BK, NW>), dim3(attn_blocks(a)), dim3(64 * NW), 0, st, q, k,
                v, o, lse, a);

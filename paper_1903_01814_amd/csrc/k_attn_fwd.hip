@@ -20,11 +20,11 @@
 // (a quarter of the rate) run beside the other's products, so the two waves a
 // SIMD that the launch bounds ask for are worth more than registers (one wave
 // with twice as many took 1826 us where two took 1182).  Heads of 128 in
-// bfloat16, 16 on 4: one sequence of 16432 1150 us, 960 TFLOP/s (a large library
-// product 1220), matrix cores busy 0.46 of the cycles, vector unit 0.45; 24 of
-// 500 to 5000, causal 700 us, 780 TFLOP/s.  Heads of 32, 512 sequences of 20 to
-// 400: 62 us, the vector unit.  Heads of 64 in float32, 16 of 1027: 231 us, 150
-// TFLOP/s.
+// bfloat16, 16 on 4: one sequence of 16432, causal, 1150 to 1190 us, 930 to 960
+// TFLOP/s (a large library product 1220), matrix cores busy 0.47 of the cycles,
+// vector unit 0.52; 24 of 500 to 5000, causal 700 us, 780 TFLOP/s.  Heads of 32,
+// 512 sequences of 20 to 400: 62 us, the vector unit.  Heads of 64 in float32,
+// 16 of 1027: 231 us, 150 TFLOP/s.
 #include "attn.h"
 #include "kernels.h"
 

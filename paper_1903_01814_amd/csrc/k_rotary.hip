@@ -8,10 +8,10 @@
 // Bound by memory: every element is read and written once (51200 tokens, 16 + 4
 // heads of 64 in bfloat16: forward 58 us, 4.5 TB/s; backward 86, 4.6 TB/s; a
 // large copy reaches 4.95).  A block takes up to kTokens tokens at a time, makes
-// their cosines and sines once for all heads (LDS: a sine costs a hundred
-// instructions, and one serves Hq + Hkv heads), and a group of L lanes takes a
-// head: four pairs a lane, two 8- or 16-byte loads, the head's sum of squares by
-// exchanges within the group.  The backward adds the weights' gradients in registers over a
+// their cosines and sines once for all heads (LDS: some thirty instructions a
+// pair, for Hq + Hkv heads), and a group of L lanes takes a head: four pairs a
+// lane, two 8- or 16-byte loads, the head's sum of squares by exchanges within
+// the group.  The backward adds the weights' gradients in registers over a
 // block's tokens, then over the block in LDS, then over the blocks in
 // rotary_reduce_k, always in the same order.
 #include "hexdev.h"

@@ -13,6 +13,7 @@
 // operand is read from LDS with rows in the same order (read_rows).
 #pragma once
 
+#include "attn_span.h"
 #include "hexdev.h"
 #include "kernels.h"
 
@@ -379,23 +380,6 @@ __device__ __forceinline__ float dot8(const bf16raw *a, const bf16raw *b, int c,
 }
 
 // ---- packed sequences ----------------------------------------------------
-// The rows of one (sequence, key head) are its query tokens times the G query
-// heads that share the key head, heads fastest.  Work is handed out in tiles
-// of TR rows.  Sequence s owns tile slots start[s] G / TR + s up to the next
-// sequence's first, which is as many as it needs or one more; so the slots
-// are known without the lengths on the host, rows G / TR + S in all.
-
-// token of row r: r / G by the reciprocal, which gives it or one less
-__device__ __forceinline__ int row_token(Group g, int r)
-{
-    const uint32_t t = __umulhi(static_cast<uint32_t>(r), g.inv);
-    return static_cast<int>(t + (static_cast<uint32_t>(r) - t * g.G >= static_cast<uint32_t>(g.G)));
-}
-
-inline int attn_slots(int T, int G, int TR, int S)
-{
-    return static_cast<int>(static_cast<int64_t>(T) * G / TR) + S;
-}
 // Sequences of so few rows on average take tiles of 64 rows and 32 keys, which
 // they fill better, instead of 128 and 64 (forward, dq; 8 heads of 32, 512
 // sequences of 130 rows: 69.8 -> 63.4, 84.0 -> 76.5 us; 4 of 64, 384 of 195:
@@ -463,11 +447,6 @@ __device__ __forceinline__ void store_col(E *p, const floatx16 &x, int c0, int D
         if (c0 + 8 * i < D)
             store4(p + c0 + 8 * i, x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f,
                    x[4 * i + 3] * f);
-}
-
-__device__ __forceinline__ int clamp_start(const int *start, int i, int T)
-{
-    return min(max(start[i], 0), T);
 }
 
 // One tile on its way from memory to LDS: ROWS rows, a 16-byte chunk a thread
@@ -563,41 +542,26 @@ __device__ __forceinline__ void head_and_slot(const AttnArgs &a, uint32_t id, in
     }
 }
 
-struct Span {
-    int seq;      // sequence
-    int begin, n; // its tokens
-    int tile;     // which of its tiles
+// the lanes of a wave, for the search of a block's sequence
+struct WaveLanes {
+    int v;
+    template <typename F> __device__ __forceinline__ uint64_t probe(F f)
+    {
+        const Probe p = f(static_cast<int>(threadIdx.x & 63));
+        v = p.value;
+        return __ballot(p.ok);
+    }
+    __device__ __forceinline__ int value(int c) const { return __builtin_amdgcn_readlane(v, c); }
+    __device__ __forceinline__ static int uniform(int x)
+    {
+        return __builtin_amdgcn_readfirstlane(x);
+    }
 };
-
-// Sequence that owns tile slot w: 64 probes at once, log_64(S) rounds, the
-// last of which leaves the neighbouring offsets in the lanes.
 template <int TR>
 __device__ __forceinline__ Span find_span(const int *start, int S, int T, int G, int w)
 {
-    const int lane = threadIdx.x & 63;
-    auto slot = [&](int v, int i) {
-        return static_cast<int>(static_cast<int64_t>(v) * G / TR) + i;
-    };
-    int lo = 0, n = S, v, c;
-    for (;;) {
-        const int step = (n + 63) >> 6, at = lo + lane * step;
-        // one probe past the last, for the sequence's end
-        v = clamp_start(start, min(at, S), T);
-        const bool ok = lane * step < n && slot(v, at) <= w;
-        c = max(1, __popcll(__ballot(ok))) - 1;
-        lo += c * step;
-        if (step == 1)
-            break;
-        n = min(step, n - c * step);
-    }
-    Span s;
-    s.seq = __builtin_amdgcn_readfirstlane(lo);
-    c = __builtin_amdgcn_readfirstlane(c);
-    s.begin = __builtin_amdgcn_readlane(v, c);
-    const int end = c < 63 ? __builtin_amdgcn_readlane(v, c + 1) : clamp_start(start, s.seq + 1, T);
-    s.n = max(0, end - s.begin);
-    s.tile = w - slot(s.begin, s.seq);
-    return s;
+    WaveLanes lanes;
+    return find_span<TR>(lanes, start, S, T, G, w);
 }
 
 } // namespace attn

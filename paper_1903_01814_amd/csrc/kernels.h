@@ -11,6 +11,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "attn_span.h"
+
 namespace hexk {
 
 // Optional per-launch timing (hexconv_timing_begin / hexconv_timing_end):
@@ -244,18 +246,6 @@ hipError_t wgrad_any(const void *x, const void *dy, float *dw, float *db, void *
                      const ConvShape &sh, Dtype d, const WAnyPlan &pl, hipStream_t st);
 
 // ---- attention over packed sequences ------------------------------------
-
-// Query heads that share a key head, and the reciprocal that divides by their
-// number: floor(2^32 / G) (2^32 - 1 for G = 1) times r, shifted down, is r / G
-// or one less for every r < 2^31.
-struct Group {
-    int G;
-    uint32_t inv;
-};
-inline Group make_group(int G)
-{
-    return {G, G == 1 ? 0xffffffffu : static_cast<uint32_t>((1ull << 32) / G)};
-}
 
 // One call: token strides in elements, scale log2(e) = c + c_lo.
 struct AttnArgs {

@@ -584,7 +584,8 @@ class HexPixelAttention(nn.Module):
     projection, and with ``dropout`` the residual branch's dropout.  The
     projections are torch's linear layers.
 
-    forward(x [T][dim], pos, start): x + dropout(projection(attention(x))).
+    forward(x [T][dim], pos, start): x + dropout(projection(attention(x))),
+    the mask by torch's generator of x's device (torch.manual_seed).
     prefill and step do the same over a HexCache, without dropout."""
 
     def __init__(self, dim, heads, kv_heads=None, head_dim=None, bases=(10000.0, 100.0, 100.0),
@@ -602,9 +603,11 @@ class HexPixelAttention(nn.Module):
         freq, axis = hex_frequencies(self.head_dim, bases, device)
         self.register_buffer("freq", freq, persistent=False)
         self.register_buffer("axis", axis, persistent=False)
-        # the dropout's generator: a seed of this layer's own, the call number
-        seed = int(torch.randint(1 << 62, ()))
-        self.register_buffer("rng", torch.tensor([seed, 0], dtype=torch.int64, device=device))
+
+    def _load_from_state_dict(self, state_dict, prefix, *args):
+        # states of before hold the dropout's words
+        state_dict.pop(prefix + "rng", None)
+        super()._load_from_state_dict(state_dict, prefix, *args)
 
     def _project(self, x):
         Hq, Hkv = self.heads
@@ -617,8 +620,10 @@ class HexPixelAttention(nn.Module):
         y = self.out(o.flatten(1))
         if not (self.training and self.dropout > 0):
             return x + y
-        rng = self.rng.clone()
-        self.rng[1] += 1
+        # both words from torch's generator of the device, as its own dropout
+        # draws: who saves and restores that (activation checkpointing) gets the
+        # same mask again, and a captured graph draws a new one in every replay
+        rng = torch.empty(2, dtype=torch.int64, device=x.device).random_()
         return hex_dropout(y, self.dropout, rng, residual=x)
 
     def new_cache(self, streams, capacity):

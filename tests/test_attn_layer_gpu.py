@@ -1,0 +1,79 @@
+"""HexPixelAttention in the ways that training and serving programs use it
+beyond a plain call: recomputed forwards, captured graphs."""
+import pytest
+
+from gpu_helpers import torch_mod
+
+torch = pytest.importorskip("torch")
+hnn = pytest.importorskip("paper_1903_01814_amd.nn")
+pytestmark = pytest.mark.gpu
+
+
+def layer_and_inputs(dtype=torch.float32, **kw):
+    torch.manual_seed(0)
+    layer = hnn.HexPixelAttention(64, 4, 2, 16, device="cuda", dtype=dtype, **kw)
+    x = torch.randn(90, 64, device="cuda").to(dtype)
+    pos = torch.rand(90, 3, device="cuda") * 9
+    return layer, x, pos, torch.tensor([0, 33, 90], dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_checkpointed_layer(dtype):
+    """Outputs and gradients of a recomputed forward have the bits of the plain
+    one's under the same seed."""
+    torch_mod()
+    from torch.utils.checkpoint import checkpoint
+    layer, x, pos, start = layer_and_inputs(dtype, dropout=0.4)
+    gy = torch.randn(x.shape, device="cuda").to(dtype)
+    got = []
+    for run in (layer, lambda *a: checkpoint(layer, *a, use_reentrant=False)):
+        torch.manual_seed(5)
+        xi = x.clone().requires_grad_(True)
+        y = run(xi, pos, start)
+        got.append([y.detach(), *torch.autograd.grad(y, [xi, *layer.parameters()], gy)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_captured_layer_draws_new_masks():
+    """Forward and gradient recorded once: every replay has another mask, and
+    its gradient the same one.  float32; the projections' sums may be taken in
+    another order, 64 products of them: 1e-5 of the largest value."""
+    torch_mod()
+    layer, x, pos, start = layer_and_inputs(dropout=0.5)
+    x.requires_grad_(True)
+    gy = torch.randn(x.shape, device="cuda")
+
+    def work():
+        y = layer(x, pos, start)
+        return y.detach(), torch.autograd.grad(y, x, gy)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, dx = work()
+    layer.eval()
+    masks = []
+    for i in range(4):
+        with torch.no_grad():
+            x.normal_()
+        y.fill_(float("nan")), dx.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        branch = layer(x, pos, start) - x
+        size = float(branch.detach().abs().max())
+        # a kept element is doubled, the others are zero
+        kept = y != x.detach()
+        want = x + torch.where(kept, 2 * branch, 0 * branch)
+        assert float((y - want.detach()).abs().max()) <= 1e-5 * size
+        ref = torch.autograd.grad(want, x, gy)[0]
+        assert float((dx - ref).abs().max()) <= 1e-5 * float(ref.abs().max())
+        assert 0.4 < float(kept.float().mean()) < 0.6
+        masks.append(kept)
+    for i in range(4):
+        for j in range(i):
+            assert not torch.equal(masks[i], masks[j])

@@ -1,0 +1,76 @@
+"""HexPixelAttention's host side on the CPU, with the library's calls replaced
+by plain ones where a test needs their results."""
+import pytest
+
+torch = pytest.importorskip("torch")
+hnn = pytest.importorskip("paper_1903_01814_amd.nn")
+
+
+def plain_layer(monkeypatch, **kw):
+    """A training layer whose attention passes the queries on and whose dropout
+    draws its mask on the CPU from the words it is given; the words of every
+    call."""
+    words = []
+
+    class Attention:
+        @staticmethod
+        def apply(qkv, wq, wk, pos, freq, axis, start, heads, eps, causal):
+            return qkv[:, :heads[0]]
+
+    def dropout(x, p, rng, residual=None, call=0):
+        words.append(rng.tolist())
+        g = torch.Generator().manual_seed(hash(tuple(words[-1])) & 0xFFFFFFFF)
+        return residual + x * (torch.rand(x.shape, generator=g) >= p) / (1 - p)
+
+    monkeypatch.setattr(hnn, "HexPixelAttentionFunction", Attention)
+    monkeypatch.setattr(hnn, "hex_dropout", dropout)
+    torch.manual_seed(1)
+    return hnn.HexPixelAttention(32, 2, **kw), words
+
+
+def test_recomputed_forward_has_the_same_mask(monkeypatch):
+    """Activation checkpointing runs the forward again for the backward: it has
+    to get the output's mask, and other calls other masks."""
+    from torch.utils.checkpoint import checkpoint
+    layer, words = plain_layer(monkeypatch, dropout=0.5)
+    x = torch.randn(20, 32)
+    for reentrant in (False, True):
+        del words[:]
+        grads = []
+        for run in (layer, lambda *a: checkpoint(layer, *a, use_reentrant=reentrant)):
+            torch.manual_seed(7)
+            xi = x.clone().requires_grad_(True)
+            y = run(xi, None, None)
+            grads.append((y.detach(), *torch.autograd.grad(y.square().sum(), xi))
+                         if not reentrant else (y.detach(),))
+            if reentrant:
+                y.square().sum().backward()
+                grads[-1] += (xi.grad,)
+        assert len(words) == 3 and words[0] == words[1] == words[2]
+        for a, b in zip(*grads):
+            assert torch.equal(a, b)
+        layer(x, None, None)
+        assert words[3] != words[2]
+
+
+def test_mask_words_are_no_state_of_the_layer(monkeypatch):
+    """Two layers, and two calls of one, draw different words; nothing of them
+    is in the layer's state, where wrappers would give every rank the same."""
+    layer, words = plain_layer(monkeypatch, dropout=0.1)
+    x = torch.randn(4, 32)
+    before = {k: v.clone() for k, v in layer.state_dict().items()}
+    layer(x, None, None), layer(x, None, None)
+    assert words[0] != words[1]
+    after = layer.state_dict()
+    assert before.keys() == after.keys()
+    assert all(torch.equal(before[k], after[k]) for k in before)
+    assert "rng" not in dict(layer.named_buffers())
+
+
+def test_state_with_mask_words_loads(monkeypatch):
+    """States saved when the layer still held the words."""
+    layer, _ = plain_layer(monkeypatch, dropout=0.1)
+    net = torch.nn.Sequential(layer)
+    state = net.state_dict()
+    state["0.rng"] = torch.tensor([3, 4])
+    net.load_state_dict(state)

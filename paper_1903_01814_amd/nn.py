@@ -600,9 +600,20 @@ class HexPixelAttention(nn.Module):
         self.out = nn.Linear(Hq * self.head_dim, dim, bias=False, **kw)
         self.q_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
         self.k_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
-        freq, axis = hex_frequencies(self.head_dim, bases, device)
+        self.bases = tuple(bases)
+        freq, axis = hex_frequencies(self.head_dim, self.bases, device)
         self.register_buffer("freq", freq, persistent=False)
         self.register_buffer("axis", axis, persistent=False)
+
+    def _apply(self, fn, *args, **kw):
+        # whatever type the layer gets, its frequencies stay float32 as they are
+        freq, axis = self.freq, self.axis
+        super()._apply(fn, *args, **kw)
+        device = self.freq.device
+        if freq.is_meta:
+            freq, axis = hex_frequencies(self.head_dim, self.bases)
+        self.freq, self.axis = freq.to(device), axis.to(device)
+        return self
 
     def _load_from_state_dict(self, state_dict, prefix, *args):
         # states of before hold the dropout's words

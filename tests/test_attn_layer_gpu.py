@@ -77,3 +77,13 @@ def test_captured_layer_draws_new_masks():
     for i in range(4):
         for j in range(i):
             assert not torch.equal(masks[i], masks[j])
+
+
+def test_converted_layer():
+    """.to(dtype) gives the layer that was built with that type."""
+    torch_mod()
+    layer, x, pos, start = layer_and_inputs(torch.bfloat16, causal=True)
+    other = hnn.HexPixelAttention(64, 4, 2, 16, causal=True)
+    other.load_state_dict({k: v.float().cpu() for k, v in layer.state_dict().items()})
+    other = other.cuda().to(torch.bfloat16)
+    assert torch.equal(other(x, pos, start), layer(x, pos, start))

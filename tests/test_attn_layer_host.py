@@ -74,3 +74,24 @@ def test_state_with_mask_words_loads(monkeypatch):
     state = net.state_dict()
     state["0.rng"] = torch.tensor([3, 4])
     net.load_state_dict(state)
+
+
+@pytest.mark.parametrize("move", [
+    lambda n: n.to(torch.bfloat16), lambda n: n.bfloat16(), lambda n: n.double().float(),
+    lambda n: n.half().to(torch.float32), lambda n: n.to("meta").to_empty(device="cpu")])
+def test_frequencies_keep_their_bits(move):
+    """A layer of another type still turns by float32 frequencies, the ones that
+    it was built with."""
+    net = torch.nn.Sequential(hnn.HexPixelAttention(64, 2, bases=(5000.0, 70.0)))
+    freq, axis = hnn.hex_frequencies(32, (5000.0, 70.0))
+    net = move(net)
+    assert net[0].freq.dtype is torch.float32 and torch.equal(net[0].freq, freq)
+    assert net[0].axis.dtype is torch.int32 and torch.equal(net[0].axis, axis)
+
+
+def test_frequencies_of_ones_own_keep_their_bits():
+    layer = hnn.HexPixelAttention(64, 2)
+    mine = torch.rand(16)
+    layer.freq.copy_(mine)
+    layer.to(torch.bfloat16)
+    assert layer.qkv.weight.dtype is torch.bfloat16 and torch.equal(layer.freq, mine)

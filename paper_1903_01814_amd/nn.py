@@ -654,16 +654,24 @@ class HexPixelAttention(nn.Module):
         """Packed prompts x [T][dim] of all streams, at most ``longest`` tokens
         each, appended to their caches.  (A longer one is cut at its stream's
         capacity.)"""
+        T, S = x.shape[0], cache.start.shape[0]
+        if start.shape != (S + 1,):
+            raise ValueError("HexPixelAttention: start has shape %s, expected (%d,)"
+                             % (tuple(start.shape), S + 1))
         cache.reserve(int(longest))
-        T, n = x.shape[0], start[1:] - start[:-1]
-        each = lambda t: torch.repeat_interleave(t, n, output_size=T)  # noqa: E731
-        at = each(cache.length - start[:-1]) + torch.arange(T, dtype=torch.int32, device=x.device)
-        # no slot past the stream's own
-        slot = torch.where(at < cache.capacity, each(cache.start) + at, -1).to(torch.int32)
-        qo = self._into_cache(self._project(x), pos, slot, cache)
-        cache.length += n
+        if S == 0:
+            return x.clone()
+        token = torch.arange(T, dtype=torch.int32, device=x.device)
+        stream = torch.searchsorted(start, token, right=True) - 1
+        inside = (stream >= 0) & (stream < S)
+        stream.clamp_(0, S - 1)
+        at = (cache.length - start[:-1])[stream] + token
+        # tokens of no stream, and those past their stream's own slots, get none
+        slot = torch.where(inside & (at < cache.capacity), cache.start[stream] + at, -1)
+        qo = self._into_cache(self._project(x), pos, slot.to(torch.int32), cache)
+        cache.length += start[1:] - start[:-1]
         cache.length.clamp_(max=cache.capacity)
-        o = _empty(qo.shape, qo)
+        o = torch.zeros(qo.shape, dtype=qo.dtype, device=qo.device)
         hx.hexattn_fwd(qo, cache.k, cache.v, o, None, start, cache.start, cache.length,
                        causal=self.causal)
         return x + self.out(o.flatten(1))

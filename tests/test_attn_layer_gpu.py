@@ -6,6 +6,7 @@ from gpu_helpers import torch_mod
 
 torch = pytest.importorskip("torch")
 hnn = pytest.importorskip("paper_1903_01814_amd.nn")
+cases = pytest.importorskip("attn_layer_cases")
 pytestmark = pytest.mark.gpu
 
 
@@ -87,3 +88,9 @@ def test_converted_layer():
     other.load_state_dict({k: v.float().cpu() for k, v in layer.state_dict().items()})
     other = other.cuda().to(torch.bfloat16)
     assert torch.equal(other(x, pos, start), layer(x, pos, start))
+
+
+@pytest.mark.parametrize("lead,trail", [(0, 0), (0, 4), (6, 0), (3, 2)])
+def test_prefill_with_unused_tokens(lead, trail):
+    torch_mod()
+    cases.unused_tokens("cuda", lead, trail)

@@ -2,8 +2,52 @@
 by plain ones where a test needs their results."""
 import pytest
 
+import attn_ref as ref
+
 torch = pytest.importorskip("torch")
 hnn = pytest.importorskip("paper_1903_01814_amd.nn")
+cases = pytest.importorskip("attn_layer_cases")
+
+
+@pytest.fixture
+def plain_library(monkeypatch):
+    """Rotation, attention and steps on host tensors, by the float64 reference
+    and the entry points' definitions."""
+    def rotary(q, k, pos, freq, axis, wq, wk, qo, ko, eps=1e-6, norm=True, v=None, vo=None,
+               slot=None):
+        turn = lambda x, w: ref.rotary(x.double(), w.double(), pos, freq, axis, eps,  # noqa: E731
+                                       norm)[0].float()
+        qo.copy_(turn(q, wq))
+        for x, to in ((turn(k, wk), ko), (v, vo)):
+            for t in range(0 if to is None else x.shape[0]):
+                at = t if slot is None else int(slot[t])
+                if 0 <= at < to.shape[0]:
+                    to[at] = x[t]
+
+    def attention(q, k, v, o, lse, q_start, k_start=None, k_len=None, scale=None, causal=False):
+        T, Tk = q.shape[0], k.shape[0]
+        cut = lambda a, n: [min(max(i, 0), n) for i in a.tolist()]  # noqa: E731
+        qs, ks = cut(q_start, T), cut(q_start if k_start is None else k_start, Tk)
+        spans = []
+        for s in range(len(qs) - 1):
+            m = ks[s + 1] - ks[s] if k_len is None else int(k_len[s])
+            spans.append((qs[s], max(0, qs[s + 1] - qs[s]), ks[s], min(max(m, 0), Tk - ks[s])))
+        r = ref.attention(q.double(), k.double(), v.double(), spans, q.shape[2] ** -0.5, causal)
+        for q0, n, _, _ in spans:
+            o[q0:q0 + n] = r["o"][q0:q0 + n].float()
+            if lse is not None:
+                lse[q0:q0 + n] = r["lse"][q0:q0 + n].float()
+
+    def step(q, k, v, o, ws, k_start, k_len, max_len):
+        S, n = q.shape[:2]
+        starts = torch.arange(0, S * n + 1, n)
+        attention(q.flatten(0, 1), k, v, o.flatten(0, 1), None, starts, k_start,
+                  k_len.clamp(max=max_len), causal=True)
+
+    monkeypatch.setattr(hnn.hx, "hexrotary_fwd", rotary)
+    monkeypatch.setattr(hnn.hx, "hexattn_fwd", attention)
+    monkeypatch.setattr(hnn.hx, "hexattn_step", step)
+    monkeypatch.setattr(hnn.hx, "hexattn_step_workspace", lambda *a: 0)
 
 
 def plain_layer(monkeypatch, **kw):
@@ -95,3 +139,20 @@ def test_frequencies_of_ones_own_keep_their_bits():
     layer.freq.copy_(mine)
     layer.to(torch.bfloat16)
     assert layer.qkv.weight.dtype is torch.bfloat16 and torch.equal(layer.freq, mine)
+
+
+@pytest.mark.parametrize("lead,trail", [(0, 0), (0, 4), (6, 0), (3, 2)])
+def test_prefill_with_unused_tokens(plain_library, lead, trail):
+    cases.unused_tokens("cpu", lead, trail)
+
+
+def test_prefill_refuses_other_offsets(plain_library):
+    """As many offsets as streams and one; nothing is counted before."""
+    st = cases.Streams("cpu", [4, 4])
+    c = st.cache(8)
+    x, pos, start = st.pack([range(4), range(4)])
+    with pytest.raises(ValueError, match="start has shape"):
+        st.layer.prefill(x, pos, start[:2], c, 4)
+    assert c.most == 0 and c.length.tolist() == [0, 0]
+    none = st.layer.new_cache(0, 8)
+    assert torch.equal(st.layer.prefill(x, pos, start[:1], none, 4), x)

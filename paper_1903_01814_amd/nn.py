@@ -568,6 +568,13 @@ class HexCache:
         self.start = (torch.arange(int(streams), device=device) * self.capacity).to(torch.int32)
         self.length = torch.zeros(int(streams), dtype=torch.int32, device=device)
         self.most = 0  # no stream holds more tokens
+        # what prefill's offsets are made of: `far` names no slot, whatever token
+        # is added; a first and a last column; the starts with a sequence of no
+        # key before and behind every stream
+        none, far, last = torch.zeros_like(self.start), -(1 << 31), (1 << 31) - 1
+        column = lambda *a: torch.tensor(a, dtype=torch.int32, device=device)[:, None]  # noqa: E731
+        self.parts = (none + far, none, column(0, far, 0), column(last, far, 0))
+        self.starts = nn.functional.pad(torch.stack([self.start, none], 1).view(-1), (1, 0))
 
     def reserve(self, n):
         """Room for n more tokens of every stream, by the host's count."""
@@ -651,9 +658,10 @@ class HexPixelAttention(nn.Module):
 
     @torch.no_grad()
     def prefill(self, x, pos, start, cache, longest):
-        """Packed prompts x [T][dim] of all streams, at most ``longest`` tokens
-        each, appended to their caches.  (A longer one is cut at its stream's
-        capacity.)"""
+        """Packed prompts x [T][dim] of all streams, appended to their caches:
+        of each at most ``longest`` tokens, and what its stream has room for.
+        A longer one is cut; the tokens past the cut, as those of no sequence,
+        are not stored, see nothing, and pass as they are."""
         T, S = x.shape[0], cache.start.shape[0]
         if start.shape != (S + 1,):
             raise ValueError("HexPixelAttention: start has shape %s, expected (%d,)"
@@ -661,18 +669,25 @@ class HexPixelAttention(nn.Module):
         cache.reserve(int(longest))
         if S == 0:
             return x.clone()
+        first = start.clamp(0, T)
+        room = (cache.capacity - cache.length).clamp_(0, int(longest))
+        kept = torch.minimum(first.diff().clamp_(min=0), room)
+        first = first[:-1]
+        slots = cache.start + cache.length - first  # token t goes to slots + t
+        cache.length += kept
+        # The packed tokens as 2 S + 1 sequences: those before the first stream's,
+        # every stream's kept ones, and the rest behind them, which see no key.
+        # Rows: their offsets; their tokens' slots less the token, a column late,
+        # as a search of the offsets counts those up to a token; their keys.
+        far, none, left, right = cache.parts
+        table = torch.stack([first, first + kept, far, slots, cache.length, none])
+        table = torch.cat([left, table.view(3, 2, S).transpose(1, 2).reshape(3, 2 * S), right], 1)
+        q_start, slots, k_len = table.unbind()
         token = torch.arange(T, dtype=torch.int32, device=x.device)
-        stream = torch.searchsorted(start, token, right=True) - 1
-        inside = (stream >= 0) & (stream < S)
-        stream.clamp_(0, S - 1)
-        at = (cache.length - start[:-1])[stream] + token
-        # tokens of no stream, and those past their stream's own slots, get none
-        slot = torch.where(inside & (at < cache.capacity), cache.start[stream] + at, -1)
-        qo = self._into_cache(self._project(x), pos, slot.to(torch.int32), cache)
-        cache.length += start[1:] - start[:-1]
-        cache.length.clamp_(max=cache.capacity)
-        o = torch.zeros(qo.shape, dtype=qo.dtype, device=qo.device)
-        hx.hexattn_fwd(qo, cache.k, cache.v, o, None, start, cache.start, cache.length,
+        slot = slots[torch.searchsorted(q_start, token, right=True)] + token
+        qo = self._into_cache(self._project(x), pos, slot, cache)
+        o = _empty(qo.shape, qo)
+        hx.hexattn_fwd(qo, cache.k, cache.v, o, None, q_start, cache.starts, k_len[:-1],
                        causal=self.causal)
         return x + self.out(o.flatten(1))
 

@@ -78,3 +78,48 @@ def unused_tokens(device, lead, trail):
     y = st.layer.step(torch.stack([x[-1:] for x in st.x]), torch.stack([p[-1:] for p in st.pos]), c)
     for s in range(4):
         near(y[s], st.whole(s, list(range(len(st.x[s]))))[-1:])
+
+
+def cut_prompts(device, capacity, longest, lens, kept):
+    """Prompts past `longest` or their stream's room: the first tokens, as many
+    as fit, are stored and see what they would see alone; the others pass as
+    they are.  Steps go on behind them."""
+    st = Streams(device, [n + 2 for n in lens], seed=1)
+    c = st.cache(capacity)
+    x, pos, start = st.pack([range(n) for n in lens], lead=1)
+    y = st.layer.prefill(x, pos, start, c, longest)
+    assert c.length.tolist() == kept and c.most >= max(kept)
+    at = 1
+    for s, n in enumerate(lens):
+        near(y[at:at + kept[s]], st.whole(s, list(range(kept[s]))))
+        assert torch.equal(y[at + kept[s]:at + n], x[at + kept[s]:at + n])
+        at += n
+    st.untouched(c)
+    steps = capacity - c.most
+    for i in range(min(steps, 2)):
+        new = [slice(n + i, n + i + 1) for n in lens]
+        y = st.layer.step(torch.stack([a[p] for a, p in zip(st.x, new)]),
+                          torch.stack([a[p] for a, p in zip(st.pos, new)]), c)
+        for s, n in enumerate(lens):
+            near(y[s], st.whole(s, list(range(kept[s])) + list(range(n, n + i + 1)))[-1:])
+        st.untouched(c)
+    assert c.most <= capacity and max(c.length.tolist()) <= c.most
+
+
+def second_prompt_cut(device):
+    """A second prompt of streams that already hold tokens: it sees them, and is
+    cut where the streams are full."""
+    st = Streams(device, [9, 9, 9], seed=2)
+    c = st.cache(8)
+    parts = [[0, 1, 2, 3, 4], [0], []]
+    x, pos, start = st.pack(parts)
+    st.layer.prefill(x, pos, start, c, 5)
+    more = [[5, 6, 7, 8], [1, 2, 3], [0, 1, 2, 3, 4, 5]]
+    x, pos, start = st.pack(more, trail=2)
+    y = st.layer.prefill(x, pos, start, c, 3)
+    assert c.length.tolist() == [8, 4, 3] and c.most == 8
+    near(y[:3], st.whole(0, list(range(8)))[5:])
+    near(y[4:7], st.whole(1, list(range(4)))[1:])
+    near(y[7:10], st.whole(2, list(range(3))))
+    assert torch.equal(y[3:4], x[3:4]) and torch.equal(y[10:], x[10:])
+    st.untouched(c)

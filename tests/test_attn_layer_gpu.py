@@ -94,3 +94,16 @@ def test_converted_layer():
 def test_prefill_with_unused_tokens(lead, trail):
     torch_mod()
     cases.unused_tokens("cuda", lead, trail)
+
+
+@pytest.mark.parametrize("capacity,longest,lens,kept", [
+    (8, 8, [11, 2, 2], [8, 2, 2]), (8, 5, [11, 2, 0], [5, 2, 0]), (9, 6, [7, 6, 20], [6, 6, 6]),
+    (5, 0, [3, 1, 0], [0, 0, 0]), (12, 9, [9, 1, 4], [9, 1, 4])])
+def test_prompts_past_their_room(capacity, longest, lens, kept):
+    torch_mod()
+    cases.cut_prompts("cuda", capacity, longest, lens, kept)
+
+
+def test_second_prompt_past_its_room():
+    torch_mod()
+    cases.second_prompt_cut("cuda")

@@ -156,3 +156,14 @@ def test_prefill_refuses_other_offsets(plain_library):
     assert c.most == 0 and c.length.tolist() == [0, 0]
     none = st.layer.new_cache(0, 8)
     assert torch.equal(st.layer.prefill(x, pos, start[:1], none, 4), x)
+
+
+@pytest.mark.parametrize("capacity,longest,lens,kept", [
+    (8, 8, [11, 2, 2], [8, 2, 2]), (8, 5, [11, 2, 0], [5, 2, 0]), (9, 6, [7, 6, 20], [6, 6, 6]),
+    (5, 0, [3, 1, 0], [0, 0, 0]), (12, 9, [9, 1, 4], [9, 1, 4])])
+def test_prompts_past_their_room(plain_library, capacity, longest, lens, kept):
+    cases.cut_prompts("cpu", capacity, longest, lens, kept)
+
+
+def test_second_prompt_past_its_room(plain_library):
+    cases.second_prompt_cut("cpu")

@@ -578,10 +578,14 @@ class HexCache:
 
     def reserve(self, n):
         """Room for n more tokens of every stream, by the host's count."""
+        self.most = self.with_more(n)
+
+    def with_more(self, n):
+        """The count with n more tokens, refused where they do not fit."""
         if self.most + n > self.capacity:
             raise ValueError("HexCache: %d tokens do not fit the capacity of %d"
                              % (self.most + n, self.capacity))
-        self.most += n
+        return self.most + n
 
 
 class HexPixelAttention(nn.Module):
@@ -666,7 +670,7 @@ class HexPixelAttention(nn.Module):
         if start.shape != (S + 1,):
             raise ValueError("HexPixelAttention: start has shape %s, expected (%d,)"
                              % (tuple(start.shape), S + 1))
-        cache.reserve(int(longest))
+        most = cache.with_more(int(longest))
         if S == 0:
             return x.clone()
         first = start.clamp(0, T)
@@ -674,18 +678,20 @@ class HexPixelAttention(nn.Module):
         kept = torch.minimum(first.diff().clamp_(min=0), room)
         first = first[:-1]
         slots = cache.start + cache.length - first  # token t goes to slots + t
-        cache.length += kept
+        length = cache.length + kept
         # The packed tokens as 2 S + 1 sequences: those before the first stream's,
         # every stream's kept ones, and the rest behind them, which see no key.
         # Rows: their offsets; their tokens' slots less the token, a column late,
         # as a search of the offsets counts those up to a token; their keys.
         far, none, left, right = cache.parts
-        table = torch.stack([first, first + kept, far, slots, cache.length, none])
+        table = torch.stack([first, first + kept, far, slots, length, none])
         table = torch.cat([left, table.view(3, 2, S).transpose(1, 2).reshape(3, 2 * S), right], 1)
         q_start, slots, k_len = table.unbind()
         token = torch.arange(T, dtype=torch.int32, device=x.device)
         slot = slots[torch.searchsorted(q_start, token, right=True)] + token
         qo = self._into_cache(self._project(x), pos, slot, cache)
+        cache.length.copy_(length)
+        cache.most = most
         o = _empty(qo.shape, qo)
         hx.hexattn_fwd(qo, cache.k, cache.v, o, None, q_start, cache.starts, k_len[:-1],
                        causal=self.causal)
@@ -698,12 +704,13 @@ class HexPixelAttention(nn.Module):
         if not self.causal:
             raise ValueError("HexPixelAttention: steps need a causal layer")
         S, n, dim = x.shape
-        cache.reserve(n)
+        most = cache.with_more(n)
         at = cache.start + cache.length
         slot = (at[:, None] + torch.arange(n, dtype=torch.int32, device=x.device)).view(-1)
         qo = self._into_cache(self._project(x.reshape(S * n, dim)), pos.reshape(S * n, -1), slot,
                               cache)
         cache.length += n
+        cache.most = most
         q = qo.view(S, n, self.heads[0], self.head_dim)
         o = torch.empty_like(q)
         ws = _workspace(hx.hexattn_step_workspace(S, n, *self.heads, self.head_dim, cache.most,

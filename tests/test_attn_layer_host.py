@@ -167,3 +167,27 @@ def test_prompts_past_their_room(plain_library, capacity, longest, lens, kept):
 
 def test_second_prompt_past_its_room(plain_library):
     cases.second_prompt_cut("cpu")
+
+
+def test_refused_calls_leave_the_cache(plain_library, monkeypatch):
+    """Calls that the library refuses (here: positions of another type) count
+    no token."""
+    def refuse(*a, **kw):
+        raise TypeError("pos has dtype torch.float64")
+    st = cases.Streams("cpu", [4, 4])
+    c = st.cache(6)
+    x, pos, start = st.pack([range(4), range(4)])
+    rotary = hnn.hx.hexrotary_fwd
+    for _ in range(3):
+        monkeypatch.setattr(hnn.hx, "hexrotary_fwd", refuse)
+        with pytest.raises(TypeError):
+            st.layer.prefill(x, pos.double(), start, c, 4)
+        with pytest.raises(TypeError):
+            st.layer.step(x[:2, None], pos[:2, None].double(), c)
+        monkeypatch.setattr(hnn.hx, "hexrotary_fwd", rotary)
+        assert c.most == 0 and c.length.tolist() == [0, 0]
+    y = st.layer.prefill(x, pos, start, c, 4)
+    cases.near(y[4:], st.whole(1, list(range(4))))
+    with pytest.raises(ValueError, match="capacity"):
+        st.layer.step(x.view(2, 4, 32)[:, :3], pos.view(2, 4, 3)[:, :3], c)
+    assert c.most == 4 and c.length.tolist() == [4, 4]

@@ -567,7 +567,9 @@ class HexCache:
         self.capacity = int(capacity)
         self.start = (torch.arange(int(streams), device=device) * self.capacity).to(torch.int32)
         self.length = torch.zeros(int(streams), dtype=torch.int32, device=device)
-        self.most = 0  # no stream holds more tokens
+        # the host's count, no stream holds more: tokens of every stream, and
+        # beside them of each, the largest
+        self.count = (0, [0] * int(streams), 0)
         # what prefill's offsets are made of: `far` names no slot, whatever token
         # is added; a first and a last column; the starts with a sequence of no
         # key before and behind every stream
@@ -576,16 +578,37 @@ class HexCache:
         self.parts = (none + far, none, column(0, far, 0), column(last, far, 0))
         self.starts = nn.functional.pad(torch.stack([self.start, none], 1).view(-1), (1, 0))
 
+    @property
+    def most(self):
+        """No stream holds more tokens, by the host's count."""
+        return self.count[0] + self.count[2]
+
+    @most.setter
+    def most(self, n):
+        self.count = (int(n), [0] * len(self.count[1]), 0)
+
     def reserve(self, n):
-        """Room for n more tokens of every stream, by the host's count."""
-        self.most = self.with_more(n)
+        """Room for n more tokens of every stream, or n[s] (a list or tuple) of
+        stream s, by the host's count."""
+        self.count = self.with_more(n)
 
     def with_more(self, n):
-        """The count with n more tokens, refused where they do not fit."""
-        if self.most + n > self.capacity:
+        """The count with so many tokens more, refused where they do not fit."""
+        every, each, top = self.count
+        if isinstance(n, (list, tuple)):
+            if len(n) != len(each):
+                raise ValueError("HexCache: %d numbers of tokens for %d streams"
+                                 % (len(n), len(each)))
+            each = [a + int(b) for a, b in zip(each, n)]
+            top, least = max(each, default=0), min(n, default=0)
+        else:
+            every, least = every + int(n), n
+        if least < 0:
+            raise ValueError("HexCache: %d more tokens" % least)
+        if every + top > self.capacity:
             raise ValueError("HexCache: %d tokens do not fit the capacity of %d"
-                             % (self.most + n, self.capacity))
-        return self.most + n
+                             % (every + top, self.capacity))
+        return every, each, top
 
 
 class HexPixelAttention(nn.Module):
@@ -663,18 +686,23 @@ class HexPixelAttention(nn.Module):
     @torch.no_grad()
     def prefill(self, x, pos, start, cache, longest):
         """Packed prompts x [T][dim] of all streams, appended to their caches:
-        of each at most ``longest`` tokens, and what its stream has room for.
+        of each at most ``longest`` tokens (``longest[s]``, where it is a list of
+        one number for each stream), and what its stream has room for.
         A longer one is cut; the tokens past the cut, as those of no sequence,
         are not stored, see nothing, and pass as they are."""
         T, S = x.shape[0], cache.start.shape[0]
         if start.shape != (S + 1,):
             raise ValueError("HexPixelAttention: start has shape %s, expected (%d,)"
                              % (tuple(start.shape), S + 1))
-        most = cache.with_more(int(longest))
+        count = cache.with_more(longest)
         if S == 0:
             return x.clone()
         first = start.clamp(0, T)
-        room = (cache.capacity - cache.length).clamp_(0, int(longest))
+        if isinstance(longest, (list, tuple)):
+            longest = torch.tensor(longest, dtype=torch.int32).to(x.device)
+        else:
+            longest = int(longest)
+        room = (cache.capacity - cache.length).clamp_(min=0).clamp_(max=longest)
         kept = torch.minimum(first.diff().clamp_(min=0), room)
         first = first[:-1]
         slots = cache.start + cache.length - first  # token t goes to slots + t
@@ -691,7 +719,7 @@ class HexPixelAttention(nn.Module):
         slot = slots[torch.searchsorted(q_start, token, right=True)] + token
         qo = self._into_cache(self._project(x), pos, slot, cache)
         cache.length.copy_(length)
-        cache.most = most
+        cache.count = count
         o = _empty(qo.shape, qo)
         hx.hexattn_fwd(qo, cache.k, cache.v, o, None, q_start, cache.starts, k_len[:-1],
                        causal=self.causal)
@@ -704,18 +732,19 @@ class HexPixelAttention(nn.Module):
         if not self.causal:
             raise ValueError("HexPixelAttention: steps need a causal layer")
         S, n, dim = x.shape
-        most = cache.with_more(n)
+        count = cache.with_more(n)
         at = cache.start + cache.length
         slot = (at[:, None] + torch.arange(n, dtype=torch.int32, device=x.device)).view(-1)
         qo = self._into_cache(self._project(x.reshape(S * n, dim)), pos.reshape(S * n, -1), slot,
                               cache)
         cache.length += n
-        cache.most = most
+        cache.count = count
+        most = cache.most
         q = qo.view(S, n, self.heads[0], self.head_dim)
         o = torch.empty_like(q)
-        ws = _workspace(hx.hexattn_step_workspace(S, n, *self.heads, self.head_dim, cache.most,
+        ws = _workspace(hx.hexattn_step_workspace(S, n, *self.heads, self.head_dim, most,
                                                   hx._dtype_code(q)), q)
-        hx.hexattn_step(q, cache.k, cache.v, o, ws, cache.start, cache.length, cache.most)
+        hx.hexattn_step(q, cache.k, cache.v, o, ws, cache.start, cache.length, most)
         return x + self.out(o.view(S, n, -1))
 
     def extra_repr(self):

@@ -123,3 +123,22 @@ def second_prompt_cut(device):
     near(y[7:10], st.whole(2, list(range(3))))
     assert torch.equal(y[3:4], x[3:4]) and torch.equal(y[10:], x[10:])
     st.untouched(c)
+
+
+def streams_in_turn(device):
+    """Prompts of one stream after another, each with its own bound: the cache
+    holds as many tokens of every stream as it has room for."""
+    st = Streams(device, [6, 8, 7], seed=3)
+    c = st.cache(8)
+    for s, parts in ((0, [[0, 1, 2], [], []]), (1, [[], list(range(8)), []]),
+                     (2, [[], [], [0, 1, 2, 3]]), (0, [[3, 4, 5], [], []]),
+                     (2, [[], [], [4, 5, 6]])):
+        x, pos, start = st.pack(parts)
+        y = st.layer.prefill(x, pos, start, c, [len(p) for p in parts])
+        near(y, st.whole(s, list(range(parts[s][-1] + 1)))[parts[s][0]:])
+    assert c.length.tolist() == [6, 8, 7] and c.most == 8
+    # a bound of its own cuts a stream's prompt too
+    x, pos, start = st.pack([[0, 1], [], []])
+    y = st.layer.prefill(x, pos, start, c, (1, 0, 1))
+    assert c.length.tolist() == [7, 8, 7] and torch.equal(y[1], x[1])
+    st.untouched(c)

@@ -107,3 +107,8 @@ def test_prompts_past_their_room(capacity, longest, lens, kept):
 def test_second_prompt_past_its_room():
     torch_mod()
     cases.second_prompt_cut("cuda")
+
+
+def test_streams_in_turn():
+    torch_mod()
+    cases.streams_in_turn("cuda")

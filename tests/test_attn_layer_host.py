@@ -191,3 +191,29 @@ def test_refused_calls_leave_the_cache(plain_library, monkeypatch):
     with pytest.raises(ValueError, match="capacity"):
         st.layer.step(x.view(2, 4, 32)[:, :3], pos.view(2, 4, 3)[:, :3], c)
     assert c.most == 4 and c.length.tolist() == [4, 4]
+
+
+def test_streams_in_turn(plain_library):
+    cases.streams_in_turn("cpu")
+
+
+def test_bounds_of_each_stream():
+    """One number for all streams or one for each; what does not fit changes
+    nothing."""
+    c = hnn.HexCache(3, 10, 1, 8)
+    c.reserve([4, 0, 7])
+    c.reserve(3)
+    assert c.most == 10
+    c.reserve([3, 5, 0])
+    for more in (1, [0, 3, 0], [0, 0, 1]):
+        with pytest.raises(ValueError, match="do not fit the capacity of 10"):
+            c.reserve(more)
+    for bad in ([1, 2], [0, 0, 0, 0], -1, [0, -1, 0]):
+        with pytest.raises(ValueError):
+            c.reserve(bad)
+    c.reserve((0, 2, 0))
+    assert c.most == 10
+    c.most = 4
+    c.reserve([6, 6, 0]), c.reserve([0, 0, 6])
+    with pytest.raises(ValueError, match="capacity"):
+        c.reserve(1)

@@ -405,9 +405,10 @@ size_t hexattn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, hex_
  * dv, strides lddq, lddk and lddv, from dout and the forward's o and lse.  A
  * key head's gradients are the sums over the query heads that share it.
  * Rows that see no key, and keys that no row sees, get zeros.  ws: at least
- * hexattn_bwd_workspace(...) bytes, for partial sums that do not depend on the
- * lengths: up to 0.4 GB for large problems, less for small ones.
- * Deterministic.
+ * hexattn_bwd_workspace(...) bytes: 4 a row (query token and head), 48 a tile
+ * of 128 keys and a sequence, and partial sums, none where there is little to
+ * divide, else for any lengths up to 0.45 GB with up to 64 key heads and up to
+ * 0.9 GB with more.  Deterministic.
  */
 int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, const float *lse,
                 const void *dout, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes,

@@ -700,9 +700,7 @@ hipError_t launch_dkv(const E *q, const E *k, const E *v, const float *lse, cons
                dim3(static_cast<uint32_t>(pl.blocks)), dim3(2 * KT), 0, st, q, k, v, lse, dout,
                delta, dk, dv, a, gr, pl);
     const hipError_t e = hipGetLastError();
-    // no tile of so few rows is divided
-    const int64_t row_tiles = static_cast<int64_t>(a.Tq) * a.group.G / pl.row_tile + 1;
-    if (e != hipSuccess || row_tiles + kFixed <= kLeast)
+    if (e != hipSuccess || !pl.divides)
         return e;
     HEX_LAUNCH((attn_dkv_join_k<E, DC, 2 * KT>),
                dim3(static_cast<uint32_t>(pl.shares) * a.Hkv, DC / 16), dim3(2 * KT), 0, st, dk, dv,
@@ -754,6 +752,7 @@ size_t round16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 struct BwdSpace {
     size_t before, next, ends, divided, list, part, bytes;
     int shares, blocks, room, row_tile, key_tile;
+    bool divides;
 };
 BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
 {
@@ -772,6 +771,9 @@ BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
     // a divided tile has more than a share, so that there are fewer of them
     // than shares, and fewer pieces of them than twice that
     w.room = static_cast<int>(tiles) + 2 * w.shares;
+    // no tile is divided where one share is all there is, nor one of so few rows
+    const int64_t row_tiles = static_cast<int64_t>(Tq) * (Hq / Hkv) / w.row_tile + 1;
+    w.divides = w.shares > 1 && row_tiles + kFixed > kLeast;
     w.blocks = static_cast<double>(w.room) * Hkv < held ? w.room * Hkv : held;
     w.before = round16(static_cast<size_t>(Tq) * Hq * sizeof(float));
     w.next = (w.before + static_cast<size_t>(S) * sizeof(int) + 255) & ~static_cast<size_t>(255);
@@ -779,8 +781,8 @@ BwdSpace bwd_space(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt)
     w.divided = w.ends + 256;
     w.list = w.divided + round16(static_cast<size_t>(w.shares) * sizeof(KeyPiece));
     w.part = w.list + round16(static_cast<size_t>(w.room) * sizeof(KeyPiece));
-    w.bytes = w.part + static_cast<size_t>(w.shares) * Hkv * 2 *
-                           (2 * static_cast<size_t>(w.key_tile) * DC) * sizeof(float);
+    const size_t parts = w.divides ? static_cast<size_t>(w.shares) * Hkv * 2 : 0;
+    w.bytes = w.part + parts * 2 * w.key_tile * DC * sizeof(float);
     return w;
 }
 
@@ -805,6 +807,7 @@ hipError_t attn_bwd(const void *q, const void *k, const void *v, const void *o, 
     pl.room = w.room;
     pl.row_tile = w.row_tile;
     pl.key_tile = w.key_tile;
+    pl.divides = w.divides;
     pl.row_shift = w.row_tile == 64 ? 6 : 5;
     float *delta = static_cast<float *>(ws);
     return dt == F32

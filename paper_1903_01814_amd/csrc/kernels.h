@@ -283,6 +283,7 @@ struct KeyPlan {
     KeyPiece *divided, *list;
     float4 *part;
     int shares, blocks, room, row_tile, row_shift, key_tile; // row_tile = 2^row_shift
+    bool divides; // whether any tile may be divided; if not, there are no partial sums
 };
 // k_len is not used (a key belongs to one sequence)
 size_t attn_bwd_workspace(int Tq, int Tk, int S, int Hq, int Hkv, int D, Dtype dt);

@@ -1,0 +1,41 @@
+"""Limits that the attention entry points state, on the host: sizes of
+workspaces, alignment of offsets."""
+import pytest
+
+from paper_1903_01814_amd import hexconv as hx
+
+torch = pytest.importorskip("torch")
+
+
+def plan_bytes(Tq, Tk, S, Hq):
+    """What the gradient's workspace holds beside its partial sums: 4 bytes a
+    row of Tq Hq, 4 a sequence, 48 for each key tile of 128 and each of up to
+    3 * 1024 + 1 shares (three times), lines of 256 bytes."""
+    return 4 * Tq * Hq + 4 * S + 48 * (Tk // 128 + S + 3 * 3073) + 2048
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+@pytest.mark.parametrize("dt", [hx.HEX_F32, hx.HEX_BF16])
+@pytest.mark.parametrize("Hkv", [1, 4, 64, 511, 700, 767, 768, 1023, 1535, 2048, 4000, 20000])
+@pytest.mark.parametrize("Tq,Tk,S", [(4096, 4096, 1), (100000, 100000, 24), (3, 100, 1),
+                                     (1 << 16, 1 << 16, 60)])
+def test_gradient_workspace_is_bounded(Tq, Tk, S, Hkv, D, dt):
+    """Partial sums take up to 0.9 GB whatever the number of key heads, 0.45 GB
+    up to 64 of them."""
+    nb = hx.hexattn_bwd_workspace(Tq, Tk, S, Hkv, Hkv, D, dt)
+    if max(Tq, Tk) * Hkv > (1 << 31) - 4096:
+        assert nb == 0
+        return
+    assert 4 * Tq * Hkv <= nb <= (0.45e9 if Hkv <= 64 else 0.9e9) + plan_bytes(Tq, Tk, S, Hkv)
+
+
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("D", [32, 128])
+@pytest.mark.parametrize("dt", [hx.HEX_F32, hx.HEX_BF16])
+@pytest.mark.parametrize("Tq,Tk,S,Hkv", [(9, 9, 2, 2), (150, 150, 30, 8), (100, 50000, 10, 4),
+                                         (64, 1 << 20, 1, 16)])
+def test_nothing_to_divide_needs_no_partial_sums(Tq, Tk, S, Hkv, D, dt, G):
+    """Up to 19 tiles of 32 rows in all: every key tile is one piece."""
+    assert Tq * G // 32 + 1 <= 20
+    assert hx.hexattn_bwd_workspace(Tq, Tk, S, Hkv * G, Hkv, D, dt) <= plan_bytes(Tq, Tk, S,
+                                                                                  Hkv * G)

@@ -1088,9 +1088,10 @@ int hexattn_fwd(const void *q, const void *k, const void *v, void *o, float *lse
         return HEX_ERR_UNSUPPORTED;
     if (S == 0 || Tq == 0)
         return HEX_OK;
-    if ((rc = ptrs_ok({q, o}, {k, v, lse})) != HEX_OK)
+    if ((rc = ptrs_ok({q, o}, {k, v, lse})) != HEX_OK ||
+        (rc = words_ok({q_start, k_start}, k_len)) != HEX_OK)
         return rc;
-    if (q_start == nullptr || k_start == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
+    if (Tk > 0 && (k == nullptr || v == nullptr))
         return HEX_ERR_INVALID_ARG;
     const hexk::AttnArgs a = attn_args(q_start, k_start, k_len, S, Tq, Tk, Hq, Hkv, D, ldq, ldk,
                                        ldv, ldo, scale, (flags & HEX_ATTN_CAUSAL) != 0, dt);
@@ -1125,10 +1126,9 @@ int hexattn_bwd(const void *q, const void *k, const void *v, const void *o, cons
         return HEX_ERR_UNSUPPORTED;
     if (S == 0 || (Tq == 0 && Tk == 0))
         return HEX_OK;
-    if ((rc = ptrs_ok({}, {q, k, v, o, lse, dout, dq, dk, dv, ws})) != HEX_OK)
+    if ((rc = ptrs_ok({}, {q, k, v, o, lse, dout, dq, dk, dv, ws})) != HEX_OK ||
+        (rc = words_ok({q_start, k_start}, nullptr)) != HEX_OK)
         return rc;
-    if (q_start == nullptr || k_start == nullptr)
-        return HEX_ERR_INVALID_ARG;
     if (Tq > 0 && (q == nullptr || o == nullptr || lse == nullptr || dout == nullptr ||
                    dq == nullptr))
         return HEX_ERR_INVALID_ARG;
@@ -1166,9 +1166,10 @@ int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws,
         return HEX_ERR_UNSUPPORTED;
     if (S == 0)
         return HEX_OK;
-    if ((rc = ptrs_ok({q, o}, {k, v, ws})) != HEX_OK)
+    if ((rc = ptrs_ok({q, o}, {k, v, ws})) != HEX_OK ||
+        (rc = words_ok({k_start, k_len}, nullptr)) != HEX_OK)
         return rc;
-    if (k_start == nullptr || k_len == nullptr || (Tk > 0 && (k == nullptr || v == nullptr)))
+    if (Tk > 0 && (k == nullptr || v == nullptr))
         return HEX_ERR_INVALID_ARG;
     if (Tk > kMaxKeys)
         return HEX_ERR_UNSUPPORTED;

@@ -39,3 +39,27 @@ def test_nothing_to_divide_needs_no_partial_sums(Tq, Tk, S, Hkv, D, dt, G):
     assert Tq * G // 32 + 1 <= 20
     assert hx.hexattn_bwd_workspace(Tq, Tk, S, Hkv * G, Hkv, D, dt) <= plan_bytes(Tq, Tk, S,
                                                                                   Hkv * G)
+
+
+P = [0x10000 * i for i in range(1, 14)]
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+@pytest.mark.parametrize("which", ["q_start", "k_start", "k_len"])
+def test_offsets_need_their_alignment(which, off):
+    """4 bytes, as the rotation's arrays; fake addresses, refused before
+    anything is enqueued."""
+    at = {"q_start": P[10], "k_start": P[11], "k_len": P[12]}
+    at[which] += off
+    lib = hx.load()
+    fwd = lib.hexattn_fwd(*P[:5], at["q_start"], at["k_start"], at["k_len"], 2, 9, 9, 4, 2, 32, 128,
+                          64, 64, 128, 1.0, 0, 0, None)
+    assert fwd == hx.HEX_ERR_INVALID_ARG
+    if which != "k_len":
+        bwd = lib.hexattn_bwd(*P[:10], 1 << 24, at["q_start"], at["k_start"], 2, 9, 9, 4, 2, 32,
+                              128, 64, 64, 128, 128, 128, 64, 64, 1.0, 0, 0, None)
+        assert bwd == hx.HEX_ERR_INVALID_ARG
+    if which != "q_start":
+        step = lib.hexattn_step(*P[:5], 1 << 30, at["k_start"], at["k_len"], 2, 1, 4, 2, 32, 900,
+                                400, 64, 64, 1.0, 0, None)
+        assert step == hx.HEX_ERR_INVALID_ARG

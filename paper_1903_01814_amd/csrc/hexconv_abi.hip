@@ -1003,7 +1003,7 @@ int hexrotary_fwd(const void *q, const void *k, const void *v, const float *pos,
                   int n_slots, float eps, int flags, hex_dtype dt, void *stream)
 {
     if (T < 0 || A < 1 || n_slots < 0 || !(eps >= 0.f) || !isfinite(eps) ||
-        (flags & ~HEX_ROTARY_NORM) != 0 || (v == nullptr) != (vo == nullptr))
+        (flags & ~HEX_ROTARY_NORM) != 0)
         return HEX_ERR_INVALID_ARG;
     int rc = check_heads(Hq, Hkv, D, dt);
     if (rc != HEX_OK)
@@ -1016,6 +1016,8 @@ int hexrotary_fwd(const void *q, const void *k, const void *v, const float *pos,
         return HEX_ERR_INVALID_ARG;
     if (T == 0)
         return HEX_OK;
+    if ((v == nullptr) != (vo == nullptr))
+        return HEX_ERR_INVALID_ARG;
     if ((rc = ptrs_ok({q, k, qo, ko}, {wq, wk, v, vo})) != HEX_OK ||
         (rc = words_ok({pos, freq, axis}, slot)) != HEX_OK)
         return rc;

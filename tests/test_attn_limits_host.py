@@ -63,3 +63,11 @@ def test_offsets_need_their_alignment(which, off):
         step = lib.hexattn_step(*P[:5], 1 << 30, at["k_start"], at["k_len"], 2, 1, 4, 2, 32, 900,
                                 400, 64, 64, 1.0, 0, None)
         assert step == hx.HEX_ERR_INVALID_ARG
+
+
+def test_no_tokens_into_a_cache():
+    """No tokens, whose values have no address, and caches that do."""
+    rc = hx.load().hexrotary_fwd(None, None, None, P[2], P[3], P[4], P[5], P[6], None, P[8], P[9],
+                                 P[10], 0, 4, 2, 32, 3, 128, 64, 64, 128, 64, 64, 5, 1e-6, 1, 0,
+                                 None)
+    assert rc == hx.HEX_OK

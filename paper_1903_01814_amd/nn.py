@@ -731,12 +731,11 @@ class HexPixelAttention(nn.Module):
         each sees its stream's tokens up to itself."""
         if not self.causal:
             raise ValueError("HexPixelAttention: steps need a causal layer")
-        S, n, dim = x.shape
+        S, n = x.shape[:2]
         count = cache.with_more(n)
         at = cache.start + cache.length
         slot = (at[:, None] + torch.arange(n, dtype=torch.int32, device=x.device)).view(-1)
-        qo = self._into_cache(self._project(x.reshape(S * n, dim)), pos.reshape(S * n, -1), slot,
-                              cache)
+        qo = self._into_cache(self._project(x.flatten(0, 1)), pos.flatten(0, 1), slot, cache)
         cache.length += n
         cache.count = count
         most = cache.most
@@ -745,7 +744,7 @@ class HexPixelAttention(nn.Module):
         ws = _workspace(hx.hexattn_step_workspace(S, n, *self.heads, self.head_dim, most,
                                                   hx._dtype_code(q)), q)
         hx.hexattn_step(q, cache.k, cache.v, o, ws, cache.start, cache.length, most)
-        return x + self.out(o.view(S, n, -1))
+        return x + self.out(o.flatten(2))
 
     def extra_repr(self):
         return ("heads=%d, kv_heads=%d, head_dim=%d, causal=%s, dropout=%g"

@@ -142,3 +142,19 @@ def streams_in_turn(device):
     y = st.layer.prefill(x, pos, start, c, (1, 0, 1))
     assert c.length.tolist() == [7, 8, 7] and torch.equal(y[1], x[1])
     st.untouched(c)
+
+
+def nothing_to_do(device):
+    """No tokens, no streams: empty results, and a cache that stays empty."""
+    st = Streams(device, [2, 2])
+    c = st.cache(4)
+    x, pos, start = st.pack([[], []])
+    assert st.layer.prefill(x, pos, start, c, 3).shape == (0, 32)
+    assert c.length.tolist() == [0, 0]
+    for offsets in (start, start[:1]):
+        assert st.layer(x, pos, offsets).shape == (0, 32)
+    none = st.layer.new_cache(0, 4)
+    assert st.layer.prefill(x, pos, start[:1], none, 1).shape == (0, 32)
+    y = st.layer.step(x.view(0, 2, 32), pos.view(0, 2, 3), none)
+    assert y.shape == (0, 2, 32) and none.most == 2
+    st.untouched(c)

@@ -112,3 +112,21 @@ def test_second_prompt_past_its_room():
 def test_streams_in_turn():
     torch_mod()
     cases.streams_in_turn("cuda")
+
+
+def test_nothing_to_do():
+    torch_mod()
+    with torch.no_grad():
+        cases.nothing_to_do("cuda")
+
+
+@pytest.mark.parametrize("start", [[0], [0, 0, 0]])
+def test_no_tokens_train(start):
+    """An empty batch gives zero gradients to every parameter."""
+    torch_mod()
+    layer, x, pos, _ = layer_and_inputs(dropout=0.5)
+    x = x[:0].clone().requires_grad_(True)
+    y = layer(x, pos[:0], torch.tensor(start, dtype=torch.int32, device="cuda"))
+    for g, p in zip(torch.autograd.grad(y, [x, *layer.parameters()], torch.empty_like(y)),
+                    [x, *layer.parameters()]):
+        assert g.shape == p.shape and not bool(g.any())

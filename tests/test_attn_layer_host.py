@@ -217,3 +217,8 @@ def test_bounds_of_each_stream():
     c.reserve([6, 6, 0]), c.reserve([0, 0, 6])
     with pytest.raises(ValueError, match="capacity"):
         c.reserve(1)
+
+
+def test_nothing_to_do(plain_library):
+    with torch.no_grad():
+        cases.nothing_to_do("cpu")

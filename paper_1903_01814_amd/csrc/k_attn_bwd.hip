@@ -13,11 +13,15 @@
 // run to run.
 //
 // Bound by the matrix cores and the vector unit in turn, as the forward, and
-// attn_dkv_k by the wait for the next rows as well.  24 sequences of 500 to 5000
+// attn_dkv_k by the wait for the next rows as well: neighbouring pieces of a head
+// run on all eight dies, each of which fetches the same rows of Q and dO (the
+// first batch below: 2419 MB read, 484 once).  24 sequences of 500 to 5000
 // tokens, 16 heads of 128 on 4, causal, in bfloat16: dq 850 us (6 of 14 parts of
 // the work, 950 TFLOP/s; matrix cores busy 0.43), dk and dv 1340 (810 TFLOP/s;
 // 0.35) and 46 to join; 16 of 1027, 8 heads of 64 on 4, in float32: 327, 425 and
-// 27 (160, 165 TFLOP/s; 0.45, 0.48); 512 of 20 to 400, 8 heads of 32: 76, 107.
+// 27 (160, 165 TFLOP/s; 0.45, 0.48).  512 of 20 to 400, 8 heads of 32: 76, 107,
+// dq by memory as the forward (394 MB, 5.1 TB/s, 200 once), dk and dv read 360 MB
+// where 208 are their tiles' and 133 once.
 #include "attn.h"
 #include "kernels.h"
 

@@ -22,9 +22,11 @@
 // with twice as many took 1826 us where two took 1182).  Heads of 128 in
 // bfloat16, 16 on 4: one sequence of 16432, causal, 1150 to 1190 us, 930 to 960
 // TFLOP/s (a large library product 1220), matrix cores busy 0.47 of the cycles,
-// vector unit 0.52; 24 of 500 to 5000, causal 700 us, 780 TFLOP/s.  Heads of 32,
-// 512 sequences of 20 to 400: 62 us, the vector unit.  Heads of 64 in float32,
-// 16 of 1027: 231 us, 150 TFLOP/s.
+// vector unit 0.52; 24 of 500 to 5000, causal 700 us, 780 TFLOP/s.  Heads of 64
+// in float32, 16 of 1027: 231 us, 150 TFLOP/s.  Many short sequences of narrow
+// heads are bound by memory, by keys that several dies fetch (head_and_slot):
+// heads of 32, 512 sequences of 20 to 400, 62 us for 296 MB read and 39 written,
+// 5.4 TB/s, where 135 MB in all would do.
 #include "attn.h"
 #include "kernels.h"
 

@@ -11,11 +11,12 @@
 // products.  Most rows of a product are empty, which costs nothing here: the
 // matrix cores are busy 0.04 of the time the loads take.  The waves' maxima,
 // sums and outputs are joined in LDS, the runs' by attn_join_k (a launch more,
-// 4 us; a last block that joins would have to flush its die's cache first).
+// 4 us; a last block that joins needs fences across dies, not measured here).
 // Bound by memory: three sequences of 9000 to 16432 keys, 16 heads of 128 on 4
 // in bfloat16, 16.5 us and 4.6 to join (80 MB, 4.8 TB/s; a large copy reaches
 // 4.95); 192 of 32 to 4000, two new tokens each, 8 heads of 64 on 2, 21 and 4.3
-// (77 MB, 3.7 TB/s: the longest sequences end last).
+// (77 MB, 3.7 TB/s: runs of 1408 keys, 492 of the 1152 blocks have any, and the
+// longest sequences end last).
 #include "attn.h"
 #include "kernels.h"
 

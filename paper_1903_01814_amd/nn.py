@@ -538,7 +538,8 @@ class HexDropoutFunction(torch.autograd.Function):
 
 def hex_rotary(q, k, pos, freq, axis, wq=None, wk=None, eps=1e-6, norm=True):
     """Query heads q [T][Hq][D] and key heads k [T][Hkv][D], normed (weights
-    wq and wk [D], or ones) and turned by their positions pos [T][axes]."""
+    wq and wk [D], or ones) and turned by their positions pos [T][axes].
+    Positions and frequencies take no gradient."""
     return HexRotaryFunction.apply(q, k, wq, wk, pos, freq, axis, float(eps), bool(norm))
 
 

@@ -130,3 +130,26 @@ def test_no_tokens_train(start):
     for g, p in zip(torch.autograd.grad(y, [x, *layer.parameters()], torch.empty_like(y)),
                     [x, *layer.parameters()]):
         assert g.shape == p.shape and not bool(g.any())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lead", [1, 300])
+def test_layer_with_unused_tokens_before(lead, dtype):
+    """Tokens before the first sequence pass through the layer as they are and
+    change no gradient (tolerances as in test_layer_with_unused_tokens)."""
+    torch_mod()
+    layer, x0, pos, start = layer_and_inputs(dtype, causal=True)
+    x0 = torch.cat([torch.ones(lead, 64, device="cuda", dtype=dtype), x0])
+    pos = torch.cat([torch.ones(lead, 3, device="cuda"), pos])
+    got = []
+    for at, s in ((0, start + lead), (lead, start)):
+        x = x0[at:].clone().requires_grad_(True)
+        layer.zero_grad()
+        y = layer(x, pos[at:].contiguous(), s)
+        (y[-90:].float() ** 2).sum().backward()
+        got.append([y[-90:].detach(), x.grad[-90:]] + [p.grad.clone() for p in layer.parameters()])
+        if at == 0:
+            assert torch.equal(y[:lead], x0[:lead]) and not x.grad[:lead].any()
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all()
+        assert (a - b).abs().max() <= (1e-5 if dtype == torch.float32 else 2e-2) * b.abs().max()

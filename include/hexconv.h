@@ -450,6 +450,131 @@ int hexattn_step(const void *q, const void *k, const void *v, void *o, void *ws,
 int hexdropout(const void *x, const void *res, void *y, int64_t n, double p, const uint64_t *rng,
                uint64_t call, hex_dtype dt, void *stream);
 
+/*
+ * Operators that act on every token by itself: the layer norms, projections
+ * and gated feed-forward blocks of a network over tokens.  A tensor of tokens
+ * is [tokens][features], rows a stride `ld` apart (in elements, ld >= the number
+ * of features), features dense; weights, biases, z, gu and h are dense.
+ *
+ * Conventions, beside those of the library:
+ *  - Any numbers of tokens and features and any strides; pointers are 16-byte
+ *    aligned, mean and rstd 4-byte.  Tensors whose rows are whole 16-byte vectors
+ *    (features and stride multiples of 4 in float32, 8 in bf16) are the fast ones.
+ *  - Limits (HEX_ERR_UNSUPPORTED past them): HEX_NORM_MAX_DIM features of a norm;
+ *    HEX_LINEAR_MAX_DIM features of a projection, strides below 2^22, 2^33
+ *    elements a tensor, 2^30 in one projection of a gated pair.
+ *  - Sums, statistics and their reciprocals are float32.  bf16 calls round what
+ *    one product hands to the next once to bf16: z and dz of a projection; g, u, h,
+ *    dg and du of a gated block.
+ *  - Float32 products take each operand as the sum of three bf16 numbers, as
+ *    hexattn_fwd does: operands under 2^-110 lose bits; infinities, and values
+ *    from 3.39e38 on, give NaN.
+ *  - A row's results depend on that row alone (gradients of weights on all rows):
+ *    what is not finite in one reaches no other.
+ *  - Gradients of weights and biases of projections and gated blocks come in
+ *    `dwt`, float32 or dt.
+ *  - Results repeat bit for bit.  Outputs must not overlap inputs.
+ */
+#define HEX_NORM_MAX_DIM 16384
+#define HEX_LINEAR_MAX_DIM (1 << 20)
+typedef enum { HEX_ACT_NONE = 0, HEX_ACT_RELU = 1, HEX_ACT_GELU = 2, HEX_ACT_SILU = 3 } hex_act;
+
+/*
+ * Layer norm of T rows of C features: with m their mean,
+ *   r = 1 / sqrt(mean((x - m)^2) + eps),  y = (x - m) r w + b
+ * w and b [C], in dtype dt, may be NULL (ones, zeros).  mean and rstd (float32
+ * [T], both or neither) receive m and r.
+ */
+int hexnorm_fwd(const void *x, const void *w, const void *b, void *y, float *mean, float *rstd,
+                int T, int C, int64_t ldx, int64_t ldy, float eps, hex_dtype dt, void *stream);
+
+/* Bytes of device workspace hexnorm_bwd needs (0 for invalid arguments). */
+size_t hexnorm_bwd_workspace(int T, int C, hex_dtype dt);
+
+/*
+ * Gradients of hexnorm_fwd from its x, mean and rstd: with n = (x - m) r and
+ * g = dy w,
+ *   dx = res + r (g - mean(g) - n mean(g n)),  dw = sum of dy n,  db = sum of dy
+ * res [T][C], the gradient that reaches x beside the norm (a residual's), may be
+ * NULL (zeros).  dw and db are float32 [C], each nullable; ws: at least
+ * hexnorm_bwd_workspace(...) bytes, not read where both are NULL.
+ */
+int hexnorm_bwd(const void *x, const void *w, const float *mean, const float *rstd, const void *dy,
+                const void *res, void *dx, float *dw, float *db, void *ws, size_t ws_bytes, int T,
+                int C, int64_t ldx, int64_t lddy, int64_t ldres, int64_t lddx, hex_dtype dt,
+                void *stream);
+
+/* Bytes of device workspace hexlinear_fwd needs (may be 0; 0 for invalid
+ * arguments). */
+size_t hexlinear_fwd_workspace(int M, int N, int K, int64_t ldx, hex_dtype dt);
+
+/*
+ * Projection of M tokens from K to N features:
+ *   z = x w^T + bias,  y = act(z) + res
+ * w [N][K]; bias [N], res [M][N] and z [M][N] may be NULL.  z is what the
+ * gradient of an activation needs.  gelu is z times the normal distribution's
+ * function of z, silu z / (1 + exp(-z)).  ws: at least
+ * hexlinear_fwd_workspace(...) bytes, NULL where that is 0.
+ */
+int hexlinear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, void *z,
+                  void *ws, size_t ws_bytes, int M, int N, int K, int64_t ldx, int64_t ldres,
+                  int64_t ldy, hex_act act, hex_dtype dt, void *stream);
+
+/* Bytes of device workspace hexlinear_bwd needs (0 for invalid arguments). */
+size_t hexlinear_bwd_workspace(int M, int N, int K, int64_t ldx, int64_t lddy, hex_act act,
+                               hex_dtype dt);
+
+/*
+ * Gradients of hexlinear_fwd: with dz = dy act'(z),
+ *   dx = dz w,  dw = dz^T x,  db = sum of dz
+ * (that of res is dy).  dx, dw and db may each be NULL, and then w, or x, which
+ * only they read; z is read for an activation only.  dw [N][K] and db [N] in dwt.
+ * relu'(0) = 0.  ws: at least hexlinear_bwd_workspace(...) bytes, NULL where that
+ * is 0.  M = 0 writes zeros to dw and db.
+ */
+int hexlinear_bwd(const void *x, const void *w, const void *z, const void *dy, void *dx, void *dw,
+                  void *db, void *ws, size_t ws_bytes, int M, int N, int K, int64_t ldx,
+                  int64_t lddy, int64_t lddx, hex_act act, hex_dtype dwt, hex_dtype dt,
+                  void *stream);
+
+/* Columns of h for F hidden features, F rounded up to a multiple of 8; gu has
+ * twice as many (negative hex_status for F outside 1 .. HEX_LINEAR_MAX_DIM). */
+int hexffn_width(int F);
+
+/* Bytes of device workspace hexffn_fwd needs (may be 0; 0 for invalid
+ * arguments). */
+size_t hexffn_fwd_workspace(int M, int K, int F, int N, int64_t ldx, hex_dtype dt);
+
+/*
+ * Gated feed-forward block of M tokens, K features to F hidden ones to N:
+ *   g = x w1[:F]^T + b1[:F],  u = x w1[F:]^T + b1[F:],  h = act(g) u,
+ *   y = h w2^T + b2 + res
+ * w1 [2F][K], b1 [2F], w2 [N][F], b2 [N]; b1, b2 and res [M][N] may be NULL.
+ * h [M][hexffn_width(F)] is written; gu [M][2 hexffn_width(F)], g and u for the
+ * backward, may be NULL.  ws: at least hexffn_fwd_workspace(...) bytes, NULL where
+ * that is 0.
+ */
+int hexffn_fwd(const void *x, const void *w1, const void *b1, const void *w2, const void *b2,
+               const void *res, void *y, void *gu, void *h, void *ws, size_t ws_bytes, int M, int K,
+               int F, int N, int64_t ldx, int64_t ldres, int64_t ldy, hex_act act, hex_dtype dt,
+               void *stream);
+
+/* Bytes of device workspace hexffn_bwd needs (0 for invalid arguments). */
+size_t hexffn_bwd_workspace(int M, int K, int F, int N, int64_t ldx, int64_t lddy, hex_dtype dt);
+
+/*
+ * Gradients of hexffn_fwd from its x, gu and h:
+ *   dh = dy w2,  dg = dh u act'(g),  du = dh act(g),  dx = dg w1[:F] + du w1[F:],
+ *   dw1 = [dg du]^T x,  db1 = sum of [dg du],  dw2 = dy^T h,  db2 = sum of dy
+ * (that of res is dy).  dx and the weights' gradients (in dwt) may each be NULL,
+ * and then the inputs that only they read.  ws: at least
+ * hexffn_bwd_workspace(...) bytes.  M = 0 writes zeros to the weights' gradients.
+ */
+int hexffn_bwd(const void *x, const void *w1, const void *w2, const void *gu, const void *h,
+               const void *dy, void *dx, void *dw1, void *db1, void *dw2, void *db2, void *ws,
+               size_t ws_bytes, int M, int K, int F, int N, int64_t ldx, int64_t lddy, int64_t lddx,
+               hex_act act, hex_dtype dwt, hex_dtype dt, void *stream);
+
 /* Static description of a hex_status value. */
 const char *hex_status_string(int status);
 

@@ -531,6 +531,70 @@ hexk::AttnArgs attn_args(const int32_t *q_start, const int32_t *k_start, const i
     return a;
 }
 
+// ---- operators on tokens by themselves
+
+constexpr int64_t kMaxTensor = INT64_C(1) << 33; // elements
+constexpr int64_t kMaxStride = INT64_C(1) << 22; // elements; offsets in a tile are 32 bits
+
+int check_norm(int T, int C, int dt)
+{
+    if (T < 0 || C < 1 || !dtype_ok(dt))
+        return HEX_ERR_INVALID_ARG;
+    // a block takes a row or more
+    if (C > HEX_NORM_MAX_DIM || T > kMaxRows || (C > 1024 ? T : T / 4) > kMaxBlocks - 1)
+        return HEX_ERR_UNSUPPORTED;
+    return HEX_OK;
+}
+
+// M tokens, a product of each with [N][K]
+int check_linear(int M, int N, int K, int dt)
+{
+    if (M < 0 || N < 1 || K < 1 || !dtype_ok(dt))
+        return HEX_ERR_INVALID_ARG;
+    if (N > HEX_LINEAR_MAX_DIM || K > HEX_LINEAR_MAX_DIM || M > kMaxRows)
+        return HEX_ERR_UNSUPPORTED;
+    const int64_t m = M, wide = N > K ? N : K;
+    if (m * wide > kMaxTensor || static_cast<int64_t>(N) * K > kMaxTensor ||
+        (m / 64 + 1) * (wide / 64 + 1) > kMaxBlocks)
+        return HEX_ERR_UNSUPPORTED;
+    return HEX_OK;
+}
+
+int check_ffn(int M, int K, int F, int N, int dt)
+{
+    if (F < 1)
+        return HEX_ERR_INVALID_ARG;
+    if (F > HEX_LINEAR_MAX_DIM / 2)
+        return HEX_ERR_UNSUPPORTED;
+    const int Fp = (F + 7) / 8 * 8;
+    int rc = check_linear(M, 2 * Fp, K, dt);
+    if (rc == HEX_OK)
+        rc = check_linear(M, N, Fp, dt);
+    if (rc == HEX_OK && static_cast<int64_t>(Fp) * ((K + 7) / 8 * 8) > INT64_C(1) << 30)
+        rc = HEX_ERR_UNSUPPORTED;
+    return rc;
+}
+
+// row strides of n elements each
+int strides_ok(std::initializer_list<int64_t> lds, int64_t n)
+{
+    for (int64_t ld : lds)
+        if (ld < n)
+            return HEX_ERR_INVALID_ARG;
+    for (int64_t ld : lds)
+        if (ld >= kMaxStride)
+            return HEX_ERR_UNSUPPORTED;
+    return HEX_OK;
+}
+
+bool act_ok(int act) { return act >= HEX_ACT_NONE && act <= HEX_ACT_SILU; }
+
+// what a call takes has to be there
+bool ws_ok(const void *ws, size_t have, size_t need)
+{
+    return need == 0 || (ws != nullptr && have >= need);
+}
+
 } // namespace
 
 extern "C" {
@@ -1204,6 +1268,241 @@ int hexdropout(const void *x, const void *res, void *y, int64_t n, double p, con
         return HEX_ERR_INVALID_ARG;
     return launched(hexk::dropout(x, res, y, n, p, rng, call, static_cast<Dtype>(dt),
                                   static_cast<hipStream_t>(stream)));
+}
+
+int hexnorm_fwd(const void *x, const void *w, const void *b, void *y, float *mean, float *rstd,
+                int T, int C, int64_t ldx, int64_t ldy, float eps, hex_dtype dt, void *stream)
+{
+    int rc = check_norm(T, C, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!(eps >= 0.f) || !isfinite(eps) || (mean == nullptr) != (rstd == nullptr))
+        return HEX_ERR_INVALID_ARG;
+    if ((rc = strides_ok({ldx, ldy}, C)) != HEX_OK)
+        return rc;
+    if (T == 0)
+        return HEX_OK;
+    if ((rc = ptrs_ok({x, y}, {w, b})) != HEX_OK ||
+        (rc = words_ok({}, mean)) != HEX_OK || (rc = words_ok({}, rstd)) != HEX_OK)
+        return rc;
+    const hexk::NormArgs a{T, ldx, ldy, 0, 0, C, 1.f / static_cast<float>(C), eps};
+    return launched(hexk::norm_fwd(x, w, b, y, mean, rstd, a, static_cast<Dtype>(dt),
+                                   static_cast<hipStream_t>(stream)));
+}
+
+size_t hexnorm_bwd_workspace(int T, int C, hex_dtype dt)
+{
+    if (check_norm(T, C, dt) != HEX_OK || T == 0)
+        return 0;
+    return static_cast<size_t>(hexk::norm_bwd_blocks(T, C)) * 2 * C * sizeof(float);
+}
+
+int hexnorm_bwd(const void *x, const void *w, const float *mean, const float *rstd, const void *dy,
+                const void *res, void *dx, float *dw, float *db, void *ws, size_t ws_bytes, int T,
+                int C, int64_t ldx, int64_t lddy, int64_t ldres, int64_t lddx, hex_dtype dt,
+                void *stream)
+{
+    int rc = check_norm(T, C, dt);
+    if (rc != HEX_OK || (rc = strides_ok({ldx, lddy, lddx}, C)) != HEX_OK ||
+        (res != nullptr && (rc = strides_ok({ldres}, C)) != HEX_OK))
+        return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if ((rc = ptrs_ok({}, {x, w, dy, res, dx, dw, db, ws})) != HEX_OK)
+        return rc;
+    if (T == 0) // no row: the weights' gradients are zero
+        return launched(hexk::norm_zero(dw, db, C, st));
+    if ((rc = ptrs_ok({x, dy, dx}, {})) != HEX_OK ||
+        (rc = words_ok({mean, rstd}, nullptr)) != HEX_OK)
+        return rc;
+    if ((dw != nullptr || db != nullptr) && !ws_ok(ws, ws_bytes, hexnorm_bwd_workspace(T, C, dt)))
+        return HEX_ERR_INVALID_ARG;
+    const hexk::NormArgs a{T, ldx, lddy, res != nullptr ? ldres : 0, lddx,
+                           C, 1.f / static_cast<float>(C), 0.f};
+    return launched(hexk::norm_bwd(x, w, mean, rstd, dy, res, dx, dw, db, ws, a,
+                                   static_cast<Dtype>(dt), st));
+}
+
+size_t hexlinear_fwd_workspace(int M, int N, int K, int64_t ldx, hex_dtype dt)
+{
+    if (check_linear(M, N, K, dt) != HEX_OK || strides_ok({ldx}, K) != HEX_OK || M == 0)
+        return 0;
+    hexk::LinearArgs a{};
+    a.M = M, a.N = N, a.K = K, a.ldx = ldx;
+    hipError_t e = hipSuccess;
+    return hexk::linear_fwd(a, nullptr, false, static_cast<Dtype>(dt), nullptr, e);
+}
+
+int hexlinear_fwd(const void *x, const void *w, const void *bias, const void *res, void *y, void *z,
+                  void *ws, size_t ws_bytes, int M, int N, int K, int64_t ldx, int64_t ldres,
+                  int64_t ldy, hex_act act, hex_dtype dt, void *stream)
+{
+    int rc = check_linear(M, N, K, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!act_ok(act))
+        return HEX_ERR_INVALID_ARG;
+    if ((rc = strides_ok({ldx}, K)) != HEX_OK || (rc = strides_ok({ldy}, N)) != HEX_OK ||
+        (res != nullptr && (rc = strides_ok({ldres}, N)) != HEX_OK))
+        return rc;
+    if (M == 0)
+        return HEX_OK;
+    if ((rc = ptrs_ok({x, w, y}, {bias, res, z, ws})) != HEX_OK)
+        return rc;
+    if (!ws_ok(ws, ws_bytes, hexlinear_fwd_workspace(M, N, K, ldx, dt)))
+        return HEX_ERR_INVALID_ARG;
+    const hexk::LinearArgs a{x, w, bias, res, y, z, M, N, K, act, ldx, res != nullptr ? ldres : 0,
+                             ldy};
+    hipError_t e = hipSuccess;
+    hexk::linear_fwd(a, ws, true, static_cast<Dtype>(dt), static_cast<hipStream_t>(stream), e);
+    return launched(e);
+}
+
+size_t hexlinear_bwd_workspace(int M, int N, int K, int64_t ldx, int64_t lddy, hex_act act,
+                               hex_dtype dt)
+{
+    if (check_linear(M, N, K, dt) != HEX_OK || strides_ok({ldx}, K) != HEX_OK ||
+        strides_ok({lddy}, N) != HEX_OK || !act_ok(act) || M == 0)
+        return 0;
+    hexk::LinearArgs a{};
+    a.M = M, a.N = N, a.K = K, a.ldx = ldx, a.act = act;
+    hexk::LinearGrads g{};
+    g.lddy = lddy;
+    hipError_t e = hipSuccess;
+    return hexk::linear_bwd(a, g, nullptr, false, static_cast<Dtype>(dt), nullptr, e);
+}
+
+int hexlinear_bwd(const void *x, const void *w, const void *z, const void *dy, void *dx, void *dw,
+                  void *db, void *ws, size_t ws_bytes, int M, int N, int K, int64_t ldx,
+                  int64_t lddy, int64_t lddx, hex_act act, hex_dtype dwt, hex_dtype dt,
+                  void *stream)
+{
+    int rc = check_linear(M, N, K, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!act_ok(act) || (dwt != HEX_F32 && dwt != dt))
+        return HEX_ERR_INVALID_ARG;
+    if ((rc = strides_ok({ldx}, K)) != HEX_OK || (rc = strides_ok({lddy}, N)) != HEX_OK ||
+        (dx != nullptr && (rc = strides_ok({lddx}, K)) != HEX_OK))
+        return rc;
+    if ((rc = ptrs_ok({}, {x, w, z, dy, dx, dw, db, ws})) != HEX_OK)
+        return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Dtype d = static_cast<Dtype>(dt), o = static_cast<Dtype>(dwt);
+    hipError_t e = hipSuccess;
+    if (M == 0) {
+        e = hexk::zero_fill(dw, static_cast<int64_t>(N) * K, o, st);
+        return launched(e != hipSuccess ? e : hexk::zero_fill(db, N, o, st));
+    }
+    if (dx == nullptr && dw == nullptr && db == nullptr)
+        return HEX_OK;
+    if (dy == nullptr || (act != HEX_ACT_NONE && z == nullptr) ||
+        (dx != nullptr && w == nullptr) || (dw != nullptr && x == nullptr) ||
+        !ws_ok(ws, ws_bytes, hexlinear_bwd_workspace(M, N, K, ldx, lddy, act, dt)))
+        return HEX_ERR_INVALID_ARG;
+    hexk::LinearArgs a{};
+    a.x = x, a.w = w, a.z = const_cast<void *>(act == HEX_ACT_NONE ? nullptr : z);
+    a.M = M, a.N = N, a.K = K, a.act = act, a.ldx = ldx;
+    const hexk::LinearGrads g{dy, dx, dw, db, lddy, lddx, o};
+    hexk::linear_bwd(a, g, ws, true, d, st, e);
+    return launched(e);
+}
+
+int hexffn_width(int F)
+{
+    if (F < 1)
+        return HEX_ERR_INVALID_ARG;
+    return F > HEX_LINEAR_MAX_DIM ? HEX_ERR_UNSUPPORTED : (F + 7) / 8 * 8;
+}
+
+size_t hexffn_fwd_workspace(int M, int K, int F, int N, int64_t ldx, hex_dtype dt)
+{
+    if (check_ffn(M, K, F, N, dt) != HEX_OK || strides_ok({ldx}, K) != HEX_OK || M == 0)
+        return 0;
+    hexk::FfnArgs a{};
+    a.M = M, a.K = K, a.F = F, a.N = N, a.ldx = ldx;
+    hipError_t e = hipSuccess;
+    return hexk::ffn_fwd(a, nullptr, false, static_cast<Dtype>(dt), nullptr, e);
+}
+
+int hexffn_fwd(const void *x, const void *w1, const void *b1, const void *w2, const void *b2,
+               const void *res, void *y, void *gu, void *h, void *ws, size_t ws_bytes, int M, int K,
+               int F, int N, int64_t ldx, int64_t ldres, int64_t ldy, hex_act act, hex_dtype dt,
+               void *stream)
+{
+    int rc = check_ffn(M, K, F, N, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!act_ok(act))
+        return HEX_ERR_INVALID_ARG;
+    if ((rc = strides_ok({ldx}, K)) != HEX_OK || (rc = strides_ok({ldy}, N)) != HEX_OK ||
+        (res != nullptr && (rc = strides_ok({ldres}, N)) != HEX_OK))
+        return rc;
+    if (M == 0)
+        return HEX_OK;
+    if ((rc = ptrs_ok({x, w1, w2, y, h}, {b1, b2, res, gu, ws})) != HEX_OK)
+        return rc;
+    if (!ws_ok(ws, ws_bytes, hexffn_fwd_workspace(M, K, F, N, ldx, dt)))
+        return HEX_ERR_INVALID_ARG;
+    const hexk::FfnArgs a{x, w1, b1, w2, b2, res, y, gu, h, M, K, F, N, act, ldx,
+                          res != nullptr ? ldres : 0, ldy};
+    hipError_t e = hipSuccess;
+    hexk::ffn_fwd(a, ws, true, static_cast<Dtype>(dt), static_cast<hipStream_t>(stream), e);
+    return launched(e);
+}
+
+size_t hexffn_bwd_workspace(int M, int K, int F, int N, int64_t ldx, int64_t lddy, hex_dtype dt)
+{
+    if (check_ffn(M, K, F, N, dt) != HEX_OK || strides_ok({ldx}, K) != HEX_OK ||
+        strides_ok({lddy}, N) != HEX_OK || M == 0)
+        return 0;
+    hexk::FfnArgs a{};
+    a.M = M, a.K = K, a.F = F, a.N = N, a.ldx = ldx;
+    hexk::FfnGrads g{};
+    g.lddy = lddy;
+    hipError_t e = hipSuccess;
+    return hexk::ffn_bwd(a, g, nullptr, false, static_cast<Dtype>(dt), nullptr, e);
+}
+
+int hexffn_bwd(const void *x, const void *w1, const void *w2, const void *gu, const void *h,
+               const void *dy, void *dx, void *dw1, void *db1, void *dw2, void *db2, void *ws,
+               size_t ws_bytes, int M, int K, int F, int N, int64_t ldx, int64_t lddy, int64_t lddx,
+               hex_act act, hex_dtype dwt, hex_dtype dt, void *stream)
+{
+    int rc = check_ffn(M, K, F, N, dt);
+    if (rc != HEX_OK)
+        return rc;
+    if (!act_ok(act) || (dwt != HEX_F32 && dwt != dt))
+        return HEX_ERR_INVALID_ARG;
+    if ((rc = strides_ok({ldx}, K)) != HEX_OK || (rc = strides_ok({lddy}, N)) != HEX_OK ||
+        (dx != nullptr && (rc = strides_ok({lddx}, K)) != HEX_OK))
+        return rc;
+    if ((rc = ptrs_ok({}, {x, w1, w2, gu, h, dy, dx, dw1, db1, dw2, db2, ws})) != HEX_OK)
+        return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Dtype d = static_cast<Dtype>(dt), o = static_cast<Dtype>(dwt);
+    hipError_t e = hipSuccess;
+    const bool inner = dx != nullptr || dw1 != nullptr || db1 != nullptr;
+    if (M == 0) {
+        const int64_t f = F;
+        if ((e = hexk::zero_fill(dw1, 2 * f * K, o, st)) == hipSuccess &&
+            (e = hexk::zero_fill(db1, 2 * f, o, st)) == hipSuccess &&
+            (e = hexk::zero_fill(dw2, f * N, o, st)) == hipSuccess)
+            e = hexk::zero_fill(db2, N, o, st);
+        return launched(e);
+    }
+    if (!inner && dw2 == nullptr && db2 == nullptr)
+        return HEX_OK;
+    if (dy == nullptr || (inner && (w2 == nullptr || gu == nullptr)) ||
+        (dx != nullptr && w1 == nullptr) || (dw1 != nullptr && x == nullptr) ||
+        (dw2 != nullptr && h == nullptr) ||
+        !ws_ok(ws, ws_bytes, hexffn_bwd_workspace(M, K, F, N, ldx, lddy, dt)))
+        return HEX_ERR_INVALID_ARG;
+    hexk::FfnArgs a{};
+    a.x = x, a.w1 = w1, a.w2 = w2, a.gu = const_cast<void *>(gu), a.h = const_cast<void *>(h);
+    a.M = M, a.K = K, a.F = F, a.N = N, a.act = act, a.ldx = ldx;
+    const hexk::FfnGrads g{dy, dx, dw1, db1, dw2, db2, lddy, lddx, o};
+    hexk::ffn_bwd(a, g, ws, true, d, st, e);
+    return launched(e);
 }
 
 int hexconv_timing_begin(void)

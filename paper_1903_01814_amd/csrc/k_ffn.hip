@@ -1,0 +1,237 @@
+// k_ffn.hip -- the gated feed-forward block and its gradients.
+//
+//   g = x wg^T + bg,  u = x wu^T + bu,  h = act(g) u,  y = h w2^T + b2 + res
+//   dh = dy w2,  dg = dh u act'(g),  du = dh act(g)
+//   dx = [dg du] [wg; wu],  dw1 = [dg du]^T x,  dw2 = dy^T h
+//
+// Both projections are one product whose waves hold a column of the gate and of
+// its partner in the same lane, so h is made in its epilogue; dg and du are made
+// in the epilogue of dh's product, and dh never reaches memory.  bfloat16 calls
+// round g, u (as kept for the backward), h, dg and du once to bfloat16, as
+// operands of the products that follow; h itself is made of unrounded g and u.
+#include "gemm.h"
+#include "tokens.h"
+
+namespace hexk {
+namespace {
+
+using gemm::Plan;
+using gemm::Side;
+
+// g + bg, u + bu to gu (nullable), h = act(g) u; zeros in the columns F .. Fp - 1
+template <typename E, int ACT> struct GatedEpi {
+    const E *bias; // bg, then bu
+    E *gu, *h;
+    int64_t Fp;
+    int F;
+    struct Cols {
+        float g[8], u[8];
+    };
+    struct Fetched {};
+    __device__ __forceinline__ Cols cols(int f) const
+    {
+        Cols c = {};
+        if (bias != nullptr) {
+            row8<E, false>(bias + f, F - f, c.g);
+            row8<E, false>(bias + F + f, F - f, c.u);
+        }
+        return c;
+    }
+    __device__ __forceinline__ Fetched fetch(int, int) const { return Fetched{}; }
+    __device__ __forceinline__ void done(int m, int f, float (&g)[8], float (&u)[8],
+                                         const Cols &c) const
+    {
+        constexpr bool FINE = sizeof(E) == 4;
+        const int k = F - f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            g[i] += c.g[i];
+            u[i] += c.u[i];
+        }
+        if (k < 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                g[i] = i < k ? g[i] : 0.f;
+                u[i] = i < k ? u[i] : 0.f;
+            }
+        if (gu != nullptr) {
+            E *p = gu + static_cast<int64_t>(m) * 2 * Fp + f;
+            save_row8<E, true>(p, 8, g);
+            save_row8<E, true>(p + Fp, 8, u);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            g[i] = activate<FINE>(g[i], ACT) * u[i];
+        if (k < 8) // act(0) u = 0 but for the sign
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                g[i] = i < k ? g[i] : 0.f;
+        save_row8<E, true>(h + static_cast<int64_t>(m) * Fp + f, 8, g);
+    }
+};
+
+// dg and du from dh, in bfloat16 or in three planes; in the columns F .. Fp - 1
+// dh, g and u are zeros, so dg and du are
+template <typename E, int ACT> struct GatedGradEpi {
+    const E *gu;
+    bf16raw *d;
+    int64_t Fp, plane;
+    struct Nothing {};
+    struct Fetched {
+        float g[8], u[8];
+    };
+    __device__ __forceinline__ Nothing cols(int) const { return Nothing{}; }
+    __device__ __forceinline__ Fetched fetch(int m, int f) const
+    {
+        Fetched x;
+        const E *p = gu + static_cast<int64_t>(m) * 2 * Fp + f;
+        row8<E, true>(p, 8, x.g);
+        row8<E, true>(p + Fp, 8, x.u);
+        return x;
+    }
+    __device__ __forceinline__ void done(int m, int f, float (&dh)[8], Nothing,
+                                         const Fetched &x) const
+    {
+        constexpr bool FINE = sizeof(E) == 4;
+        const int64_t at = static_cast<int64_t>(m) * 2 * Fp + f;
+        float dg[8], du[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float a;
+            const float s = derivative<FINE>(x.g[i], ACT, a);
+            dg[i] = dh[i] * x.u[i] * s;
+            du[i] = dh[i] * a;
+        }
+        if constexpr (FINE) {
+            save_planes(d + at, plane, dg);
+            save_planes(d + at + Fp, plane, du);
+        } else {
+            save_row8<bf16raw, true>(d + at, 8, dg);
+            save_row8<bf16raw, true>(d + at + Fp, 8, du);
+        }
+    }
+};
+
+template <typename E, int ACT>
+hipError_t gated_product(const Plan &pl, const Side &W, const Side &X, float *ws, const FfnArgs &a,
+                         int64_t Fp, hipStream_t st)
+{
+    return gemm::launch<false, false, true>(
+        pl, W, X, static_cast<int>(Fp), ws,
+        GatedEpi<E, ACT>{static_cast<const E *>(a.b1), static_cast<E *>(a.gu),
+                         static_cast<E *>(a.h), Fp, a.F},
+        st);
+}
+
+template <typename E, int ACT>
+hipError_t gated_grad(const Plan &pl, const Side &W2, const Side &DY, float *ws, const void *gu,
+                      bf16raw *d, int64_t Fp, int64_t plane, hipStream_t st)
+{
+    return gemm::launch<true, false, false>(
+        pl, W2, DY, 0, ws, GatedGradEpi<E, ACT>{static_cast<const E *>(gu), d, Fp, plane}, st);
+}
+
+// f<E, ACT>(args) for the type and the activation
+#define HEX_BY_ACT(f, E, ...)                                                                 \
+    (act == ACT_RELU   ? f<E, ACT_RELU>(__VA_ARGS__)                                          \
+     : act == ACT_GELU ? f<E, ACT_GELU>(__VA_ARGS__)                                          \
+     : act == ACT_SILU ? f<E, ACT_SILU>(__VA_ARGS__)                                          \
+                       : f<E, ACT_NONE>(__VA_ARGS__))
+#define HEX_BY_TYPE(f, ...)                                                                   \
+    (dt == F32 ? HEX_BY_ACT(f, float, __VA_ARGS__) : HEX_BY_ACT(f, bf16raw, __VA_ARGS__))
+
+} // namespace
+
+size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err)
+{
+    const int planes = dt == F32 ? 3 : 1;
+    const int64_t Fp = round8(a.F);
+    const Halves none{0, 0}, halves{a.F, static_cast<int>(Fp)};
+    Space sp{static_cast<char *>(ws)};
+    PackJobs jobs{}, late{};
+    const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, none, sp, jobs);
+    const Side W1 = operand(a.w1, nullptr, 0, 2 * a.F, a.K, a.K, dt, halves, sp, jobs);
+    const Side W2 = operand(a.w2, nullptr, 0, a.N, a.F, a.F, dt, none, sp, jobs);
+    const Side H = operand(a.h, nullptr, 0, a.M, static_cast<int>(Fp), Fp, dt, none, sp, late);
+    const Plan p1 = gemm::make_plan(a.M, a.F, a.K, true, planes);
+    const Plan p2 = gemm::make_plan(a.M, a.N, a.F, false, planes);
+    const size_t b1 = gemm::part_bytes(p1, true), b2 = gemm::part_bytes(p2, false);
+    float *part = sp.take<float>((b1 > b2 ? b1 : b2) / 4);
+    if (!run)
+        return sp.used;
+    if ((err = pack(jobs, dt, st)) != hipSuccess)
+        return sp.used;
+    const int act = a.act;
+    err = HEX_BY_TYPE(gated_product, p1, W1, X, part, a, Fp, st);
+    if (err == hipSuccess && (err = pack(late, dt, st)) == hipSuccess)
+        err = linear_product(p2, W2, H, part, a.b2, a.res, a.y, nullptr, a.ldr, a.ldy, ACT_NONE, dt,
+                             st);
+    return sp.used;
+}
+
+size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt, hipStream_t st,
+               hipError_t &err)
+{
+    const int planes = dt == F32 ? 3 : 1;
+    const int64_t Fp = round8(a.F);
+    const int W = static_cast<int>(2 * Fp);
+    const Halves none{0, 0}, halves{a.F, static_cast<int>(Fp)};
+    Space sp{static_cast<char *>(ws)};
+    PackJobs dyj{}, w2j{}, w1j{}, xj{}, hj{};
+    const Side DY = operand(g.dy, nullptr, 0, a.M, a.N, g.lddy, dt, none, sp, dyj);
+    const Side W2 = operand(a.w2, nullptr, 0, a.N, a.F, a.F, dt, none, sp, w2j);
+    const Side W1 = operand(a.w1, nullptr, 0, 2 * a.F, a.K, a.K, dt, halves, sp, w1j);
+    const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, none, sp, xj);
+    const Side H = operand(a.h, nullptr, 0, a.M, static_cast<int>(Fp), Fp, dt, none, sp, hj);
+    const int64_t plane = static_cast<int64_t>(a.M) * W;
+    bf16raw *d = sp.take<bf16raw>(planes * plane);
+    const Side D{d, W, plane, a.M};
+    const Plan ph = gemm::make_plan(a.M, a.F, a.N, false, planes);
+    const Plan px = gemm::make_plan(a.M, a.K, W, false, planes);
+    const Plan p1 = gemm::make_plan(W, a.K, a.M, false, planes);
+    const Plan p2 = gemm::make_plan(a.N, a.F, a.M, false, planes);
+    size_t most = 0;
+    for (const Plan *p : {&ph, &px, &p1, &p2})
+        most = gemm::part_bytes(*p, false) > most ? gemm::part_bytes(*p, false) : most;
+    float *part = sp.take<float>(most / 4);
+    const int64_t sums1 = static_cast<int64_t>(col_sum_slices(a.M, W)) * W;
+    const int64_t sums2 = static_cast<int64_t>(col_sum_slices(a.M, a.N)) * a.N;
+    float *sums = sp.take<float>(sums1 > sums2 ? sums1 : sums2);
+    if (!run)
+        return sp.used;
+    // dg and du are needed for all but dw2 and db2
+    const bool inner = g.dx != nullptr || g.dw1 != nullptr || g.db1 != nullptr;
+    PackJobs jobs{}, more{};
+    auto add = [](PackJobs &to, const PackJobs &j, bool wanted) {
+        if (wanted && j.n > 0)
+            to.job[to.n++] = j.job[0];
+    };
+    add(jobs, dyj, inner || g.dw2 != nullptr);
+    add(jobs, w2j, inner);
+    add(jobs, w1j, g.dx != nullptr);
+    add(jobs, xj, g.dw1 != nullptr);
+    add(more, hj, g.dw2 != nullptr);
+    if ((err = pack(jobs, dt, st)) != hipSuccess || (err = pack(more, dt, st)) != hipSuccess)
+        return sp.used;
+    const int act = a.act;
+    if (inner && (err = HEX_BY_TYPE(gated_grad, ph, tall(W2, a.F), DY, part, a.gu, d, Fp, plane,
+                                    st)) != hipSuccess)
+        return sp.used;
+    if (g.dx != nullptr && (err = store_product(false, px, tall(W1, a.K), D, part, g.dx, g.lddx,
+                                                none, dt, st)) != hipSuccess)
+        return sp.used;
+    if (g.dw1 != nullptr && (err = store_product(true, p1, tall(X, a.K), tall(D, W), part, g.dw1,
+                                                 a.K, halves, g.dwt, st)) != hipSuccess)
+        return sp.used;
+    if (g.dw2 != nullptr && (err = store_product(true, p2, tall(H, a.F), tall(DY, a.N), part,
+                                                 g.dw2, a.F, none, g.dwt, st)) != hipSuccess)
+        return sp.used;
+    if (g.db1 != nullptr && (err = col_sum(d, W, plane, planes, a.M, W, halves, sums, g.db1, BF16,
+                                           g.dwt, st)) != hipSuccess)
+        return sp.used;
+    if (g.db2 != nullptr)
+        err = col_sum(g.dy, g.lddy, 0, 1, a.M, a.N, none, sums, g.db2, dt, g.dwt, st);
+    return sp.used;
+}
+
+} // namespace hexk

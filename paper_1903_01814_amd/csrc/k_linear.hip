@@ -1,0 +1,292 @@
+// k_linear.hip -- projections: y = act(x w^T + b) + res, and their gradients.
+//
+//   z = x w^T + b,  y = act(z) + res
+//   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum over rows of dz
+//
+// Matrix products of gemm.h with their epilogues; what bounds them stands there.
+// bfloat16 calls round z (where it is kept) and dz once to bfloat16, as operands
+// of the products that follow; sums are float32.
+#include "gemm.h"
+#include "tokens.h"
+
+namespace hexk {
+namespace {
+
+using gemm::Plan;
+using gemm::Side;
+
+struct Nothing {};
+
+// y = act(v + bias) + res, z = v + bias
+template <typename E, int ACT> struct LinearEpi {
+    const E *bias, *res;
+    E *y, *z;
+    int64_t ldr, ldy;
+    int N;
+    bool vec; // N, ldr and ldy whole vectors
+    struct Cols {
+        float b[8];
+    };
+    struct Fetched {
+        float r[8];
+    };
+    __device__ __forceinline__ Cols cols(int n) const
+    {
+        Cols c = {};
+        if (bias != nullptr)
+            row8<E, true>(bias + n, N - n, c.b);
+        return c;
+    }
+    __device__ __forceinline__ Fetched fetch(int m, int n) const
+    {
+        Fetched f = {};
+        if (res == nullptr)
+            return f;
+        if (vec)
+            row8<E, true>(res + m * ldr + n, 8, f.r);
+        else
+            row8<E, false>(res + m * ldr + n, N - n, f.r);
+        return f;
+    }
+    __device__ __forceinline__ void done(int m, int n, float (&v)[8], const Cols &c,
+                                         const Fetched &f) const
+    {
+        E *pz = z + static_cast<int64_t>(m) * N + n, *py = y + m * ldy + n;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] += c.b[i];
+        if (z != nullptr) {
+            if (vec)
+                save_row8<E, true>(pz, 8, v);
+            else
+                save_row8<E, false>(pz, N - n, v);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = activate<sizeof(E) == 4>(v[i], ACT) + f.r[i];
+        if (vec)
+            save_row8<E, true>(py, 8, v);
+        else
+            save_row8<E, false>(py, N - n, v);
+    }
+};
+
+// Whether a tensor of rows of n elements, ld apart, is an operand as it is
+// (bfloat16, whole vectors); others are packed.
+bool ready(int64_t n, int64_t ld, Dtype dt) { return dt == BF16 && n % 8 == 0 && ld % 8 == 0; }
+
+} // namespace
+
+// The operand of a tensor [rows][cols]: itself, or a place in the workspace and
+// the job that fills it.
+Side operand(const void *src, const void *z, int act, int rows, int cols, int64_t ld, Dtype dt,
+             Halves map, Space &ws, PackJobs &jobs)
+{
+    if (act == ACT_NONE && map.half == map.halfp && ready(cols, ld, dt))
+        return Side{static_cast<const bf16raw *>(src), ld, 0, rows};
+    const int planes = dt == F32 ? 3 : 1;
+    const int64_t dld = round8(cols), drows = map.half > 0 ? 2 * static_cast<int64_t>(map.halfp) : rows;
+    bf16raw *dst = ws.take<bf16raw>(planes * drows * dld);
+    PackJob &q = jobs.job[jobs.n++];
+    q = PackJob{src, z, dst, ld, dld, drows * dld, drows, rows, cols, map.half, map.halfp, act, 0};
+    return Side{dst, dld, drows * dld, static_cast<int>(drows)};
+}
+// the same tensor read along its rows of memory: its columns are the operand's
+Side tall(const Side &s, int cols)
+{
+    Side t = s;
+    t.rows = static_cast<int>(round8(cols));
+    return t;
+}
+
+namespace {
+
+// y = v in O; rows may skip those between two halves
+template <typename O> struct StoreEpi {
+    O *y;
+    int64_t ldy;
+    int N;
+    Halves map;
+    bool vec;
+    struct Fetched {};
+    __device__ __forceinline__ Nothing cols(int) const { return Nothing{}; }
+    __device__ __forceinline__ Fetched fetch(int, int) const { return Fetched{}; }
+    __device__ __forceinline__ void done(int m, int n, float (&v)[8], Nothing, Fetched) const
+    {
+        const int row = map.row(m);
+        if (row < 0)
+            return;
+        O *p = y + row * ldy + n;
+        if (vec)
+            save_row8<O, true>(p, 8, v);
+        else
+            save_row8<O, false>(p, N - n, v);
+    }
+};
+
+template <typename O>
+hipError_t store_as(bool tall_q, const Plan &pl, const Side &P, const Side &Q, float *ws, O *y,
+                         int64_t ldy, Halves map, hipStream_t st)
+{
+    const bool vec = pl.N % 8 == 0 && ldy % (16 / static_cast<int64_t>(sizeof(O))) == 0;
+    const StoreEpi<O> e{y, ldy, pl.N, map, vec};
+    return tall_q ? gemm::launch<true, true, false>(pl, P, Q, 0, ws, e, st)
+                  : gemm::launch<true, false, false>(pl, P, Q, 0, ws, e, st);
+}
+
+} // namespace
+
+// D = Q P stored as it is: Q wide (data gradient) or tall (weight gradient), P tall
+hipError_t store_product(bool tall_q, const Plan &pl, const Side &P, const Side &Q, float *ws,
+                         void *y, int64_t ldy, Halves map, Dtype dt, hipStream_t st)
+{
+    return dt == F32 ? store_as(tall_q, pl, P, Q, ws, static_cast<float *>(y), ldy, map, st)
+                     : store_as(tall_q, pl, P, Q, ws, static_cast<bf16raw *>(y), ldy, map, st);
+}
+
+namespace {
+
+template <typename E, int ACT>
+hipError_t product_of(const Plan &pl, const Side &W, const Side &X, float *ws, const void *bias,
+                      const void *res, void *y, void *z, int64_t ldr, int64_t ldy, hipStream_t st)
+{
+    constexpr int64_t per = 16 / sizeof(E);
+    const bool vec = pl.N % 8 == 0 && ldr % per == 0 && ldy % per == 0;
+    return gemm::launch<false, false, false>(
+        pl, W, X, 0, ws,
+        LinearEpi<E, ACT>{static_cast<const E *>(bias), static_cast<const E *>(res),
+                          static_cast<E *>(y), static_cast<E *>(z), ldr, ldy, pl.N, vec},
+        st);
+}
+
+} // namespace
+
+hipError_t linear_product(const Plan &pl, const Side &W, const Side &X, float *ws, const void *bias,
+                          const void *res, void *y, void *z, int64_t ldr, int64_t ldy, int act,
+                          Dtype dt, hipStream_t st)
+{
+#define HEX_PRODUCT(E, ACT) product_of<E, ACT>(pl, W, X, ws, bias, res, y, z, ldr, ldy, st)
+#define HEX_PRODUCTS(E)                                                                       \
+    (act == ACT_RELU   ? HEX_PRODUCT(E, ACT_RELU)                                             \
+     : act == ACT_GELU ? HEX_PRODUCT(E, ACT_GELU)                                             \
+     : act == ACT_SILU ? HEX_PRODUCT(E, ACT_SILU)                                             \
+                       : HEX_PRODUCT(E, ACT_NONE))
+    return dt == F32 ? HEX_PRODUCTS(float) : HEX_PRODUCTS(bf16raw);
+#undef HEX_PRODUCTS
+#undef HEX_PRODUCT
+}
+
+size_t linear_fwd(const LinearArgs &a, void *ws, bool run, Dtype dt, hipStream_t st,
+                  hipError_t &err)
+{
+    Space sp{static_cast<char *>(ws)};
+    PackJobs jobs{};
+    const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, Halves{0, 0}, sp, jobs);
+    const Side W = operand(a.w, nullptr, 0, a.N, a.K, a.K, dt, Halves{0, 0}, sp, jobs);
+    const Plan pl = gemm::make_plan(a.M, a.N, a.K, false, dt == F32 ? 3 : 1);
+    float *part = sp.take<float>(gemm::part_bytes(pl, false) / 4);
+    if (!run)
+        return sp.used;
+    if ((err = pack(jobs, dt, st)) == hipSuccess)
+        err = linear_product(pl, W, X, part, a.bias, a.res, a.y, a.z, a.ldr, a.ldy, a.act, dt, st);
+    return sp.used;
+}
+
+size_t linear_bwd(const LinearArgs &a, const LinearGrads &g, void *ws, bool run, Dtype dt,
+                  hipStream_t st, hipError_t &err)
+{
+    // all places are taken whatever is asked for, so that one size does
+    const int planes = dt == F32 ? 3 : 1;
+    const Halves none{0, 0};
+    Space sp{static_cast<char *>(ws)};
+    PackJobs dzj{}, xj{}, wj{};
+    const Side DZ = operand(g.dy, a.z, a.act, a.M, a.N, g.lddy, dt, none, sp, dzj);
+    const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, none, sp, xj);
+    const Side W = operand(a.w, nullptr, 0, a.N, a.K, a.K, dt, none, sp, wj);
+    const Plan px = gemm::make_plan(a.M, a.K, a.N, false, planes);
+    const Plan pw = gemm::make_plan(a.N, a.K, a.M, false, planes);
+    const size_t part = gemm::part_bytes(px, false), partw = gemm::part_bytes(pw, false);
+    float *parts = sp.take<float>((part > partw ? part : partw) / 4);
+    float *sums = sp.take<float>(static_cast<int64_t>(col_sum_slices(a.M, a.N)) * a.N);
+    if (!run)
+        return sp.used;
+    PackJobs jobs{};
+    for (const PackJobs *j : {&dzj, g.dw != nullptr ? &xj : nullptr, g.dx != nullptr ? &wj : nullptr})
+        if (j != nullptr && j->n > 0)
+            jobs.job[jobs.n++] = j->job[0];
+    if ((err = pack(jobs, dt, st)) != hipSuccess)
+        return sp.used;
+    if (g.dx != nullptr &&
+        (err = store_product(false, px, tall(W, a.K), DZ, parts, g.dx, g.lddx, none, dt, st)) !=
+            hipSuccess)
+        return sp.used;
+    if (g.dw != nullptr &&
+        (err = store_product(true, pw, tall(X, a.K), tall(DZ, a.N), parts, g.dw, a.K, none, g.dwt,
+                             st)) != hipSuccess)
+        return sp.used;
+    if (g.db != nullptr) {
+        if (dzj.n > 0)
+            err = col_sum(DZ.p, DZ.ld, DZ.plane, planes, a.M, a.N, none, sums, g.db, BF16, g.dwt, st);
+        else
+            err = col_sum(g.dy, g.lddy, 0, 1, a.M, a.N, none, sums, g.db, dt, g.dwt, st);
+    }
+    return sp.used;
+}
+
+namespace gemm {
+
+// The division with the least estimated time: rounds of the blocks that the card
+// holds at a time, each its steps, its start and its epilogue; a split adds its
+// sums' way through memory and a launch.
+Plan make_plan(int M, int N, int K, bool gated, int planes)
+{
+    struct Tile {
+        int rows, per_cu;
+        double full, alone, fixed; // us a step with all blocks of a unit at work, and with one
+    };
+    static constexpr Tile tiles[] = {{256, 1, 2.2, 2.2, 6.0}, {128, 2, 1.4, 0.8, 3.0}, {64, 4, 1.1, 0.4, 2.0}};
+    Plan best{};
+    double least = 0;
+    const int cus = device_cus();
+    for (const Tile &t : tiles) {
+        Plan p{};
+        p.M = M;
+        p.N = N;
+        p.K = K;
+        p.tile = t.rows;
+        const int cols = gated && t.rows > 64 ? t.rows / 2 : t.rows;
+        p.mt = static_cast<int>((static_cast<int64_t>(M) + t.rows - 1) / t.rows);
+        p.nt = (N + cols - 1) / cols;
+        p.kt = (K + 63) / 64;
+        p.steps = p.kt * (planes == 3 ? 6 : 1);
+        p.Np = (N + 7) / 8 * 8;
+        const int64_t blocks = static_cast<int64_t>(p.mt) * p.nt;
+        for (int want = 1; want <= 64 && want <= p.steps; want = want < 4 ? want + 1 : want * 3 / 2) {
+            const int per = (p.steps + want - 1) / want, splits = (p.steps + per - 1) / per;
+            const double bytes = 4.0 * splits * M * p.Np * (gated ? 2 : 1);
+            if (splits > 1 && (bytes > 256e6 || blocks * splits > 16 * cus))
+                break;
+            const double rounds_d = static_cast<double>(blocks * splits) / (static_cast<double>(cus) * t.per_cu);
+            const double whole = static_cast<double>((blocks * splits + static_cast<int64_t>(cus) * t.per_cu - 1) / (static_cast<int64_t>(cus) * t.per_cu));
+            const double step = rounds_d <= 1.0 / t.per_cu ? t.alone : t.full;
+            double us = whole * (per * step + t.fixed);
+            if (splits > 1)
+                us += 5.0 + 2 * bytes / 4e6;
+            if (best.tile == 0 || us < least) {
+                least = us;
+                best = p;
+                best.per = per;
+                best.splits = splits;
+            }
+        }
+    }
+    return best;
+}
+
+size_t part_bytes(const Plan &p, bool gated)
+{
+    return p.splits > 1 ? static_cast<size_t>(p.splits) * p.M * p.Np * (gated ? 2 : 1) * 4 : 0;
+}
+
+} // namespace gemm
+} // namespace hexk

@@ -329,4 +329,63 @@ hipError_t rotary_zero(float *dwq, float *dwk, int D, hipStream_t st);
 hipError_t dropout(const void *x, const void *res, void *y, int64_t n, double p,
                    const uint64_t *rng, uint64_t call, Dtype dt, hipStream_t st);
 
+// ---- layer norm -----------------------------------------------------------
+// Row strides in elements; ldy: of y, in the backward of dy.  inv = 1 / C.
+struct NormArgs {
+    int64_t T, ldx, ldy, ldr, lddx;
+    int C;
+    float inv, eps;
+};
+hipError_t norm_fwd(const void *x, const void *w, const void *b, void *y, float *mean, float *rstd,
+                    const NormArgs &a, Dtype dt, hipStream_t st);
+// ws: norm_bwd_blocks(T, C) * 2 C floats
+int norm_bwd_blocks(int64_t T, int C);
+hipError_t norm_bwd(const void *x, const void *w, const float *mean, const float *rstd,
+                    const void *dy, const void *res, void *dx, float *dw, float *db, void *ws,
+                    const NormArgs &a, Dtype dt, hipStream_t st);
+hipError_t norm_zero(float *dw, float *db, int C, hipStream_t st);
+
+// ---- projections ----------------------------------------------------------
+enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+// y [M][N] = act(x [M][K] w [N][K]^T + bias) + res, z what the activation takes
+struct LinearArgs {
+    const void *x, *w, *bias, *res;
+    void *y, *z;
+    int M, N, K, act;
+    int64_t ldx, ldr, ldy;
+};
+struct LinearGrads {
+    const void *dy;
+    void *dx, *dw, *db; // dw and db in dwt
+    int64_t lddy, lddx;
+    Dtype dwt;
+};
+// Bytes of workspace that the call takes; with `run` also the call.
+size_t linear_fwd(const LinearArgs &a, void *ws, bool run, Dtype dt, hipStream_t st,
+                  hipError_t &err);
+size_t linear_bwd(const LinearArgs &a, const LinearGrads &g, void *ws, bool run, Dtype dt,
+                  hipStream_t st, hipError_t &err);
+// p[0 .. n - 1] := 0
+hipError_t zero_fill(void *p, int64_t n, Dtype dt, hipStream_t st);
+
+// ---- gated feed-forward ---------------------------------------------------
+// h = act(x wg^T + bg) (x wu^T + bu), y = h w2^T + b2 + res; w1 = wg over wu.
+// gu [M][2 Fp] and h [M][Fp] with Fp = F rounded up to 8.
+struct FfnArgs {
+    const void *x, *w1, *b1, *w2, *b2, *res;
+    void *y, *gu, *h;
+    int M, K, F, N, act;
+    int64_t ldx, ldr, ldy;
+};
+struct FfnGrads {
+    const void *dy;
+    void *dx, *dw1, *db1, *dw2, *db2;
+    int64_t lddy, lddx;
+    Dtype dwt;
+};
+size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err);
+size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt, hipStream_t st,
+               hipError_t &err);
+
 } // namespace hexk

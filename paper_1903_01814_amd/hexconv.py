@@ -31,6 +31,12 @@ HEX_ATTN_CAUSAL = 1
 HEX_ROTARY_NORM = 1
 HEX_ATTN_MAX_DIM = 128
 HEX_ROTARY_MAX_AXES = 8
+HEX_NORM_MAX_DIM = 16384
+HEX_LINEAR_MAX_DIM = 1 << 20
+HEX_ACT_NONE = 0
+HEX_ACT_RELU = 1
+HEX_ACT_GELU = 2
+HEX_ACT_SILU = 3
 
 # (name, argtypes, restype) of every exported symbol
 _P = ctypes.c_void_p
@@ -73,6 +79,18 @@ SIGNATURES = {
     "hexattn_step_workspace": ([_I] * 7, _S),
     "hexattn_step": ([_P] * 5 + [_S] + [_P] * 2 + [_I] * 7 + [_L] * 2 + [_F, _I, _P], _I),
     "hexdropout": ([_P] * 3 + [_L, ctypes.c_double, _P, ctypes.c_uint64, _I, _P], _I),
+    "hexnorm_fwd": ([_P] * 6 + [_I] * 2 + [_L] * 2 + [_F, _I, _P], _I),
+    "hexnorm_bwd_workspace": ([_I] * 3, _S),
+    "hexnorm_bwd": ([_P] * 10 + [_S] + [_I] * 2 + [_L] * 4 + [_I, _P], _I),
+    "hexlinear_fwd_workspace": ([_I] * 3 + [_L, _I], _S),
+    "hexlinear_fwd": ([_P] * 7 + [_S] + [_I] * 3 + [_L] * 3 + [_I, _I, _P], _I),
+    "hexlinear_bwd_workspace": ([_I] * 3 + [_L] * 2 + [_I] * 2, _S),
+    "hexlinear_bwd": ([_P] * 8 + [_S] + [_I] * 3 + [_L] * 3 + [_I] * 3 + [_P], _I),
+    "hexffn_width": ([_I], _I),
+    "hexffn_fwd_workspace": ([_I] * 4 + [_L, _I], _S),
+    "hexffn_fwd": ([_P] * 10 + [_S] + [_I] * 4 + [_L] * 3 + [_I, _I, _P], _I),
+    "hexffn_bwd_workspace": ([_I] * 4 + [_L] * 2 + [_I], _S),
+    "hexffn_bwd": ([_P] * 12 + [_S] + [_I] * 4 + [_L] * 3 + [_I] * 3 + [_P], _I),
     "hexconv_timing_begin": ([], _I),
     "hexconv_timing_end": ([_I, ctypes.c_char_p, _IP, ctypes.POINTER(ctypes.c_double), _IP],
                            _I),
@@ -667,3 +685,159 @@ def hexdropout(x, res, y, p: float, rng, call: int = 0, stream=None):
                            _array(rng, "rng", rng.dtype, (2,)), call, dt, _stream(stream))
     _ok("hexdropout", rc)
     return y
+
+
+# --------------------------------------- operators on tokens by themselves
+
+def _rows(t, name, dtype, n, cols):
+    """Pointer and row stride of [n][cols] with dense rows; None passes through."""
+    if t is None:
+        return None, cols
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype or not t.is_cuda or len(shape) != 2 or shape != (n, cols):
+        _refuse(t, name, dtype, (n, cols))
+    if cols > 1 and stride[1] != 1 and n > 0:
+        raise ValueError("hexconv: the rows of %s must be dense" % name)
+    # one row, or none: any stride does
+    return t.data_ptr(), stride[0] if n > 1 else cols
+
+
+def _grad_dtype(ty, grads):
+    """The one type of the weights' gradients that are given, float32 or ty."""
+    torch = _torch()
+    got = [t.dtype for t in grads if t is not None] or [torch.float32]
+    if any(t is not got[0] for t in got) or (got[0] is not torch.float32 and got[0] is not ty):
+        raise TypeError("hexconv: the gradients of weights must be all float32 or all %s" % ty)
+    return got[0]
+
+
+def hexnorm_fwd(x, w, b, y, mean=None, rstd=None, eps: float = 1e-5, stream=None):
+    """y (and mean, rstd, float32 [T]) <- layer norm of the rows of x [T][C],
+    weights w and b [C] (each may be None)."""
+    T, C = x.shape
+    dt, ty, f32 = _dtype_code(x), x.dtype, _torch().float32
+    px, ldx = _rows(x, "x", ty, T, C)
+    py, ldy = _rows(y, "y", ty, T, C)
+    rc = load().hexnorm_fwd(px, _array(w, "w", ty, (C,)), _array(b, "b", ty, (C,)), py,
+                            _array(mean, "mean", f32, (T,)), _array(rstd, "rstd", f32, (T,)), T, C,
+                            ldx, ldy, eps, dt, _stream(stream))
+    _ok("hexnorm_fwd", rc)
+    return y
+
+
+def hexnorm_bwd_workspace(T, C, dt):
+    return load().hexnorm_bwd_workspace(T, C, dt)
+
+
+def hexnorm_bwd(x, w, mean, rstd, dy, res, dx, dw, db, ws, stream=None):
+    """dx and the float32 dw, db [C] (each may be None) <- gradients of
+    hexnorm_fwd; res (may be None): added to dx."""
+    T, C = x.shape
+    dt, ty, f32 = _dtype_code(x), x.dtype, _torch().float32
+    px, ldx = _rows(x, "x", ty, T, C)
+    pg, ldg = _rows(dy, "dy", ty, T, C)
+    pr, ldr = _rows(res, "res", ty, T, C)
+    pd, ldd = _rows(dx, "dx", ty, T, C)
+    rc = load().hexnorm_bwd(px, _array(w, "w", ty, (C,)), _array(mean, "mean", f32, (T,)),
+                            _array(rstd, "rstd", f32, (T,)), pg, pr, pd,
+                            _array(dw, "dw", f32, (C,)), _array(db, "db", f32, (C,)), *_ws(ws), T, C,
+                            ldx, ldg, ldr, ldd, dt, _stream(stream))
+    _ok("hexnorm_bwd", rc)
+    return dx, dw, db
+
+
+def hexlinear_fwd_workspace(M, N, K, ldx, dt):
+    return load().hexlinear_fwd_workspace(M, N, K, ldx, dt)
+
+
+def hexlinear_fwd(x, w, bias, res, y, z=None, ws=None, act: int = HEX_ACT_NONE, stream=None):
+    """y <- act(z) + res with z = x w^T + bias, x [M][K] and w [N][K]; bias,
+    res and z (which receives it) may be None."""
+    M, K = x.shape
+    N = w.shape[0]
+    dt, ty = _dtype_code(x), x.dtype
+    px, ldx = _rows(x, "x", ty, M, K)
+    pr, ldr = _rows(res, "res", ty, M, N)
+    py, ldy = _rows(y, "y", ty, M, N)
+    rc = load().hexlinear_fwd(px, _array(w, "w", ty, (N, K)), _array(bias, "bias", ty, (N,)), pr,
+                              py, _array(z, "z", ty, (M, N)), *_ws(ws), M, N, K, ldx, ldr, ldy, act,
+                              dt, _stream(stream))
+    _ok("hexlinear_fwd", rc)
+    return y
+
+
+def hexlinear_bwd_workspace(M, N, K, ldx, lddy, act, dt):
+    return load().hexlinear_bwd_workspace(M, N, K, ldx, lddy, act, dt)
+
+
+def hexlinear_bwd(x, w, z, dy, dx, dw, db, ws, act: int = HEX_ACT_NONE, stream=None):
+    """dx, dw and db (each may be None; dw and db float32 or of x's type) <-
+    gradients of hexlinear_fwd; z for an activation only."""
+    M, K = x.shape
+    N = dy.shape[1]
+    dt, ty = _dtype_code(x), x.dtype
+    gt = _grad_dtype(ty, (dw, db))
+    px, ldx = _rows(x, "x", ty, M, K)
+    pg, ldg = _rows(dy, "dy", ty, M, N)
+    pd, ldd = _rows(dx, "dx", ty, M, K)
+    rc = load().hexlinear_bwd(px, _array(w, "w", ty, (N, K)), _array(z, "z", ty, (M, N)), pg, pd,
+                              _array(dw, "dw", gt, (N, K)), _array(db, "db", gt, (N,)), *_ws(ws), M,
+                              N, K, ldx, ldg, ldd, act, dt if gt is ty else HEX_F32, dt,
+                              _stream(stream))
+    _ok("hexlinear_bwd", rc)
+    return dx, dw, db
+
+
+def hexffn_width(F: int) -> int:
+    """Columns of h for F hidden features (gu has twice as many)."""
+    rc = load().hexffn_width(F)
+    if rc < 0:
+        raise HexError("hexffn_width", rc)
+    return rc
+
+
+def hexffn_fwd_workspace(M, K, F, N, ldx, dt):
+    return load().hexffn_fwd_workspace(M, K, F, N, ldx, dt)
+
+
+def hexffn_fwd(x, w1, b1, w2, b2, res, y, gu, h, ws=None, act: int = HEX_ACT_SILU, stream=None):
+    """y <- h w2^T + b2 + res, h = act(x w1[:F]^T + b1[:F]) (x w1[F:]^T + b1[F:]);
+    x [M][K], w1 [2F][K], w2 [N][F]; b1, b2, res and gu may be None.  h
+    [M][hexffn_width(F)] and gu [M][2 hexffn_width(F)] are for the backward."""
+    M, K = x.shape
+    N, F = w2.shape
+    dt, ty, Fp = _dtype_code(x), x.dtype, hexffn_width(F)
+    px, ldx = _rows(x, "x", ty, M, K)
+    pr, ldr = _rows(res, "res", ty, M, N)
+    py, ldy = _rows(y, "y", ty, M, N)
+    rc = load().hexffn_fwd(px, _array(w1, "w1", ty, (2 * F, K)), _array(b1, "b1", ty, (2 * F,)),
+                           _array(w2, "w2", ty, (N, F)), _array(b2, "b2", ty, (N,)), pr, py,
+                           _array(gu, "gu", ty, (M, 2 * Fp)), _array(h, "h", ty, (M, Fp)), *_ws(ws),
+                           M, K, F, N, ldx, ldr, ldy, act, dt, _stream(stream))
+    _ok("hexffn_fwd", rc)
+    return y
+
+
+def hexffn_bwd_workspace(M, K, F, N, ldx, lddy, dt):
+    return load().hexffn_bwd_workspace(M, K, F, N, ldx, lddy, dt)
+
+
+def hexffn_bwd(x, w1, w2, gu, h, dy, dx, dw1, db1, dw2, db2, ws, act: int = HEX_ACT_SILU,
+               stream=None):
+    """dx and the weights' gradients (each may be None; float32 or of x's
+    type) <- gradients of hexffn_fwd."""
+    M, K = x.shape
+    N, F = w2.shape
+    dt, ty, Fp = _dtype_code(x), x.dtype, hexffn_width(F)
+    gt = _grad_dtype(ty, (dw1, db1, dw2, db2))
+    px, ldx = _rows(x, "x", ty, M, K)
+    pg, ldg = _rows(dy, "dy", ty, M, N)
+    pd, ldd = _rows(dx, "dx", ty, M, K)
+    rc = load().hexffn_bwd(px, _array(w1, "w1", ty, (2 * F, K)), _array(w2, "w2", ty, (N, F)),
+                           _array(gu, "gu", ty, (M, 2 * Fp)), _array(h, "h", ty, (M, Fp)), pg, pd,
+                           _array(dw1, "dw1", gt, (2 * F, K)), _array(db1, "db1", gt, (2 * F,)),
+                           _array(dw2, "dw2", gt, (N, F)), _array(db2, "db2", gt, (N,)), *_ws(ws),
+                           M, K, F, N, ldx, ldg, ldd, act, dt if gt is ty else HEX_F32, dt,
+                           _stream(stream))
+    _ok("hexffn_bwd", rc)
+    return dx, dw1, db1, dw2, db2

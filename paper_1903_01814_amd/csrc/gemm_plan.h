@@ -10,15 +10,21 @@ int device_cus();
 
 namespace gemm {
 
+// One launch: rows `first` .. first + rows - 1 of D in mt x nt tiles.
+struct Part {
+    int tile;      // 256, 128 or 64 rows and columns
+    int first, rows, mt, nt;
+    int kt, steps; // tiles of k, and of all products of planes
+    int splits, per; // parts of the contraction, of so many steps; 0: runs of all tiles'
+                     // steps, as many as compute units (256 only)
+};
 // D[M][N] over K, `planes` 1 or 3 (float32).  gated: N counts the columns of one
-// half, a tile has as many of each.
+// half, a tile has half its columns of each (64: all of each).
 struct Plan {
     int M, N, K;
-    int tile;      // rows and columns of a block's tile: 256, 128 or 64
-    int mt, nt;    // tiles
-    int kt, steps; // tiles of 64 k, and of all products of planes
-    int splits, per;
     int64_t Np; // columns of the split sums
+    int parts;
+    Part part[2];
 };
 
 Plan make_plan(int M, int N, int K, bool gated, int planes);

@@ -233,60 +233,4 @@ size_t linear_bwd(const LinearArgs &a, const LinearGrads &g, void *ws, bool run,
     return sp.used;
 }
 
-namespace gemm {
-
-// The division with the least estimated time: rounds of the blocks that the card
-// holds at a time, each its steps, its start and its epilogue; a split adds its
-// sums' way through memory and a launch.
-Plan make_plan(int M, int N, int K, bool gated, int planes)
-{
-    struct Tile {
-        int rows, per_cu;
-        double full, alone, fixed; // us a step with all blocks of a unit at work, and with one
-    };
-    static constexpr Tile tiles[] = {{256, 1, 2.2, 2.2, 6.0}, {128, 2, 1.4, 0.8, 3.0}, {64, 4, 1.1, 0.4, 2.0}};
-    Plan best{};
-    double least = 0;
-    const int cus = device_cus();
-    for (const Tile &t : tiles) {
-        Plan p{};
-        p.M = M;
-        p.N = N;
-        p.K = K;
-        p.tile = t.rows;
-        const int cols = gated && t.rows > 64 ? t.rows / 2 : t.rows;
-        p.mt = static_cast<int>((static_cast<int64_t>(M) + t.rows - 1) / t.rows);
-        p.nt = (N + cols - 1) / cols;
-        p.kt = (K + 63) / 64;
-        p.steps = p.kt * (planes == 3 ? 6 : 1);
-        p.Np = (N + 7) / 8 * 8;
-        const int64_t blocks = static_cast<int64_t>(p.mt) * p.nt;
-        for (int want = 1; want <= 64 && want <= p.steps; want = want < 4 ? want + 1 : want * 3 / 2) {
-            const int per = (p.steps + want - 1) / want, splits = (p.steps + per - 1) / per;
-            const double bytes = 4.0 * splits * M * p.Np * (gated ? 2 : 1);
-            if (splits > 1 && (bytes > 256e6 || blocks * splits > 16 * cus))
-                break;
-            const double rounds_d = static_cast<double>(blocks * splits) / (static_cast<double>(cus) * t.per_cu);
-            const double whole = static_cast<double>((blocks * splits + static_cast<int64_t>(cus) * t.per_cu - 1) / (static_cast<int64_t>(cus) * t.per_cu));
-            const double step = rounds_d <= 1.0 / t.per_cu ? t.alone : t.full;
-            double us = whole * (per * step + t.fixed);
-            if (splits > 1)
-                us += 5.0 + 2 * bytes / 4e6;
-            if (best.tile == 0 || us < least) {
-                least = us;
-                best = p;
-                best.per = per;
-                best.splits = splits;
-            }
-        }
-    }
-    return best;
-}
-
-size_t part_bytes(const Plan &p, bool gated)
-{
-    return p.splits > 1 ? static_cast<size_t>(p.splits) * p.M * p.Np * (gated ? 2 : 1) * 4 : 0;
-}
-
-} // namespace gemm
 } // namespace hexk

@@ -464,8 +464,9 @@ int hexdropout(const void *x, const void *res, void *y, int64_t n, double p, con
  *    HEX_LINEAR_MAX_DIM features of a projection, strides below 2^22, 2^33
  *    elements a tensor, 2^30 in one projection of a gated pair.
  *  - Sums, statistics and their reciprocals are float32.  bf16 calls round what
- *    one product hands to the next once to bf16: z and dz of a projection; g, u, h,
- *    dg and du of a gated block.
+ *    one product hands to the next once to bf16: z and dz of a projection; h, dg
+ *    and du of a gated block, whose g and u keep 10 bits or more between 2^-14 and
+ *    2^15 (7 where one of eight neighbours lies outside).
  *  - Float32 products take each operand as the sum of three bf16 numbers, as
  *    hexattn_fwd does: operands under 2^-110 lose bits; infinities, and values
  *    from 3.39e38 on, give NaN.
@@ -551,7 +552,7 @@ size_t hexffn_fwd_workspace(int M, int K, int F, int N, int64_t ldx, hex_dtype d
  *   y = h w2^T + b2 + res
  * w1 [2F][K], b1 [2F], w2 [N][F], b2 [N]; b1, b2 and res [M][N] may be NULL.
  * h [M][hexffn_width(F)] is written; gu [M][2 hexffn_width(F)], g and u for the
- * backward, may be NULL.  ws: at least hexffn_fwd_workspace(...) bytes, NULL where
+ * backward in a form of the library's own, may be NULL.  ws: at least hexffn_fwd_workspace(...) bytes, NULL where
  * that is 0.
  */
 int hexffn_fwd(const void *x, const void *w1, const void *b1, const void *w2, const void *b2,

@@ -430,10 +430,11 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
         // one product of planes: all but the last tile of k are whole
         if (a.steps == a.kt)
 #pragma unroll 1
-            for (; ahead > 3; --t) {
+            while (ahead > 3) { // three a time, counted by steady
                 steady(s0, s1);
                 steady(s1, s2);
                 steady(s2, s0);
+                --t;
             }
 #pragma unroll 1
         for (; t > 0; --t) {

@@ -7,8 +7,9 @@
 // Both projections are one product whose waves hold a column of the gate and of
 // its partner in the same lane, so h is made in its epilogue; dg and du are made
 // in the epilogue of dh's product, and dh never reaches memory.  bfloat16 calls
-// round g, u (as kept for the backward), h, dg and du once to bfloat16, as
-// operands of the products that follow; h itself is made of unrounded g and u.
+// round h, dg and du once to bfloat16, as operands of the products that follow, and g
+// and u where they are kept for the backward (below); h is made of unrounded ones.
+#include "few.h"
 #include "gemm.h"
 #include "tokens.h"
 
@@ -17,6 +18,69 @@ namespace {
 
 using gemm::Plan;
 using gemm::Side;
+
+// ---- how g and u are kept for the backward: float32 as they are; bfloat16 calls
+// have 16 bits a value.  With bfloat16's 8 bits of precision there, dx and dw1
+// would carry three roundings of like size (g and u, dg and du, the result: 3.0e-3
+// of their norm); so eight values in a row become float16, 11 bits, where all of
+// them have its exponents, 2^-14 .. 2^15, and bfloat16 where one has not: 2.4e-3,
+// as a projection's gradients have.  The first value's last bit says which (1:
+// float16), so that it is off by up to twice a rounding.
+struct Kept {
+    template <typename E> static __device__ __forceinline__ void save(E *p, const float (&v)[8])
+    {
+        if constexpr (sizeof(E) == 4) {
+            save_row8<E, true>(p, 8, v);
+        } else {
+            float most = fabsf(v[0]), least = fabsf(v[0]);
+#pragma unroll
+            for (int i = 1; i < 8; ++i) {
+                most = fmaxf(most, fabsf(v[i]));
+                least = fminf(least, fabsf(v[i]));
+            }
+            // a NaN is not seen by the two, but by the sum
+            float nan = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                nan += 0.f * v[i];
+            uint4 u;
+            if (most < 32768.f && least >= 6.103515625e-5f && nan == 0.f) {
+                half8 h;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    h[i] = static_cast<_Float16>(v[i]);
+                u = __builtin_bit_cast(uint4, h);
+                u.x |= 1u;
+            } else {
+                pack8<bf16raw>(v, &u);
+                // the first to 7 bits, to nearest even
+                const uint32_t b = __float_as_uint(v[0]);
+                const uint32_t r = v[0] != v[0] ? 0x7fc0u : (b + 0xffffu + (b >> 17 & 1u)) >> 17 << 1;
+                u.x = (u.x & 0xffff0000u) | r;
+            }
+            *reinterpret_cast<uint4 *>(p) = u;
+        }
+    }
+    template <typename E> static __device__ __forceinline__ void load(const E *p, float (&v)[8])
+    {
+        if constexpr (sizeof(E) == 4) {
+            row8<E, true>(p, 8, v);
+        } else {
+            const uint4 u = *reinterpret_cast<const uint4 *>(p);
+            if (u.x & 1u) {
+                const half8 h = __builtin_bit_cast(half8, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[i] = static_cast<float>(h[i]);
+            } else {
+                unpack8<bf16raw>(&u, v);
+            }
+        }
+    }
+
+  private:
+    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+};
 
 // g + bg, u + bu to gu (nullable), h = act(g) u; zeros in the columns F .. Fp - 1
 template <typename E, int ACT> struct GatedEpi {
@@ -56,8 +120,8 @@ template <typename E, int ACT> struct GatedEpi {
             }
         if (gu != nullptr) {
             E *p = gu + static_cast<int64_t>(m) * 2 * Fp + f;
-            save_row8<E, true>(p, 8, g);
-            save_row8<E, true>(p + Fp, 8, u);
+            Kept::save(p, g);
+            Kept::save(p + Fp, u);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -85,8 +149,8 @@ template <typename E, int ACT> struct GatedGradEpi {
     {
         Fetched x;
         const E *p = gu + static_cast<int64_t>(m) * 2 * Fp + f;
-        row8<E, true>(p, 8, x.g);
-        row8<E, true>(p + Fp, 8, x.u);
+        Kept::load(p, x.g);
+        Kept::load(p + Fp, x.u);
         return x;
     }
     __device__ __forceinline__ void done(int m, int f, float (&dh)[8], Nothing,
@@ -112,15 +176,22 @@ template <typename E, int ACT> struct GatedGradEpi {
     }
 };
 
+template <typename E, int ACT> GatedEpi<E, ACT> gated(const FfnArgs &a)
+{
+    return GatedEpi<E, ACT>{static_cast<const E *>(a.b1), static_cast<E *>(a.gu),
+                            static_cast<E *>(a.h), round8(a.F), a.F};
+}
 template <typename E, int ACT>
 hipError_t gated_product(const Plan &pl, const Side &W, const Side &X, float *ws, const FfnArgs &a,
-                         int64_t Fp, hipStream_t st)
+                         hipStream_t st)
 {
-    return gemm::launch<false, false, true>(
-        pl, W, X, static_cast<int>(Fp), ws,
-        GatedEpi<E, ACT>{static_cast<const E *>(a.b1), static_cast<E *>(a.gu),
-                         static_cast<E *>(a.h), Fp, a.F},
-        st);
+    return gemm::launch<false, false, true>(pl, W, X, static_cast<int>(round8(a.F)), ws,
+                                            gated<E, ACT>(a), st);
+}
+template <typename E, int ACT> hipError_t gated_few(const FfnArgs &a, hipStream_t st)
+{
+    return few::launch<E, true>(few::Args{a.w1, a.x, a.ldx, a.M, a.F, a.K, a.F}, gated<E, ACT>(a),
+                                st);
 }
 
 template <typename E, int ACT>
@@ -131,21 +202,18 @@ hipError_t gated_grad(const Plan &pl, const Side &W2, const Side &DY, float *ws,
         pl, W2, DY, 0, ws, GatedGradEpi<E, ACT>{static_cast<const E *>(gu), d, Fp, plane}, st);
 }
 
-// f<E, ACT>(args) for the type and the activation
-#define HEX_BY_ACT(f, E, ...)                                                                 \
-    (act == ACT_RELU   ? f<E, ACT_RELU>(__VA_ARGS__)                                          \
-     : act == ACT_GELU ? f<E, ACT_GELU>(__VA_ARGS__)                                          \
-     : act == ACT_SILU ? f<E, ACT_SILU>(__VA_ARGS__)                                          \
-                       : f<E, ACT_NONE>(__VA_ARGS__))
-#define HEX_BY_TYPE(f, ...)                                                                   \
-    (dt == F32 ? HEX_BY_ACT(f, float, __VA_ARGS__) : HEX_BY_ACT(f, bf16raw, __VA_ARGS__))
-
 } // namespace
 
 size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err)
 {
-    const int planes = dt == F32 ? 3 : 1;
+    const int act = a.act, planes = dt == F32 ? 3 : 1;
     const int64_t Fp = round8(a.F);
+    const Output o{a.b2, a.res, a.y, nullptr, a.ldr, a.ldy};
+    if (a.M <= few::kMost) {
+        if (run && (err = HEX_BY_TYPE(gated_few, a, st)) == hipSuccess)
+            err = linear_few(a.w2, a.h, Fp, a.M, a.N, a.F, o, ACT_NONE, dt, st);
+        return 0;
+    }
     const Halves none{0, 0}, halves{a.F, static_cast<int>(Fp)};
     Space sp{static_cast<char *>(ws)};
     PackJobs jobs{}, late{};
@@ -157,15 +225,10 @@ size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, h
     const Plan p2 = gemm::make_plan(a.M, a.N, a.F, false, planes);
     const size_t b1 = gemm::part_bytes(p1, true), b2 = gemm::part_bytes(p2, false);
     float *part = sp.take<float>((b1 > b2 ? b1 : b2) / 4);
-    if (!run)
-        return sp.used;
-    if ((err = pack(jobs, dt, st)) != hipSuccess)
-        return sp.used;
-    const int act = a.act;
-    err = HEX_BY_TYPE(gated_product, p1, W1, X, part, a, Fp, st);
-    if (err == hipSuccess && (err = pack(late, dt, st)) == hipSuccess)
-        err = linear_product(p2, W2, H, part, a.b2, a.res, a.y, nullptr, a.ldr, a.ldy, ACT_NONE, dt,
-                             st);
+    if (run && (err = pack(jobs, dt, st)) == hipSuccess &&
+        (err = HEX_BY_TYPE(gated_product, p1, W1, X, part, a, st)) == hipSuccess &&
+        (err = pack(late, dt, st)) == hipSuccess)
+        err = linear_product(p2, W2, H, part, o, ACT_NONE, dt, st);
     return sp.used;
 }
 

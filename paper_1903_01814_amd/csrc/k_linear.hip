@@ -6,6 +6,7 @@
 // Matrix products of gemm.h with their epilogues; what bounds them stands there.
 // bfloat16 calls round z (where it is kept) and dz once to bfloat16, as operands
 // of the products that follow; sums are float32.
+#include "few.h"
 #include "gemm.h"
 #include "tokens.h"
 
@@ -147,48 +148,58 @@ hipError_t store_product(bool tall_q, const Plan &pl, const Side &P, const Side 
 namespace {
 
 template <typename E, int ACT>
-hipError_t product_of(const Plan &pl, const Side &W, const Side &X, float *ws, const void *bias,
-                      const void *res, void *y, void *z, int64_t ldr, int64_t ldy, hipStream_t st)
+LinearEpi<E, ACT> epilogue(const Output &o, int N)
 {
     constexpr int64_t per = 16 / sizeof(E);
-    const bool vec = pl.N % 8 == 0 && ldr % per == 0 && ldy % per == 0;
-    return gemm::launch<false, false, false>(
-        pl, W, X, 0, ws,
-        LinearEpi<E, ACT>{static_cast<const E *>(bias), static_cast<const E *>(res),
-                          static_cast<E *>(y), static_cast<E *>(z), ldr, ldy, pl.N, vec},
-        st);
+    const bool vec = N % 8 == 0 && o.ldr % per == 0 && o.ldy % per == 0;
+    return LinearEpi<E, ACT>{static_cast<const E *>(o.bias), static_cast<const E *>(o.res),
+                             static_cast<E *>(o.y), static_cast<E *>(o.z), o.ldr, o.ldy, N, vec};
+}
+
+template <typename E, int ACT>
+hipError_t product_of(const Plan &pl, const Side &W, const Side &X, float *ws, const Output &o,
+                      hipStream_t st)
+{
+    return gemm::launch<false, false, false>(pl, W, X, 0, ws, epilogue<E, ACT>(o, pl.N), st);
+}
+template <typename E, int ACT>
+hipError_t few_of(const few::Args &a, const Output &o, hipStream_t st)
+{
+    return few::launch<E, false>(a, epilogue<E, ACT>(o, a.N), st);
 }
 
 } // namespace
 
-hipError_t linear_product(const Plan &pl, const Side &W, const Side &X, float *ws, const void *bias,
-                          const void *res, void *y, void *z, int64_t ldr, int64_t ldy, int act,
-                          Dtype dt, hipStream_t st)
+hipError_t linear_product(const Plan &pl, const Side &W, const Side &X, float *ws, const Output &o,
+                          int act, Dtype dt, hipStream_t st)
 {
-#define HEX_PRODUCT(E, ACT) product_of<E, ACT>(pl, W, X, ws, bias, res, y, z, ldr, ldy, st)
-#define HEX_PRODUCTS(E)                                                                       \
-    (act == ACT_RELU   ? HEX_PRODUCT(E, ACT_RELU)                                             \
-     : act == ACT_GELU ? HEX_PRODUCT(E, ACT_GELU)                                             \
-     : act == ACT_SILU ? HEX_PRODUCT(E, ACT_SILU)                                             \
-                       : HEX_PRODUCT(E, ACT_NONE))
-    return dt == F32 ? HEX_PRODUCTS(float) : HEX_PRODUCTS(bf16raw);
-#undef HEX_PRODUCTS
-#undef HEX_PRODUCT
+    return HEX_BY_TYPE(product_of, pl, W, X, ws, o, st);
+}
+
+hipError_t linear_few(const void *w, const void *x, int64_t ldx, int M, int N, int K,
+                      const Output &o, int act, Dtype dt, hipStream_t st)
+{
+    const few::Args a{w, x, ldx, M, N, K, 0};
+    return HEX_BY_TYPE(few_of, a, o, st);
 }
 
 size_t linear_fwd(const LinearArgs &a, void *ws, bool run, Dtype dt, hipStream_t st,
                   hipError_t &err)
 {
+    const Output o{a.bias, a.res, a.y, a.z, a.ldr, a.ldy};
+    if (a.M <= few::kMost) {
+        if (run)
+            err = linear_few(a.w, a.x, a.ldx, a.M, a.N, a.K, o, a.act, dt, st);
+        return 0;
+    }
     Space sp{static_cast<char *>(ws)};
     PackJobs jobs{};
     const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, Halves{0, 0}, sp, jobs);
     const Side W = operand(a.w, nullptr, 0, a.N, a.K, a.K, dt, Halves{0, 0}, sp, jobs);
     const Plan pl = gemm::make_plan(a.M, a.N, a.K, false, dt == F32 ? 3 : 1);
     float *part = sp.take<float>(gemm::part_bytes(pl, false) / 4);
-    if (!run)
-        return sp.used;
-    if ((err = pack(jobs, dt, st)) == hipSuccess)
-        err = linear_product(pl, W, X, part, a.bias, a.res, a.y, a.z, a.ldr, a.ldy, a.act, dt, st);
+    if (run && (err = pack(jobs, dt, st)) == hipSuccess)
+        err = linear_product(pl, W, X, part, o, a.act, dt, st);
     return sp.used;
 }
 

@@ -8,6 +8,15 @@
 
 namespace hexk {
 
+// f<E, ACT>(args) for the type `dt` and the activation `act`
+#define HEX_BY_ACT(f, E, ...)                                                                 \
+    (act == ACT_RELU   ? f<E, ACT_RELU>(__VA_ARGS__)                                          \
+     : act == ACT_GELU ? f<E, ACT_GELU>(__VA_ARGS__)                                          \
+     : act == ACT_SILU ? f<E, ACT_SILU>(__VA_ARGS__)                                          \
+                       : f<E, ACT_NONE>(__VA_ARGS__))
+#define HEX_BY_TYPE(f, ...)                                                                   \
+    (dt == F32 ? HEX_BY_ACT(f, float, __VA_ARGS__) : HEX_BY_ACT(f, bf16raw, __VA_ARGS__))
+
 constexpr int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
 
 // Two halves of `half` rows (or columns), the second from `halfp` on, as one run
@@ -78,10 +87,18 @@ gemm::Side operand(const void *src, const void *z, int act, int rows, int cols, 
 // its columns as the operand's rows
 gemm::Side tall(const gemm::Side &s, int cols);
 
-// y = act(x w^T + bias) + res of operands W and X
+// What a projection's sums become: y = act(z) + res, z = sums + bias.
+struct Output {
+    const void *bias, *res;
+    void *y, *z;
+    int64_t ldr, ldy;
+};
+// of operands W and X
 hipError_t linear_product(const gemm::Plan &pl, const gemm::Side &W, const gemm::Side &X, float *ws,
-                          const void *bias, const void *res, void *y, void *z, int64_t ldr,
-                          int64_t ldy, int act, Dtype dt, hipStream_t st);
+                          const Output &o, int act, Dtype dt, hipStream_t st);
+// of a few tokens, tensors as they are
+hipError_t linear_few(const void *w, const void *x, int64_t ldx, int M, int N, int K,
+                      const Output &o, int act, Dtype dt, hipStream_t st);
 // y [map(m)] = Q P in dt: P tall, Q wide (data gradient) or tall (weight gradient)
 hipError_t store_product(bool tall_q, const gemm::Plan &pl, const gemm::Side &P,
                          const gemm::Side &Q, float *ws, void *y, int64_t ldy, Halves map, Dtype dt,

@@ -6,8 +6,8 @@ Bounds.  A half step of bfloat16 is R = 2^-8 of a value, of float32 2^-24.  A
 float32 sum of n products is off by at most (n + 32) 2^-24 of the sum of their
 magnitudes (every addition rounded once; the 32 hold the rounding of what is
 summed, 2^-24 of a product that the three-part products leave out, and the joins
-of partial sums).  bfloat16 calls round z, dz, g, u, h, dg and du once (R) where
-they are operands of a next product.  Activations: |act'| <= 1.13, |act''| <= 0.8
+of partial sums).  bfloat16 calls round z, dz, h, dg and du once (R) where they
+are operands of a next product, and keep g and u to 2^-7 or better for the backward.  Activations: |act'| <= 1.13, |act''| <= 0.8
 (gelu; silu 1.10 and 0.5), values off by 1e-6 of z (the fast forms' 1.5e-7 and
 their exponentials' roundings)."""
 import math
@@ -117,7 +117,8 @@ def ffn(x, w1, b1, w2, b2, res, name, dt, dy=None, gt=None):
     rg = R[gt or dt]
     dh = dy @ w2
     edh = acc(N) * (dy.abs() @ w2.abs())
-    kg, ku = eg + R[dt] * g.abs(), eu + R[dt] * u.abs()  # g and u as they are kept
+    keep = 2.0 ** -7 if dt == "bf16" else 0.0
+    kg, ku = eg + keep * g.abs(), eu + keep * u.abs()  # g and u as they are kept
     dg, du = dh * u * d, dh * a
     edg = (edh * u.abs() * s1 + dh.abs() * s1 * ku + (dh * u).abs() * (s2 * kg + 2 * sa) +
            R[dt] * dg.abs() + 2.0 ** -22 * dg.abs())

@@ -2,8 +2,8 @@
 // stream), D[m][n] = sum over k of x[m][k] w[n][k] with the epilogues of gemm.h.
 //
 // The time is that of reading the weights once, so all of them have to be on
-// their way at once: a block takes 16 rows of w (GATED: and their 16 partners),
-// its waves take chunks of 128 bytes of k in turn, four chunks' loads ahead, and
+// their way at once: a block takes 16 rows of w (or eight; GATED: and as many
+// partners), its waves take chunks of 128 bytes of k in turn, four chunks' loads ahead, and
 // add their sums in LDS at the end, in the waves' order.  No workspace, nothing
 // laid out before: float32 is multiplied as it is, and rows of any alignment are
 // read as they lie.
@@ -69,66 +69,67 @@ __device__ __forceinline__ floatx4 multiply(const uint4 &a, const uint4 &b, floa
     return c;
 }
 
-template <typename E, int TG, bool GATED, bool VEC, typename Epi>
-__global__ __launch_bounds__(1024) void few_k(Args a, Epi e)
+// WR and XR: loads of eight rows of w (1 or 2) and of x (1, 2, 4).  Half the rows a
+// block, half of the product's then unused, where there would not be a block for
+// every compute unit otherwise.
+template <typename E, int WR, int XR, bool GATED, bool VEC, typename Epi>
+__global__ __launch_bounds__(GATED ? 512 : 1024) void few_k(Args a, Epi e)
 {
     constexpr int V = 16 / sizeof(E), KC = 8 * V; // k of a vector, of a chunk
-    constexpr int H = GATED ? 2 : 1, R = H + TG;  // pieces of 16 rows x 128 bytes
-    constexpr int U = 4;                          // chunks' loads under way
+    constexpr int H = GATED ? 2 : 1, TG = (XR + 1) / 2;
+    constexpr int R = H + TG, L = H * WR + XR;    // pieces of 16 rows x 128 bytes; loads
+    constexpr int U = L <= 3 ? 4 : L <= 6 ? 3 : 2; // chunks' loads under way
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * (8 * WR);
     char *mine = lds + wave * (R * 2048);
 
-    // this lane's two rows of each piece, its vector of their chunks
+    // this lane's row and place in LDS of each load, its vector of the chunks
     const int lr = lane >> 3, lc = lane & 7;
-    const E *row[R][2];
-    bool live[R][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = lr + 8 * i, n = min(n0 + r, a.N - 1);
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-            row[h][i] = static_cast<const E *>(a.w) + static_cast<int64_t>(n + h * a.half) * a.K;
-            live[h][i] = true;
-        }
-#pragma unroll
-        for (int g = 0; g < TG; ++g) {
-            const int m = 16 * g + r;
-            live[H + g][i] = m < a.M;
-            row[H + g][i] = static_cast<const E *>(a.x) + (m < a.M ? m : 0) * a.ldx;
-        }
-    }
-    const int chunks = (a.K + KC - 1) / KC;
     auto at = [&](int piece, int r, int c) {
         return reinterpret_cast<uint4 *>(mine + piece * 2048 + r * 128 + ((c ^ (r >> 1 & 7)) << 4));
     };
+    const E *row[L];
+    bool live[L];
+    uint4 *to[L];
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+        if (l < H * WR) {
+            const int h = l / WR, r = lr + 8 * (l % WR), n = min(n0 + r, a.N - 1);
+            row[l] = static_cast<const E *>(a.w) + static_cast<int64_t>(n + h * a.half) * a.K;
+            live[l] = true;
+            to[l] = at(h, r, lc);
+        } else {
+            const int x = l - H * WR, m = lr + 8 * x;
+            live[l] = m < a.M;
+            row[l] = static_cast<const E *>(a.x) + (m < a.M ? m : 0) * a.ldx;
+            to[l] = at(H + x / 2, lr + 8 * (x % 2), lc);
+        }
+    }
+    const int chunks = (a.K + KC - 1) / KC;
 
     floatx4 acc[H][TG] = {};
     for (int c0 = wave; c0 < chunks; c0 += waves * U) {
-        uint4 u[U][R][2];
+        uint4 u[U][L];
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             const int k = (c0 + j * waves) * KC + lc * V;
 #pragma unroll
-            for (int p = 0; p < R; ++p)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    u[j][p][i] = live[p][i] ? load16<E, VEC>(row[p][i] + (k < a.K ? k : 0), a.K - k)
-                                            : uint4{0, 0, 0, 0};
+            for (int l = 0; l < L; ++l)
+                u[j][l] = live[l] ? load16<E, VEC>(row[l] + (k < a.K ? k : 0), a.K - k)
+                                  : uint4{0, 0, 0, 0};
         }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             if (c0 + j * waves >= chunks)
                 break;
 #pragma unroll
-            for (int p = 0; p < R; ++p)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    *at(p, lr + 8 * i, lc) = u[j][p][i];
+            for (int l = 0; l < L; ++l)
+                *to[l] = u[j][l];
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
+                // rows that no load wrote: what lies there, in results that are not used
                 const int r = lane & 15, c = 4 * s + (lane >> 4);
                 uint4 f[R];
 #pragma unroll
@@ -154,9 +155,9 @@ __global__ __launch_bounds__(1024) void few_k(Args a, Epi e)
             *reinterpret_cast<floatx4 *>(sums + ((wave * H + h) * TG + g) * 256 +
                                          (lane & 15) * 16 + 4 * (lane >> 4)) = acc[h][g];
     __syncthreads();
-    // two threads a token, eight columns each
-    const int g = threadIdx.x >> 5, t = threadIdx.x >> 1 & 15, m = 16 * g + t;
-    const int n = n0 + 8 * (threadIdx.x & 1);
+    // a thread eight columns of a token
+    const int t = threadIdx.x / WR % 16, g = threadIdx.x / (16 * WR), m = 16 * g + t;
+    const int n = n0 + 8 * (threadIdx.x % WR);
     if (g >= TG || m >= a.M || n >= a.N)
         return;
     const auto cols = e.cols(n);
@@ -177,29 +178,41 @@ __global__ __launch_bounds__(1024) void few_k(Args a, Epi e)
         e.done(m, n, v[0], cols, f);
 }
 
-template <typename E, int TG, bool GATED, typename Epi>
+template <typename E, int WR, int XR, bool GATED, typename Epi>
 hipError_t launch_for(const Args &a, const Epi &e, bool vec, hipStream_t st)
 {
-    const int blocks = (a.N + 15) / 16, chunks = static_cast<int>((a.K * sizeof(E) + 127) / 128);
-    // 16 waves where the blocks do not fill the card, eight else; none without a
-    // chunk
-    int waves = blocks > device_cus() ? 8 : 16;
+    const int blocks = (a.N + 8 * WR - 1) / (8 * WR);
+    const int chunks = static_cast<int>((a.K * sizeof(E) + 127) / 128);
+    // 16 waves where a compute unit has one block, eight else; none without a chunk
+    int waves = GATED || blocks > device_cus() ? 8 : 16;
     while (waves > 1 && waves / 2 >= chunks)
         waves /= 2;
-    const size_t lds = static_cast<size_t>(waves) * ((GATED ? 2 : 1) + TG) * 2048;
+    const size_t lds = static_cast<size_t>(waves) * ((GATED ? 2 : 1) + (XR + 1) / 2) * 2048;
     if (vec)
-        HEX_LAUNCH((few_k<E, TG, GATED, true, Epi>), dim3(blocks), dim3(64 * waves), lds, st, a, e);
+        HEX_LAUNCH((few_k<E, WR, XR, GATED, true, Epi>), dim3(blocks), dim3(64 * waves), lds, st, a,
+                   e);
     else
-        HEX_LAUNCH((few_k<E, TG, GATED, false, Epi>), dim3(blocks), dim3(64 * waves), lds, st, a, e);
+        HEX_LAUNCH((few_k<E, WR, XR, GATED, false, Epi>), dim3(blocks), dim3(64 * waves), lds, st,
+                   a, e);
     return hipGetLastError();
+}
+
+template <typename E, int WR, bool GATED, typename Epi>
+hipError_t launch_rows(const Args &a, const Epi &e, hipStream_t st)
+{
+    constexpr int64_t V = 16 / sizeof(E);
+    const bool vec = a.K % V == 0 && a.ldx % V == 0;
+    return a.M <= 8    ? launch_for<E, WR, 1, GATED>(a, e, vec, st)
+           : a.M <= 16 ? launch_for<E, WR, 2, GATED>(a, e, vec, st)
+                       : launch_for<E, WR, 4, GATED>(a, e, vec, st);
 }
 
 // M up to kMost; rows of w and x of any alignment
 template <typename E, bool GATED, typename Epi>
 hipError_t launch(const Args &a, const Epi &e, hipStream_t st)
 {
-    const bool vec = a.K % (16 / sizeof(E)) == 0 && a.ldx % (16 / static_cast<int64_t>(sizeof(E))) == 0;
-    return a.M <= 16 ? launch_for<E, 1, GATED>(a, e, vec, st) : launch_for<E, 2, GATED>(a, e, vec, st);
+    return (a.N + 15) / 16 < device_cus() ? launch_rows<E, 1, GATED>(a, e, st)
+                                          : launch_rows<E, 2, GATED>(a, e, st);
 }
 
 } // namespace few

@@ -7,8 +7,9 @@
 // row of memory is one m or n) or contiguous in m or n ("tall": a row of memory
 // is one k); the forward takes wide and wide, the data gradient a tall P (the
 // weights as they are), the weight gradient tall and tall.  A float32 operand is
-// three bfloat16 planes (attn.h, Split) and a product six products of planes,
-// small ones first: the same kernel over six times the contraction.
+// three bfloat16 planes (attn.h, Split), all of a tile in LDS together, and a product
+// six products of planes: the large one in sums of its own, so that it is rounded as
+// often as a plain one, and each operand read once for three.
 //
 // A block has BM x BN of D, its NM x NN waves parts of it in 32 x 32 x 16 products
 // with P as the rows.  The sums go through LDS once, 32 rows a wave at a time, so
@@ -59,7 +60,7 @@ struct Side {
 struct Args {
     Side P, Q;
     int M, N, K;
-    int kt, steps;   // tiles of k, and of all products of planes
+    int steps;       // tiles of k
     // (M: the row behind the tiles' last one)
     int per;         // steps of a split (grid.y splits); 0: the blocks share all
                      // tiles' steps evenly, in runs that end within tiles
@@ -70,11 +71,6 @@ struct Args {
                      // runs, a tile each: number tile + block
     int64_t Np;
 };
-
-// planes of the six products of a float32 contraction, small ones first: P and
-// Q of product i in bits 2 i
-constexpr int kPlanesP = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
-constexpr int kPlanesQ = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
 
 typedef const __attribute__((address_space(1))) void *GlobalPtr;
 typedef __attribute__((address_space(3))) void *LdsPtr;
@@ -115,15 +111,14 @@ template <bool TALL, int B, int KS, int NW> struct Loader {
     // Load j of a tile; base: of the block's rows and the tile's k.  As an
     // instruction of its own, so that the compiler does not wait for loads of one
     // buffer where another is read (it did, in one turn of three); meet() in the
-    // kernel waits.  It has no result in registers, and a buffer is read behind a
-    // meeting only.
+    // kernel waits.  It has no result in registers, a buffer is read behind a
+    // meeting only, and nothing else here uses m0.
     __device__ __forceinline__ void load(char *lds, int wave, const char *base, int j) const
     {
         const uint32_t to = static_cast<uint32_t>(
             reinterpret_cast<uintptr_t>((LdsPtr)(lds + 1024 * (wave + NW * j))));
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to),
-                     "v"(at[j]), "s"(base)
-                     : "m0");
+                     "v"(at[j]), "s"(base));
     }
     // a tile of `left` k: the chunks past them become zeros, each lane in its place
     __device__ __forceinline__ void load_part(char *lds, int wave, const char *base, int left) const
@@ -201,12 +196,14 @@ __device__ __forceinline__ void tile_of(int b, int mt, int nt, int &m, int &n)
 // GATED: done(m, f, g, u, ..), columns f of both halves.
 // APART: the epilogue has LDS of its own, and a block goes on to further tiles,
 // whose first loads are under way during it.
-template <bool TP, bool TQ, int BM, int BN, int KS, int NM, int NN, bool APART, bool GATED,
+template <int PL, bool TP, bool TQ, int BM, int BN, int KS, int NM, int NN, bool APART, bool GATED,
           typename Epi>
-__global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
+__global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gemm_k(Args a, Epi e)
 {
     constexpr int NW = NM * NN, WM = BM / NM, WN = BN / NN, TM = WM / 32, TN = WN / 32;
-    constexpr int kBytesP = BN * KS * 2, kBytes = (BM + BN) * KS * 2, S = KS / 16;
+    // a plane of P, then one of Q, and so on
+    constexpr int kBytesP = BN * KS * 2, kPlane = (BM + BN) * KS * 2, kBytes = PL * kPlane;
+    constexpr int S = KS / 16;
     constexpr int kSlice = 32 * WN * 4;        // a wave's sums in the epilogue
     constexpr int kFirst = kBytes / kSlice;    // waves that s0 has room for
     __shared__ __align__(1024) char s0[kBytes];
@@ -254,12 +251,11 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
     };
     using LoadP = Loader<TP, BN, KS, NW>;
     using LoadQ = Loader<TQ, BM, KS, NW>;
-    constexpr int kLoads = LoadP::J + LoadQ::J; // of a wave and a whole tile
+    constexpr int kLoads = PL * (LoadP::J + LoadQ::J); // of a wave and a whole tile
     LoadP lp;
     LoadQ lq;
     const char *baseP, *baseQ;
-    // the next k to load and its product of planes; tiles of k yet to be loaded
-    int pair, k, ahead;
+    int k, ahead; // the next tile of k to load, how many there are yet
     auto start = [&]() HEX_INLINE {
         lp.set(
             a.P.ld,
@@ -276,13 +272,8 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
             a.Q.ld, [&](int r) HEX_INLINE { return min(r, a.Q.rows - 1 - m0); }, a.Q.rows - m0, wave, lane);
         baseP = reinterpret_cast<const char *>(a.P.p + (TP ? n0 : n0 * a.P.ld));
         baseQ = reinterpret_cast<const char *>(a.Q.p + (TQ ? m0 : m0 * a.Q.ld));
-        pair = 5; // one plane: both numbers 0
         k = first;
         ahead = tiles;
-        if (a.steps != a.kt) {
-            pair = first / a.kt;
-            k = first - pair * a.kt;
-        }
     };
     // Loads what there is of the next tile of k.  open: whether that was a whole
     // one, so that the number of its loads is known.
@@ -292,24 +283,25 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
         if (ahead-- <= 0)
             return;
         const int left = a.K - k * KS;
-        const char *p = baseP + 2 * ((kPlanesP >> 2 * pair & 3) * a.P.plane + k * stepP);
-        const char *q = baseQ + 2 * ((kPlanesQ >> 2 * pair & 3) * a.Q.plane + k * stepQ);
         open = left >= KS;
-        if (open) {
 #pragma unroll
-            for (int j = 0; j < LoadP::J; ++j)
-                lp.load(lds, wave, p, j);
+        for (int l = 0; l < PL; ++l) {
+            const char *p = baseP + 2 * (k * stepP + l * a.P.plane);
+            const char *q = baseQ + 2 * (k * stepQ + l * a.Q.plane);
+            char *to = lds + l * kPlane;
+            if (open) {
 #pragma unroll
-            for (int j = 0; j < LoadQ::J; ++j)
-                lq.load(lds + kBytesP, wave, q, j);
-        } else {
-            lp.load_part(lds, wave, p, left);
-            lq.load_part(lds + kBytesP, wave, q, left);
+                for (int j = 0; j < LoadP::J; ++j)
+                    lp.load(to, wave, p, j);
+#pragma unroll
+                for (int j = 0; j < LoadQ::J; ++j)
+                    lq.load(to + kBytesP, wave, q, j);
+            } else {
+                lp.load_part(to, wave, p, left);
+                lq.load_part(to + kBytesP, wave, q, left);
+            }
         }
-        if (++k == a.kt) {
-            k = 0;
-            ++pair;
-        }
+        ++k;
     };
     // Every wave has read what it read of LDS, and its loads are there but for
     // those of the last tile (all, where their number is not known).
@@ -323,26 +315,35 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
 
-    floatx16 acc[TN][TM];
-    bf16x8 fp[2][TN], fq[2][TM];
+    constexpr int kSums = PL == 3 ? 2 : 1; // the large products', the small ones'
+    floatx16 acc[kSums][TN][TM];
+    bf16x8 fp[2][PL][TN], fq[2][PL][TM];
     // operand i in the order that multiply_one takes them
+    constexpr int kReads = PL * (TN + TM);
     auto read_one = [&](char *lds, int s, int to, int i) HEX_INLINE {
-        if (i >= 1 && i <= TM)
-            fq[to][i - 1] = rq.read(lds + kBytesP, i - 1, s);
+        const int l = i / (TN + TM), x = i % (TN + TM);
+        char *from = lds + l * kPlane;
+        if (x >= 1 && x <= TM)
+            fq[to][l][x - 1] = rq.read(from + kBytesP, x - 1, s);
         else
-            fp[to][i == 0 ? 0 : i - TM] = rp.read(lds, i == 0 ? 0 : i - TM, s);
+            fp[to][l][x == 0 ? 0 : x - TM] = rp.read(from, x == 0 ? 0 : x - TM, s);
     };
     auto read = [&](char *lds, int s, int to) HEX_INLINE {
 #pragma unroll
-        for (int i = 0; i < TN + TM; ++i)
+        for (int i = 0; i < kReads; ++i)
             read_one(lds, s, to, i);
     };
+    // planes of P and Q of product x
+    constexpr int kProducts = (PL == 3 ? 6 : 1) * TN * TM;
     auto multiply_one = [&](int from, int i) HEX_INLINE {
-        acc[i / TM][i % TM] = mma(fp[from][i / TM], fq[from][i % TM], acc[i / TM][i % TM]);
+        constexpr int kP[6] = {0, 1, 0, 1, 2, 0}, kQ[6] = {0, 0, 1, 1, 0, 2};
+        const int x = i / (TN * TM), j = i / TM % TN, m = i % TM;
+        floatx16 &c = acc[PL == 3 && x > 0 ? 1 : 0][j][m];
+        c = mma(fp[from][kP[x]][j], fq[from][kQ[x]][m], c);
     };
     auto multiply = [&](int from) HEX_INLINE {
 #pragma unroll
-        for (int i = 0; i < TN * TM; ++i)
+        for (int i = 0; i < kProducts; ++i)
             multiply_one(from, i);
     };
     // a tile in `here`, its first operands in registers; the next in `next` and the
@@ -362,7 +363,6 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
     // one by one between the products, not in a row before them (256 x 256, 8192 of
     // k: 545 -> 492 us, 8192 of contraction with a tall P: 512 -> 454).
     auto steady = [&](char *here, char *next) HEX_INLINE {
-        constexpr int kProducts = TN * TM, kReads = TN + TM;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const bool last = s == S - 1;
@@ -382,10 +382,13 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
 #pragma unroll
                 for (int x = 0; x < kLoads; ++x)
                     if (last && x * kProducts / kLoads == i) {
-                        if (x < LoadP::J)
-                            lp.load(here, wave, p, x);
+                        constexpr int J = LoadP::J + LoadQ::J;
+                        const int l = x / J, j = x % J;
+                        char *to = here + l * kPlane;
+                        if (j < LoadP::J)
+                            lp.load(to, wave, p + 2 * l * a.P.plane, j);
                         else
-                            lq.load(here + kBytesP, wave, q, x - LoadP::J);
+                            lq.load(to + kBytesP, wave, q + 2 * l * a.Q.plane, j - LoadP::J);
                     }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -408,10 +411,12 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
     begin();
     for (bool fresh = false;; fresh = true) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int x = 0; x < kSums; ++x)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-                acc[j][i] = floatx16{};
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+                    acc[x][j][i] = floatx16{};
         meet(fresh); // an epilogue's loads and stores are not counted
         if (tiles % 3 == 0) {
             load(s2);
@@ -427,15 +432,14 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
         if (tiles % 3 != 0)
             turn(s2, s0);
         int t = tiles / 3;
-        // one product of planes: all but the last tile of k are whole
-        if (a.steps == a.kt)
+        // all but the last tile of k are whole
 #pragma unroll 1
-            while (ahead > 3) { // three a time, counted by steady
-                steady(s0, s1);
-                steady(s1, s2);
-                steady(s2, s0);
-                --t;
-            }
+        while (ahead > 3) { // three a time, counted by steady
+            steady(s0, s1);
+            steady(s1, s2);
+            steady(s2, s0);
+            --t;
+        }
 #pragma unroll 1
         for (; t > 0; --t) {
             turn(s0, s1);
@@ -501,10 +505,14 @@ __global__ __launch_bounds__(64 * NM *NN, 2) void gemm_k(Args a, Epi e)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    *chunk(row, 8 * j + 2 * r + h) =
-                        float4{acc[j][i][4 * r], acc[j][i][4 * r + 1], acc[j][i][4 * r + 2],
-                               acc[j][i][4 * r + 3]};
+                for (int r = 0; r < 4; ++r) {
+                    float v[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        v[x] = PL == 3 ? acc[0][j][i][4 * r + x] + acc[kSums - 1][j][i][4 * r + x]
+                                       : acc[0][j][i][4 * r + x];
+                    *chunk(row, 8 * j + 2 * r + h) = float4{v[0], v[1], v[2], v[3]};
+                }
             __builtin_amdgcn_wave_barrier();
             if (part != nullptr) {
 #pragma unroll 1
@@ -634,7 +642,8 @@ __global__ __launch_bounds__(kThreads) void join_runs_k(Args a, int64_t G, Epi e
 }
 
 // Launches a planned product (gemm_plan.h); ws: part_bytes of the plan.
-template <bool TP, bool TQ, bool GATED, typename Epi>
+// PL: planes of the operands.
+template <int PL, bool TP, bool TQ, bool GATED, typename Epi>
 hipError_t launch(const Plan &pl, const Side &P, const Side &Q, int half, float *ws, const Epi &e,
                   hipStream_t st)
 {
@@ -647,7 +656,6 @@ hipError_t launch(const Plan &pl, const Side &P, const Side &Q, int half, float 
         a.M = p.first + p.rows;
         a.N = pl.N;
         a.K = pl.K;
-        a.kt = p.kt;
         a.steps = p.steps;
         a.per = p.per;
         a.first = p.first;
@@ -659,23 +667,27 @@ hipError_t launch(const Plan &pl, const Side &P, const Side &Q, int half, float 
         const uint32_t blocks = static_cast<uint32_t>(p.mt * p.nt);
         const dim3 grid(blocks, static_cast<uint32_t>(p.splits));
         if (p.tile == 256) {
-            // a block a compute unit, which goes through tiles
-            const uint32_t cus = static_cast<uint32_t>(device_cus());
-            HEX_LAUNCH((gemm_k<TP, TQ, 256, 256, 32, 2, 4, true, GATED, Epi>),
-                       dim3(p.splits == 0 || blocks > cus ? cus : blocks), dim3(512), 0, st, a, e);
-            if ((err = hipGetLastError()) == hipSuccess && p.splits == 0) {
-                HEX_LAUNCH((join_runs_k<256, GATED, Epi>),
-                           dim3(blocks * (256 * 256 / 8 / kThreads / (GATED ? 2 : 1))),
-                           dim3(kThreads), 0, st, a, cus, e);
-                err = hipGetLastError();
+            if constexpr (PL == 1) {
+                // a block a compute unit, which goes through tiles
+                const uint32_t cus = static_cast<uint32_t>(device_cus());
+                HEX_LAUNCH((gemm_k<1, TP, TQ, 256, 256, 32, 2, 4, true, GATED, Epi>),
+                           dim3(p.splits == 0 || blocks > cus ? cus : blocks), dim3(512), 0, st, a,
+                           e);
+                if ((err = hipGetLastError()) == hipSuccess && p.splits == 0) {
+                    HEX_LAUNCH((join_runs_k<256, GATED, Epi>),
+                               dim3(blocks * (256 * 256 / 8 / kThreads / (GATED ? 2 : 1))),
+                               dim3(kThreads), 0, st, a, cus, e);
+                    err = hipGetLastError();
+                }
             }
             continue;
         } else if (p.tile == 128) {
-            HEX_LAUNCH((gemm_k<TP, TQ, 128, 128, 32, 2, 2, false, GATED, Epi>), grid, dim3(256), 0,
-                       st, a, e);
+            HEX_LAUNCH((gemm_k<PL, TP, TQ, 128, 128, 32, 2, 2, false, GATED, Epi>), grid, dim3(256),
+                       0, st, a, e);
         } else {
-            HEX_LAUNCH((gemm_k<TP, TQ, 64, GATED ? 128 : 64, 64, 2, 2, false, GATED, Epi>), grid,
-                       dim3(256), 0, st, a, e);
+            HEX_LAUNCH((gemm_k<PL, TP, TQ, 64, GATED ? 128 : 64, PL == 3 ? 32 : 64, 2, 2, false,
+                               GATED, Epi>),
+                       grid, dim3(256), 0, st, a, e);
         }
         err = hipGetLastError();
         if (err != hipSuccess || p.splits == 1)

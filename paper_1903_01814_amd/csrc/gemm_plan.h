@@ -14,14 +14,14 @@ namespace gemm {
 struct Part {
     int tile;      // 256, 128 or 64 rows and columns
     int first, rows, mt, nt;
-    int kt, steps; // tiles of k, and of all products of planes
+    int steps;     // tiles of k
     int splits, per; // parts of the contraction, of so many steps; 0: runs of all tiles'
                      // steps, as many as compute units (256 only)
 };
 // D[M][N] over K, `planes` 1 or 3 (float32).  gated: N counts the columns of one
 // half, a tile has half its columns of each (64: all of each).
 struct Plan {
-    int M, N, K;
+    int M, N, K, planes;
     int64_t Np; // columns of the split sums
     int parts;
     Part part[2];

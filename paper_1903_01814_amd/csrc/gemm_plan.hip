@@ -11,12 +11,14 @@ namespace {
 // of several; us of a block's start and epilogue.  Measured over 1024 to 16384
 // tokens and 1024 to 8192 of k; the estimates below meet those times within 15 %.
 struct Tile {
-    int rows, cols, ks, per_cu;
+    int planes, rows, cols, ks, per_cu;
     double alone, each, fixed;
 };
-constexpr Tile kTiles[] = {{256, 256, 32, 1, 0.9, 0.9, 9.0},
-                           {128, 128, 32, 3, 0.32, 0.29, 5.0},
-                           {64, 64, 64, 3, 0.235, 0.17, 3.0}};
+constexpr Tile kTiles[] = {{1, 256, 256, 32, 1, 0.9, 0.9, 9.0},
+                           {1, 128, 128, 32, 3, 0.32, 0.29, 5.0},
+                           {1, 64, 64, 64, 3, 0.235, 0.17, 3.0},
+                           {3, 128, 128, 32, 1, 1.32, 1.32, 7.0},
+                           {3, 64, 64, 32, 2, 0.5, 0.46, 3.0}};
 
 // The unit with the most blocks decides; a split adds its sums' way through
 // memory and a launch.
@@ -55,6 +57,8 @@ double plan_rows(Part &best, int first, int rows, int N, int K, bool gated, int 
         }
     };
     for (const Tile &t : kTiles) {
+        if (t.planes != planes)
+            continue;
         Part p{};
         const int cols = gated && t.rows > 64 ? t.cols / 2 : t.cols;
         p.tile = t.rows;
@@ -62,8 +66,7 @@ double plan_rows(Part &best, int first, int rows, int N, int K, bool gated, int 
         p.rows = rows;
         p.mt = static_cast<int>((static_cast<int64_t>(rows) + t.rows - 1) / t.rows);
         p.nt = (N + cols - 1) / cols;
-        p.kt = (K + t.ks - 1) / t.ks;
-        p.steps = p.kt * (planes == 3 ? 6 : 1);
+        p.steps = (K + t.ks - 1) / t.ks;
         const int64_t blocks = static_cast<int64_t>(p.mt) * p.nt;
         p.splits = 1;
         p.per = p.steps;
@@ -97,6 +100,7 @@ Plan make_plan(int M, int N, int K, bool gated, int planes)
     pl.M = M;
     pl.N = N;
     pl.K = K;
+    pl.planes = planes;
     pl.Np = (N + 7) / 8 * 8;
     pl.parts = 1;
     double least = plan_rows(pl.part[0], 0, M, N, K, gated, planes);
@@ -104,6 +108,8 @@ Plan make_plan(int M, int N, int K, bool gated, int planes)
     // themselves: another launch, 2 us
     const int cus = device_cus();
     for (const Tile &t : kTiles) {
+        if (t.planes != planes)
+            continue;
         const int cols = gated && t.rows > 64 ? t.cols / 2 : t.cols;
         const int64_t nt = (N + cols - 1) / cols, mt = (static_cast<int64_t>(M) + t.rows - 1) / t.rows;
         const int64_t each = mt * nt / cus, rows = each * cus / nt * t.rows;
@@ -114,8 +120,7 @@ Plan make_plan(int M, int N, int K, bool gated, int planes)
         a.rows = static_cast<int>(rows);
         a.mt = static_cast<int>(rows / t.rows);
         a.nt = static_cast<int>(nt);
-        a.kt = (K + t.ks - 1) / t.ks;
-        a.steps = a.per = a.kt * (planes == 3 ? 6 : 1);
+        a.steps = a.per = (K + t.ks - 1) / t.ks;
         a.splits = 1;
         const double us = 2.0 + cost(a, t, pl.Np, gated, cus) +
                           plan_rows(b, a.rows, M - a.rows, N, K, gated, planes);

@@ -185,7 +185,7 @@ template <typename E, int ACT>
 hipError_t gated_product(const Plan &pl, const Side &W, const Side &X, float *ws, const FfnArgs &a,
                          hipStream_t st)
 {
-    return gemm::launch<false, false, true>(pl, W, X, static_cast<int>(round8(a.F)), ws,
+    return gemm::launch<sizeof(E) == 4 ? 3 : 1, false, false, true>(pl, W, X, static_cast<int>(round8(a.F)), ws,
                                             gated<E, ACT>(a), st);
 }
 template <typename E, int ACT> hipError_t gated_few(const FfnArgs &a, hipStream_t st)
@@ -198,7 +198,7 @@ template <typename E, int ACT>
 hipError_t gated_grad(const Plan &pl, const Side &W2, const Side &DY, float *ws, const void *gu,
                       bf16raw *d, int64_t Fp, int64_t plane, hipStream_t st)
 {
-    return gemm::launch<true, false, false>(
+    return gemm::launch<sizeof(E) == 4 ? 3 : 1, true, false, false>(
         pl, W2, DY, 0, ws, GatedGradEpi<E, ACT>{static_cast<const E *>(gu), d, Fp, plane}, st);
 }
 

@@ -131,8 +131,16 @@ hipError_t store_as(bool tall_q, const Plan &pl, const Side &P, const Side &Q, f
 {
     const bool vec = pl.N % 8 == 0 && ldy % (16 / static_cast<int64_t>(sizeof(O))) == 0;
     const StoreEpi<O> e{y, ldy, pl.N, map, vec};
-    return tall_q ? gemm::launch<true, true, false>(pl, P, Q, 0, ws, e, st)
-                  : gemm::launch<true, false, false>(pl, P, Q, 0, ws, e, st);
+    // operands in one plane or in three
+    if (pl.planes == 3) {
+        if constexpr (sizeof(O) == 4)
+            return tall_q ? gemm::launch<3, true, true, false>(pl, P, Q, 0, ws, e, st)
+                          : gemm::launch<3, true, false, false>(pl, P, Q, 0, ws, e, st);
+        else
+            return hipErrorInvalidValue; // float32 operands have float32 results
+    }
+    return tall_q ? gemm::launch<1, true, true, false>(pl, P, Q, 0, ws, e, st)
+                  : gemm::launch<1, true, false, false>(pl, P, Q, 0, ws, e, st);
 }
 
 } // namespace
@@ -160,7 +168,8 @@ template <typename E, int ACT>
 hipError_t product_of(const Plan &pl, const Side &W, const Side &X, float *ws, const Output &o,
                       hipStream_t st)
 {
-    return gemm::launch<false, false, false>(pl, W, X, 0, ws, epilogue<E, ACT>(o, pl.N), st);
+    return gemm::launch<sizeof(E) == 4 ? 3 : 1, false, false, false>(
+        pl, W, X, 0, ws, epilogue<E, ACT>(o, pl.N), st);
 }
 template <typename E, int ACT>
 hipError_t few_of(const few::Args &a, const Output &o, hipStream_t st)

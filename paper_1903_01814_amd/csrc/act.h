@@ -125,25 +125,34 @@ template <typename E> __device__ __forceinline__ void pack8(const float (&v)[8],
                          __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
     }
 }
+// the elements as they lie in memory, to be unpacked later
+template <typename E> struct Raw8 {
+    uint4 u[sizeof(E) / 2];
+};
+template <typename E, bool VEC> __device__ __forceinline__ Raw8<E> raw8(const E *p, int n)
+{
+    Raw8<E> r = {};
+    if (n >= 8) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int q = 0; q < static_cast<int>(sizeof(E) / 2); ++q)
+                r.u[q] = reinterpret_cast<const uint4 *>(p)[q];
+        } else {
+            __builtin_memcpy(r.u, p, sizeof(r.u)); // at any element
+        }
+    } else if (n > 0) {
+        E v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < n ? p[i] : E(0);
+        __builtin_memcpy(r.u, v, sizeof(v));
+    }
+    return r;
+}
 template <typename E, bool VEC>
 __device__ __forceinline__ void row8(const E *p, int n, float (&v)[8])
 {
-    constexpr int Q = sizeof(E) / 2;
-    if (n >= 8) {
-        uint4 u[Q];
-        if constexpr (VEC) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-                u[q] = reinterpret_cast<const uint4 *>(p)[q];
-        } else {
-            __builtin_memcpy(u, p, sizeof(u)); // at any element
-        }
-        unpack8<E>(u, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = i < n ? to_f(p[i]) : 0.f;
-    }
+    unpack8<E>(raw8<E, VEC>(p, n).u, v);
 }
 template <typename E, bool VEC>
 __device__ __forceinline__ void save_row8(E *p, int n, const float (&v)[8])

@@ -88,15 +88,17 @@ __global__ __launch_bounds__(kThreads) void col_sum_k(const E *x, int64_t ld, in
     part[blockIdx.y * static_cast<int64_t>(cols) + blockIdx.x * 64 + threadIdx.x] = t;
 }
 
+constexpr int kJoin = 1024;
 template <typename O>
-__global__ __launch_bounds__(kThreads) void col_join_k(const float *part, int slices, int cols,
-                                                       Halves map, O *out)
+__global__ __launch_bounds__(kJoin) void col_join_k(const float *part, int slices, int cols,
+                                                    Halves map, O *out)
 {
-    __shared__ float lds[16][17];
+    __shared__ float lds[kJoin / 16][17];
     const int c = blockIdx.x * 16 + threadIdx.x % 16, sub = threadIdx.x / 16;
     float t = 0.f;
     if (c < cols)
-        for (int s = sub; s < slices; s += 16)
+#pragma unroll 8
+        for (int s = sub; s < slices; s += kJoin / 16)
             t += part[static_cast<int64_t>(s) * cols + c];
     lds[sub][threadIdx.x % 16] = t;
     __syncthreads();
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void col_join_k(const float *part, int sl
         return;
     t = 0.f;
 #pragma unroll
-    for (int s = 0; s < 16; ++s)
+    for (int s = 0; s < kJoin / 16; ++s)
         t += lds[s][threadIdx.x % 16];
     out[to] = from_f<O>(t);
 }
@@ -165,10 +167,10 @@ hipError_t col_sum(const void *x, int64_t ld, int64_t plane, int planes, int64_t
         return e;
     const dim3 join(static_cast<uint32_t>((cols + 15) / 16));
     if (dst == F32)
-        HEX_LAUNCH((col_join_k<float>), join, dim3(kThreads), 0, st, part, slices, cols, map,
+        HEX_LAUNCH((col_join_k<float>), join, dim3(kJoin), 0, st, part, slices, cols, map,
                    static_cast<float *>(out));
     else
-        HEX_LAUNCH((col_join_k<bf16raw>), join, dim3(kThreads), 0, st, part, slices, cols, map,
+        HEX_LAUNCH((col_join_k<bf16raw>), join, dim3(kJoin), 0, st, part, slices, cols, map,
                    static_cast<bf16raw *>(out));
     return hipGetLastError();
 }

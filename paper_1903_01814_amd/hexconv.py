@@ -702,6 +702,20 @@ def _rows(t, name, dtype, n, cols):
     return t.data_ptr(), stride[0] if n > 1 else cols
 
 
+def _stream_on(stream, x, *others):
+    """The stream of a call on x's device, which has to be the current one and
+    that of every other tensor."""
+    torch = _torch()
+    d = x.get_device()
+    if d != torch.cuda.current_device():
+        raise ValueError("hexconv: tensors on device %d, the current one is %d"
+                         % (d, torch.cuda.current_device()))
+    for t in others:
+        if t is not None and t.get_device() != d:
+            raise ValueError("hexconv: tensors on devices %d and %d" % (d, t.get_device()))
+    return torch._C._cuda_getCurrentRawStream(d) if stream is None else _stream(stream)
+
+
 def _grad_dtype(ty, grads):
     """The one type of the weights' gradients that are given, float32 or ty."""
     torch = _torch()
@@ -720,7 +734,7 @@ def hexnorm_fwd(x, w, b, y, mean=None, rstd=None, eps: float = 1e-5, stream=None
     py, ldy = _rows(y, "y", ty, T, C)
     rc = load().hexnorm_fwd(px, _array(w, "w", ty, (C,)), _array(b, "b", ty, (C,)), py,
                             _array(mean, "mean", f32, (T,)), _array(rstd, "rstd", f32, (T,)), T, C,
-                            ldx, ldy, eps, dt, _stream(stream))
+                            ldx, ldy, eps, dt, _stream_on(stream, x, w, b, y, mean, rstd))
     _ok("hexnorm_fwd", rc)
     return y
 
@@ -741,7 +755,8 @@ def hexnorm_bwd(x, w, mean, rstd, dy, res, dx, dw, db, ws, stream=None):
     rc = load().hexnorm_bwd(px, _array(w, "w", ty, (C,)), _array(mean, "mean", f32, (T,)),
                             _array(rstd, "rstd", f32, (T,)), pg, pr, pd,
                             _array(dw, "dw", f32, (C,)), _array(db, "db", f32, (C,)), *_ws(ws), T, C,
-                            ldx, ldg, ldr, ldd, dt, _stream(stream))
+                            ldx, ldg, ldr, ldd, dt,
+                            _stream_on(stream, x, w, mean, rstd, dy, res, dx, dw, db, ws))
     _ok("hexnorm_bwd", rc)
     return dx, dw, db
 
@@ -761,7 +776,7 @@ def hexlinear_fwd(x, w, bias, res, y, z=None, ws=None, act: int = HEX_ACT_NONE, 
     py, ldy = _rows(y, "y", ty, M, N)
     rc = load().hexlinear_fwd(px, _array(w, "w", ty, (N, K)), _array(bias, "bias", ty, (N,)), pr,
                               py, _array(z, "z", ty, (M, N)), *_ws(ws), M, N, K, ldx, ldr, ldy, act,
-                              dt, _stream(stream))
+                              dt, _stream_on(stream, x, w, bias, res, y, z, ws))
     _ok("hexlinear_fwd", rc)
     return y
 
@@ -783,7 +798,7 @@ def hexlinear_bwd(x, w, z, dy, dx, dw, db, ws, act: int = HEX_ACT_NONE, stream=N
     rc = load().hexlinear_bwd(px, _array(w, "w", ty, (N, K)), _array(z, "z", ty, (M, N)), pg, pd,
                               _array(dw, "dw", gt, (N, K)), _array(db, "db", gt, (N,)), *_ws(ws), M,
                               N, K, ldx, ldg, ldd, act, dt if gt is ty else HEX_F32, dt,
-                              _stream(stream))
+                              _stream_on(stream, x, w, z, dy, dx, dw, db, ws))
     _ok("hexlinear_bwd", rc)
     return dx, dw, db
 
@@ -813,7 +828,8 @@ def hexffn_fwd(x, w1, b1, w2, b2, res, y, gu, h, ws=None, act: int = HEX_ACT_SIL
     rc = load().hexffn_fwd(px, _array(w1, "w1", ty, (2 * F, K)), _array(b1, "b1", ty, (2 * F,)),
                            _array(w2, "w2", ty, (N, F)), _array(b2, "b2", ty, (N,)), pr, py,
                            _array(gu, "gu", ty, (M, 2 * Fp)), _array(h, "h", ty, (M, Fp)), *_ws(ws),
-                           M, K, F, N, ldx, ldr, ldy, act, dt, _stream(stream))
+                           M, K, F, N, ldx, ldr, ldy, act, dt,
+                           _stream_on(stream, x, w1, b1, w2, b2, res, y, gu, h, ws))
     _ok("hexffn_fwd", rc)
     return y
 
@@ -838,6 +854,6 @@ def hexffn_bwd(x, w1, w2, gu, h, dy, dx, dw1, db1, dw2, db2, ws, act: int = HEX_
                            _array(dw1, "dw1", gt, (2 * F, K)), _array(db1, "db1", gt, (2 * F,)),
                            _array(dw2, "dw2", gt, (N, F)), _array(db2, "db2", gt, (N,)), *_ws(ws),
                            M, K, F, N, ldx, ldg, ldd, act, dt if gt is ty else HEX_F32, dt,
-                           _stream(stream))
+                           _stream_on(stream, x, w1, w2, gu, h, dy, dx, dw1, db1, dw2, db2, ws))
     _ok("hexffn_bwd", rc)
     return dx, dw1, db1, dw2, db2

@@ -1,5 +1,6 @@
-"""PyTorch layers over libhexconv: hexagonal convolution, pooling, and
-attention over lit pixels, as ``torch.autograd.Function``s and
+"""PyTorch layers over libhexconv: hexagonal convolution, pooling, attention
+over lit pixels, and the layer norms, projections and gated feed-forward blocks
+of a network over such tokens, as ``torch.autograd.Function``s and
 ``nn.Module``s, so that they drop into models written with the PyTorch API the
 way the paper's layers do (Sec. 2.4).
 
@@ -557,6 +558,294 @@ def hex_dropout(x, p, rng, residual=None, call=0):
     return HexDropoutFunction.apply(x, residual, float(p), rng, int(call))
 
 
+# ----------------------------------------- operators on tokens by themselves
+
+ACTIVATIONS = {None: hx.HEX_ACT_NONE, "relu": hx.HEX_ACT_RELU, "gelu": hx.HEX_ACT_GELU,
+               "silu": hx.HEX_ACT_SILU}
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError("hex: no activation %r, there are %s"
+                         % (name, ", ".join(map(repr, ACTIVATIONS))))
+    return ACTIVATIONS[name]
+
+
+def _matrix(x):
+    """x [..][features] as rows that the library takes: dense, 16-byte aligned, not
+    overlapping, less than 2^22 elements apart."""
+    m = x.reshape(-1, x.shape[-1])
+    n, c = m.shape
+    if (c > 1 and m.stride(1) != 1) or (n > 1 and not c <= m.stride(0) < 1 << 22):
+        return m.contiguous()
+    return m if m.data_ptr() % 16 == 0 else m.clone()
+
+
+def _aligned(*tensors):
+    """Weights as the library takes them: contiguous and 16-byte aligned."""
+    out = []
+    for t in tensors:
+        if t is not None:
+            t = t.contiguous()
+            t = t if t.data_ptr() % 16 == 0 else t.clone()
+        out.append(t)
+    return out
+
+
+def _keeps(*tensors):
+    """Whether a backward may follow."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _row_stride(m):
+    return m.stride(0) if m.shape[0] > 1 else m.shape[1]
+
+
+def _new(wanted, shape, like, dtype=None):
+    return _empty(shape, like, dtype) if wanted else None
+
+
+def _norm_fwd(x, w, b, eps, keep):
+    """Normed rows, and with keep their means and reciprocal deviations."""
+    y = _empty(x.shape, x)
+    mean, rstd = (_new(keep, x.shape[:1], x, torch.float32) for _ in range(2))
+    hx.hexnorm_fwd(x, w, b, y, mean, rstd, eps=eps)
+    return y, mean, rstd
+
+
+def _norm_bwd(x, w, b, mean, rstd, g, res):
+    """dx, and the weights' gradients in their dtype."""
+    T, C = x.shape
+    dx = _empty(x.shape, x)
+    dw, db = _new(w is not None, (C,), x, torch.float32), _new(b is not None, (C,), x, torch.float32)
+    ws = None
+    if dw is not None or db is not None:
+        ws = _workspace(hx.hexnorm_bwd_workspace(T, C, hx._dtype_code(x)), x)
+    hx.hexnorm_bwd(x, w, mean, rstd, g, res, dx, dw, db, ws)
+    return (dx, None if dw is None else dw.to(w.dtype), None if db is None else db.to(b.dtype))
+
+
+class HexLayerNormFunction(torch.autograd.Function):
+    """Layer norm of the rows of a matrix (hexnorm_fwd)."""
+
+    @staticmethod
+    def forward(ctx, x, w, b, eps, keep):
+        w, b = _aligned(w, b)
+        y, mean, rstd = _norm_fwd(x, w, b, eps, keep)
+        ctx.save_for_backward(x, w, b, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, g):
+        x, w, b, mean, rstd = ctx.saved_tensors
+        return _norm_bwd(x, w, b, mean, rstd, _matrix(g), None) + (None, None)
+
+
+class HexLinearFunction(torch.autograd.Function):
+    """act(x w^T + b) + residual of a matrix's rows (hexlinear_fwd)."""
+
+    @staticmethod
+    def forward(ctx, x, w, b, res, act, keep):
+        (M, K), N, code = x.shape, w.shape[0], hx._dtype_code(x)
+        w, b = _aligned(w, b)
+        y = _empty((M, N), x)
+        z = _new(keep and act != hx.HEX_ACT_NONE, (M, N), x)
+        ws = _workspace(hx.hexlinear_fwd_workspace(M, N, K, _row_stride(x), code), x)
+        hx.hexlinear_fwd(x, w, b, res, y, z, ws, act=act)
+        ctx.save_for_backward(x, w, z)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    def backward(ctx, g):
+        x, w, z = ctx.saved_tensors
+        need_x, need_w, need_b, need_res = ctx.needs_input_grad[:4]
+        g = _matrix(g)
+        (M, K), N = x.shape, w.shape[0]
+        dx, dw, db = _new(need_x, x.shape, x), _new(need_w, w.shape, w), _new(need_b, (N,), w)
+        ws = _workspace(hx.hexlinear_bwd_workspace(M, N, K, _row_stride(x), _row_stride(g), ctx.act,
+                                                   hx._dtype_code(x)), x)
+        hx.hexlinear_bwd(x, w, z, g, dx, dw, db, ws, act=ctx.act)
+        return dx, dw, db, g if need_res else None, None, None
+
+
+class HexFeedForwardFunction(torch.autograd.Function):
+    """Gated feed-forward block of a matrix's rows (hexffn_fwd), with a layer norm
+    before it (eps not None) and a residual: the rows themselves (res True) or none.
+    The gradients of the norm's input and of the residual are added in one pass."""
+
+    @staticmethod
+    def forward(ctx, x, nw, nb, w1, b1, w2, b2, res, eps, act, keep):
+        (M, K), (N, F), code = x.shape, w2.shape, hx._dtype_code(x)
+        nw, nb, w1, b1, w2, b2 = _aligned(nw, nb, w1, b1, w2, b2)
+        n, mean, rstd = (x, None, None) if eps is None else _norm_fwd(x, nw, nb, eps, keep)
+        Fp = hx.hexffn_width(F)
+        y, h, gu = _empty((M, N), x), _empty((M, Fp), x), _new(keep, (M, 2 * Fp), x)
+        ws = _workspace(hx.hexffn_fwd_workspace(M, K, F, N, _row_stride(n), code), x)
+        hx.hexffn_fwd(n, w1, b1, w2, b2, x if res else None, y, gu, h, ws, act=act)
+        if keep:
+            ctx.save_for_backward(x, nw, nb, n if n is not x else None, mean, rstd, w1, b1, w2, b2,
+                                  gu, h)
+        ctx.res, ctx.eps, ctx.act = res, eps, act
+        return y
+
+    @staticmethod
+    def backward(ctx, g):
+        x, nw, nb, n, mean, rstd, w1, b1, w2, b2, gu, h = ctx.saved_tensors
+        n = x if n is None else n
+        need = ctx.needs_input_grad
+        g = _matrix(g)
+        (M, K), (N, F) = n.shape, w2.shape
+        inner = need[0] or need[1] or need[2]
+        dn = _new(inner, n.shape, n)
+        dw1, db1 = _new(need[3], w1.shape, w1), _new(need[4], (2 * F,), w1)
+        dw2, db2 = _new(need[5], w2.shape, w2), _new(need[6], (N,), w2)
+        ws = _workspace(hx.hexffn_bwd_workspace(M, K, F, N, _row_stride(n), _row_stride(g),
+                                                hx._dtype_code(x)), x)
+        hx.hexffn_bwd(n, w1, w2, gu, h, g, dn, dw1, db1, dw2, db2, ws, act=ctx.act)
+        dnw = dnb = None
+        if ctx.eps is not None and inner:
+            dx, dnw, dnb = _norm_bwd(x, nw, nb, mean, rstd, dn, g if ctx.res else None)
+        elif need[0]:
+            dx = dn + g if ctx.res else dn
+        else:
+            dx = None
+        return dx, dnw, dnb, dw1, db1, dw2, db2, None, None, None, None
+
+
+def hex_layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last axis of x, weight and bias [features] or None."""
+    y = HexLayerNormFunction.apply(_matrix(x), weight, bias, float(eps), _keeps(x, weight, bias))
+    return y.view(x.shape)
+
+
+def hex_linear(x, weight, bias=None, residual=None, activation=None):
+    """activation(x weight^T + bias) + residual over the last axis of x: weight
+    [out, in], activation None, "relu", "gelu" or "silu"."""
+    shape = x.shape[:-1] + weight.shape[:1]
+    if residual is not None:
+        if residual.shape != shape:
+            raise ValueError("hex_linear: residual has shape %s, expected %s"
+                             % (tuple(residual.shape), tuple(shape)))
+        residual = _matrix(residual)
+    y = HexLinearFunction.apply(_matrix(x), weight, bias, residual, _activation(activation),
+                                _keeps(x, weight, bias, residual))
+    return y.view(shape)
+
+
+def hex_feed_forward(x, w1, w2, b1=None, b2=None, activation="silu", residual=False, norm=None):
+    """(activation(n w1[:F]^T + b1[:F]) (n w1[F:]^T + b1[F:])) w2^T + b2, plus x where
+    `residual` is true; n is x, or with norm = (weight, bias, eps) its layer norm."""
+    if residual and w2.shape[0] != x.shape[-1]:
+        raise ValueError("hex_feed_forward: a residual needs as many features out as in")
+    nw, nb, eps = (None, None, None) if norm is None else norm
+    y = HexFeedForwardFunction.apply(_matrix(x), nw, nb, w1, b1, w2, b2, bool(residual),
+                                     None if eps is None else float(eps), _activation(activation),
+                                     _keeps(x, nw, nb, w1, b1, w2, b2))
+    return y.view(x.shape[:-1] + w2.shape[:1])
+
+
+class HexLayerNorm(nn.Module):
+    """Layer norm over the last axis, of ``dim`` features."""
+
+    def __init__(self, dim, eps=1e-5, bias=True, device=None, dtype=None):
+        super().__init__()
+        kw = {"device": device, "dtype": dtype}
+        self.eps = float(eps)
+        self.weight = nn.Parameter(torch.ones(int(dim), **kw))
+        if bias:
+            self.bias = nn.Parameter(torch.zeros(int(dim), **kw))
+        else:
+            self.register_parameter("bias", None)
+
+    def forward(self, x):
+        return hex_layer_norm(x, self.weight, self.bias, self.eps)
+
+    def extra_repr(self):
+        return "%d, eps=%g, bias=%s" % (self.weight.shape[0], self.eps, self.bias is not None)
+
+
+class HexLinear(nn.Module):
+    """Projection over the last axis with an activation (None, "relu", "gelu",
+    "silu"); forward(x, residual=None) adds the residual in the same pass.
+    Initial weights and bias are uniform in +-1/sqrt(in_features)."""
+
+    def __init__(self, in_features, out_features, bias=True, activation=None, device=None,
+                 dtype=None):
+        super().__init__()
+        _activation(activation)
+        kw = {"device": device, "dtype": dtype}
+        self.activation = activation
+        self.weight = nn.Parameter(torch.empty((int(out_features), int(in_features)), **kw))
+        if bias:
+            self.bias = nn.Parameter(torch.empty(int(out_features), **kw))
+        else:
+            self.register_parameter("bias", None)
+        self.reset_parameters()
+
+    def reset_parameters(self):
+        with torch.no_grad():
+            bound = 1.0 / math.sqrt(self.weight.shape[1])
+            self.weight.uniform_(-bound, bound)
+            if self.bias is not None:
+                self.bias.uniform_(-bound, bound)
+
+    def forward(self, x, residual=None):
+        return hex_linear(x, self.weight, self.bias, residual, self.activation)
+
+    def extra_repr(self):
+        return "%d, %d, bias=%s, activation=%s" % (self.weight.shape[1], self.weight.shape[0],
+                                                   self.bias is not None, self.activation)
+
+
+class HexFeedForward(nn.Module):
+    """Gated feed-forward layer: x + dropout(down(act(gate n) up n)) with n the layer
+    norm of x (``norm`` False: x itself).  ``weight1`` holds the gate's rows, then
+    the other projection's.  Each token by itself: forward takes any leading axes, and
+    is its own form for single tokens."""
+
+    def __init__(self, dim, hidden, activation="silu", bias=False, norm=True, dropout=0.0, eps=1e-5,
+                 device=None, dtype=None):
+        super().__init__()
+        _activation(activation)
+        kw = {"device": device, "dtype": dtype}
+        dim, hidden = int(dim), int(hidden)
+        self.activation, self.dropout = activation, float(dropout)
+        self.norm = HexLayerNorm(dim, eps, **kw) if norm else None
+        self.weight1 = nn.Parameter(torch.empty((2 * hidden, dim), **kw))
+        self.weight2 = nn.Parameter(torch.empty((dim, hidden), **kw))
+        if bias:
+            self.bias1 = nn.Parameter(torch.empty(2 * hidden, **kw))
+            self.bias2 = nn.Parameter(torch.empty(dim, **kw))
+        else:
+            self.register_parameter("bias1", None)
+            self.register_parameter("bias2", None)
+        self.reset_parameters()
+
+    def reset_parameters(self):
+        with torch.no_grad():
+            for w, b in ((self.weight1, self.bias1), (self.weight2, self.bias2)):
+                bound = 1.0 / math.sqrt(w.shape[1])
+                w.uniform_(-bound, bound)
+                if b is not None:
+                    b.uniform_(-bound, bound)
+
+    def forward(self, x):
+        drop = self.training and self.dropout > 0
+        n = self.norm
+        y = hex_feed_forward(x, self.weight1, self.weight2, self.bias1, self.bias2, self.activation,
+                             not drop, None if n is None else (n.weight, n.bias, n.eps))
+        if not drop:
+            return y
+        rng = torch.empty(2, dtype=torch.int64, device=x.device).random_()
+        return hex_dropout(y, self.dropout, rng, residual=x)
+
+    def extra_repr(self):
+        return "%d, %d, activation=%s, bias=%s, dropout=%g" % (
+            self.weight2.shape[0], self.weight2.shape[1], self.activation, self.bias1 is not None,
+            self.dropout)
+
+
 class HexCache:
     """Keys and values of S streams, `capacity` tokens each, for
     HexPixelAttention.prefill and .step."""
@@ -617,14 +906,15 @@ class HexPixelAttention(nn.Module):
     heads, root-mean-square norm of every query and key head, rotation by
     positions of len(bases) axes, softmax attention (grouped heads), output
     projection, and with ``dropout`` the residual branch's dropout.  The
-    projections are torch's linear layers.
+    projections are torch's linear layers; with ``norm`` the branch starts with a
+    layer norm, and they are the library's, the residual added in the last one.
 
     forward(x [T][dim], pos, start): x + dropout(projection(attention(x))),
     the mask by torch's generator of x's device (torch.manual_seed).
     prefill and step do the same over a HexCache, without dropout."""
 
     def __init__(self, dim, heads, kv_heads=None, head_dim=None, bases=(10000.0, 100.0, 100.0),
-                 causal=False, dropout=0.0, eps=1e-6, device=None, dtype=None):
+                 causal=False, dropout=0.0, eps=1e-6, norm=False, device=None, dtype=None):
         super().__init__()
         self.heads = (int(heads), int(kv_heads or heads))
         self.head_dim = int(head_dim or dim // heads)
@@ -633,6 +923,7 @@ class HexPixelAttention(nn.Module):
         kw = {"device": device, "dtype": dtype}
         self.qkv = nn.Linear(dim, (Hq + 2 * Hkv) * self.head_dim, bias=False, **kw)
         self.out = nn.Linear(Hq * self.head_dim, dim, bias=False, **kw)
+        self.norm = HexLayerNorm(dim, **kw) if norm else None
         self.q_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
         self.k_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
         self.bases = tuple(bases)
@@ -657,15 +948,23 @@ class HexPixelAttention(nn.Module):
 
     def _project(self, x):
         Hq, Hkv = self.heads
-        return self.qkv(x).view(-1, Hq + 2 * Hkv, self.head_dim)
+        qkv = self.qkv(x) if self.norm is None else hex_linear(self.norm(x), self.qkv.weight)
+        return qkv.view(-1, Hq + 2 * Hkv, self.head_dim)
+
+    def _leave(self, o, x):
+        """The output projection of o, and x."""
+        if self.norm is None:
+            return x + self.out(o)
+        return hex_linear(o, self.out.weight, residual=x)
 
     def forward(self, x, pos, start):
         o = HexPixelAttentionFunction.apply(self._project(x), self.q_norm, self.k_norm, pos,
                                             self.freq, self.axis, start, self.heads, self.eps,
                                             self.causal)
-        y = self.out(o.flatten(1))
         if not (self.training and self.dropout > 0):
-            return x + y
+            return self._leave(o.flatten(1), x)
+        y = self.out(o.flatten(1)) if self.norm is None else hex_linear(o.flatten(1),
+                                                                        self.out.weight)
         # both words from torch's generator of the device, as its own dropout
         # draws: who saves and restores that (activation checkpointing) gets the
         # same mask again, and a captured graph draws a new one in every replay
@@ -724,7 +1023,7 @@ class HexPixelAttention(nn.Module):
         o = _empty(qo.shape, qo)
         hx.hexattn_fwd(qo, cache.k, cache.v, o, None, q_start, cache.starts, k_len[:-1],
                        causal=self.causal)
-        return x + self.out(o.flatten(1))
+        return self._leave(o.flatten(1), x)
 
     @torch.no_grad()
     def step(self, x, pos, cache):
@@ -745,8 +1044,42 @@ class HexPixelAttention(nn.Module):
         ws = _workspace(hx.hexattn_step_workspace(S, n, *self.heads, self.head_dim, most,
                                                   hx._dtype_code(q)), q)
         hx.hexattn_step(q, cache.k, cache.v, o, ws, cache.start, cache.length, most)
-        return x + self.out(o.flatten(2))
+        return self._leave(o.flatten(2), x)
 
     def extra_repr(self):
         return ("heads=%d, kv_heads=%d, head_dim=%d, causal=%s, dropout=%g"
                 % (self.heads + (self.head_dim, self.causal, self.dropout)))
+
+
+class HexPixelBlock(nn.Module):
+    """A block of a network over packed lit pixels: x + attention(norm(x)), then x +
+    feed-forward(norm(x)), both with dropout in training.  ``hidden``: features
+    between the feed-forward's projections, 8/3 of ``dim`` rounded to whole vectors by
+    default.
+
+    forward, prefill and step as those of HexPixelAttention.  The feed-forward acts
+    on every token by itself, on those outside ``start`` and past a prompt's cut too."""
+
+    def __init__(self, dim, heads, kv_heads=None, head_dim=None, hidden=None,
+                 bases=(10000.0, 100.0, 100.0), causal=False, dropout=0.0, activation="silu",
+                 device=None, dtype=None):
+        super().__init__()
+        kw = {"device": device, "dtype": dtype}
+        hidden = (8 * int(dim) // 3 + 7) // 8 * 8 if hidden is None else hidden
+        self.attention = HexPixelAttention(dim, heads, kv_heads, head_dim, bases, causal, dropout,
+                                           norm=True, **kw)
+        self.feed_forward = HexFeedForward(dim, hidden, activation, dropout=dropout, **kw)
+
+    def forward(self, x, pos, start):
+        return self.feed_forward(self.attention(x, pos, start))
+
+    def new_cache(self, streams, capacity):
+        return self.attention.new_cache(streams, capacity)
+
+    @torch.no_grad()
+    def prefill(self, x, pos, start, cache, longest):
+        return self.feed_forward(self.attention.prefill(x, pos, start, cache, longest))
+
+    @torch.no_grad()
+    def step(self, x, pos, cache):
+        return self.feed_forward(self.attention.step(x, pos, cache))

@@ -458,3 +458,132 @@ def test_chain_repeats_and_replays(T, K, F, dt):
     torch.cuda.synchronize()
     for n in want:
         assert torch.equal(out[n], other[n]), n
+
+
+# ------------------------------------------------- sizes of whole training batches
+
+def big64(a, b, chunk=2048):
+    """a b^T in float64 on the device, and the sum of its terms' magnitudes."""
+    out, mag = (torch.empty(a.shape[0], b.shape[0], dtype=torch.float64, device="cuda")
+                for _ in range(2))
+    bt, ba = b.double().t().contiguous(), b.double().abs().t().contiguous()
+    for i in range(0, a.shape[0], chunk):
+        x = a[i:i + chunk].double()
+        out[i:i + chunk], mag[i:i + chunk] = x @ bt, x.abs() @ ba
+    return out, mag
+
+
+def near_big(got, want, mag, n, dt, what):
+    err = (got.double() - want).abs()
+    bound = ref.acc(n) * mag + ref.R[dt] * want.abs()
+    bad = err > bound
+    assert not bool(bad.any()), "%s: %d off, worst %.3g of its bound" % (
+        what, int(bad.sum()), float((err / bound).max()))
+
+
+@pytest.mark.parametrize("T,N,K,dt", [
+    (8500, 2300, 1000, "bf16"),   # large tiles, a rest of rows, part of a tile of k
+    (4100, 2050, 2030, "bf16"),   # odd features, laid out before
+    (20000, 1032, 1016, "bf16"),  # the contraction of dw shared by all units
+    (2100, 1000, 2088, "f32"),
+    (9000, 520, 300, "f32"),
+])
+def test_linear_large(T, N, K, dt):
+    """Every row and column of products whose blocks go through large tiles and
+    share the contraction in runs."""
+    torch_mod()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    ty = tdtype(dt)
+    mk = lambda *s, k=1.0: (torch.randn(s, generator=g, device="cuda") * k).to(ty)  # noqa: E731
+    x, w, r, dy = mk(T, K), mk(N, K, k=K ** -0.5), mk(T, N), mk(T, N)
+    y, dx, dw, db = nan(T, N, dt=dt), nan(T, K, dt=dt), nan(N, K, dt=dt), nan(N, dt=dt)
+    code = hx._dtype_code(x)
+    hx.hexlinear_fwd(x, w, None, r, y, None, space(hx.hexlinear_fwd_workspace(T, N, K, K, code)))
+    hx.hexlinear_bwd(x, w, None, dy, dx, dw, db,
+                     space(hx.hexlinear_bwd_workspace(T, N, K, K, N, 0, code)))
+    z, mag = big64(x, w)
+    near_big(y, z + r.double(), mag + r.double().abs(), K, dt, "y")
+    near_big(dx, *big64(dy, w.t().contiguous()), N, dt, "dx")
+    near_big(dw, *big64(dy.t().contiguous(), x.t().contiguous()), T, dt, "dw")
+    near_big(db, dy.double().sum(0), dy.double().abs().sum(0), T, dt, "db")
+    del z, mag
+
+
+@pytest.mark.parametrize("T,K,F", [(8300, 1000, 1500), (5000, 520, 2731)])
+def test_ffn_large(T, K, F):
+    """The gated product and its gradient over large tiles, bfloat16: every h within
+    its bound; the other results by the norm of their errors, which are independent
+    roundings."""
+    torch_mod()
+    g = torch.Generator(device="cuda").manual_seed(F)
+    mk = lambda *s, k=1.0: (torch.randn(s, generator=g, device="cuda") * k).bfloat16()  # noqa: E731
+    x, w1, w2, dy = mk(T, K), mk(2 * F, K, k=K ** -0.5), mk(K, F, k=F ** -0.5), mk(T, K)
+    Fp, code = hx.hexffn_width(F), hx._dtype_code(x)
+    y, h, gu = nan(T, K, dt="bf16"), nan(T, Fp, dt="bf16"), nan(T, 2 * Fp, dt="bf16")
+    hx.hexffn_fwd(x, w1, None, w2, None, x, y, gu, h, space(hx.hexffn_fwd_workspace(T, K, F, K, K, code)))
+    dx, dw1, dw2 = nan(T, K, dt="bf16"), nan(2 * F, K, dt="bf16"), nan(K, F, dt="bf16")
+    hx.hexffn_bwd(x, w1, w2, gu, h, dy, dx, dw1, None, dw2, None,
+                  space(hx.hexffn_bwd_workspace(T, K, F, K, K, K, code)))
+    z, mag = big64(x, w1)
+    a, s = ref.act(z[:, :F], "silu")
+    h64 = a * z[:, F:]
+    eg = ref.acc(K) * mag + 1e-6 * z.abs()
+    lim = (1.2 * (eg[:, :F] * z[:, F:].abs() + a.abs() * eg[:, F:]) + ref.R["bf16"] * h64.abs() +
+           2.0 ** -22 * h64.abs())
+    assert bool(((h[:, :F].double() - h64).abs() <= lim).all())
+    assert not bool(h[:, F:].any())
+    rel = lambda p, q: float((p.double() - q).norm() / q.norm())  # noqa: E731
+    # a rounding is 2^-8 / sqrt 3 of a value at the low end of a step, half that at the
+    # high end: 1.7e-3 of a norm; two of them 2.4e-3, kept g and u 2.5e-4 more
+    y64 = h64 @ w2.double().t().contiguous() + x.double()
+    assert rel(y, y64) <= 2.5e-3
+    dh = dy.double() @ w2.double()
+    dz = torch.cat([dh * z[:, F:] * s, dh * a], 1)
+    assert rel(dx, dz @ w1.double()) <= 2.6e-3
+    assert rel(dw1, dz.t().contiguous() @ x.double()) <= 2.6e-3
+    assert rel(dw2, dy.double().t().contiguous() @ h64) <= 2.6e-3
+
+
+@pytest.mark.parametrize("scale", [1e-7, 1e4, 1e9])
+@pytest.mark.parametrize("T", [5, 200])
+def test_ffn_magnitudes(T, scale):
+    """g and u far outside float16's exponents: kept as bfloat16, to 2^-7."""
+    torch_mod()
+    g = torch.Generator().manual_seed(3)
+    x64, x = normal(g, T, 40, dt="bf16", std=scale)
+    w164, w1 = normal(g, 2 * 72, 40, dt="bf16", std=0.15)
+    w264, w2 = normal(g, 40, 72, dt="bf16", std=0.1)
+    dy64, dy = normal(g, T, 40, dt="bf16")
+    z = lambda *s: torch.zeros(s, dtype=torch.float64)  # noqa: E731
+    want = ref.ffn(x64, w164, z(144), w264, z(40), z(T, 40), "silu", "bf16", dy64)
+    code = hx._dtype_code(x)
+    y, gu, h = nan(T, 40, dt="bf16"), nan(T, 144, dt="bf16"), nan(T, 72, dt="bf16")
+    hx.hexffn_fwd(x, w1, None, w2, None, None, y, gu, h,
+                  space(hx.hexffn_fwd_workspace(T, 40, 72, 40, 40, code)))
+    got = {"dx": nan(T, 40, dt="bf16"), "dw1": nan(144, 40, dt="bf16"), "dw2": nan(40, 72, dt="bf16")}
+    hx.hexffn_bwd(x, w1, w2, gu, h, dy, got["dx"], got["dw1"], None, got["dw2"], None,
+                  space(hx.hexffn_bwd_workspace(T, 40, 72, 40, 40, 40, code)))
+    got["y"] = y
+    for n in got:
+        near(got[n], want[n], n)
+
+
+@pytest.mark.parametrize("T", [6, 90])
+def test_ffn_keeps_tokens_apart(T):
+    """Infinities and NaN of a token reach no other, forward and in dx."""
+    torch_mod()
+    for dt in DTYPES:
+        a = run_ffn(T, 40, 64, 40, dt, bias=False, res=False)
+        x = a["x"].clone()
+        x[1, 3], x[T - 2, 0] = float("nan"), float("inf")
+        code = hx._dtype_code(x)
+        y, gu, h = torch.empty_like(a["y"]), torch.empty_like(a["gu"]), torch.empty_like(a["h"])
+        hx.hexffn_fwd(x, a["w1"], None, a["w2"], None, None, y, gu, h,
+                      space(hx.hexffn_fwd_workspace(T, 40, 64, 40, 40, code)))
+        dx = torch.empty_like(a["dx"])
+        hx.hexffn_bwd(x, a["w1"], a["w2"], gu, h, a["dy"], dx, None, None, None, None,
+                      space(hx.hexffn_bwd_workspace(T, 40, 64, 40, 40, 40, code)))
+        keep = [i for i in range(T) if i not in (1, T - 2)]
+        assert torch.equal(y[keep], a["y"][keep]) and torch.equal(dx[keep], a["dx"][keep])
+        assert torch.isnan(y[1]).all() and torch.isnan(dx[1]).all()
+        assert not torch.isfinite(y[T - 2]).all()

@@ -70,6 +70,7 @@ struct Args {
     float *part;     // split sums [split][M - first][Np], null where there is one; of
                      // runs, a tile each: number tile + block
     int64_t Np;
+    float *sums;     // split sums over k of Q, [split][M - first]
 };
 
 typedef const __attribute__((address_space(1))) void *GlobalPtr;
@@ -194,11 +195,13 @@ __device__ __forceinline__ void tile_of(int b, int mt, int nt, int &m, int &n)
 //   fetch(m, n)      what an element needs from memory
 //   done(m, n, v, cols, fetched)
 // GATED: done(m, f, g, u, ..), columns f of both halves.
+// Epi::kSums: sum(m, v) too, with the sums of Q over k (the gradient of a bias): a
+// product of ones by the operands that the first column of tiles reads anyway.
 // APART: the epilogue has LDS of its own, and a block goes on to further tiles,
 // whose first loads are under way during it.
 template <int PL, bool TP, bool TQ, int BM, int BN, int KS, int NM, int NN, bool APART, bool GATED,
           typename Epi>
-__global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gemm_k(Args a, Epi e)
+__global__ __launch_bounds__(64 * NM *NN, PL == 3 && BM == 64 && BN == 128 ? 1 : 2) void gemm_k(Args a, Epi e)
 {
     constexpr int NW = NM * NN, WM = BM / NM, WN = BN / NN, TM = WM / 32, TN = WN / 32;
     // a plane of P, then one of Q, and so on
@@ -341,10 +344,28 @@ __global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gem
         floatx16 &c = acc[PL == 3 && x > 0 ? 1 : 0][j][m];
         c = mma(fp[from][kP[x]][j], fq[from][kQ[x]][m], c);
     };
+    // the sums of Q over k, by the waves of the first columns
+    constexpr bool SUMS = Epi::kSums && !APART;
+    floatx16 total[SUMS ? TM : 1];
+    bool adding = false;
+    auto add_up = [&](int from) HEX_INLINE {
+        if constexpr (SUMS) {
+            if (adding) {
+                const __bf16 one = static_cast<__bf16>(1.f);
+                const bf16x8 ones = {one, one, one, one, one, one, one, one};
+#pragma unroll
+                for (int l = PL - 1; l >= 0; --l)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+                        total[i] = mma(ones, fq[from][l][i], total[i]);
+            }
+        }
+    };
     auto multiply = [&](int from) HEX_INLINE {
 #pragma unroll
         for (int i = 0; i < kProducts; ++i)
             multiply_one(from, i);
+        add_up(from);
     };
     // a tile in `here`, its first operands in registers; the next in `next` and the
     // one after it on their way
@@ -392,6 +413,7 @@ __global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gem
                     }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            add_up(s & 1);
         }
     };
     // Three tiles of k a turn of the loop; one or two before them where they are left
@@ -417,6 +439,12 @@ __global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gem
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
                     acc[x][j][i] = floatx16{};
+        if constexpr (SUMS) {
+            adding = wn == 0 && n0 == 0;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                total[i] = floatx16{};
+        }
         meet(fresh); // an epilogue's loads and stores are not counted
         if (tiles % 3 == 0) {
             load(s2);
@@ -487,6 +515,21 @@ __global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gem
                      : wave < kFirst ? s0 + wave * kSlice
                                      : s1 + (wave - kFirst) * kSlice;
         const int h = lane >> 5, row = lane & 31;
+        if constexpr (SUMS) {
+            if (adding && h == 0) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const int m = mw + 32 * i + row;
+                    if (m >= a.M)
+                        continue;
+                    if (a.part != nullptr)
+                        a.sums[blockIdx.y * static_cast<int64_t>(a.M - a.first) + m - a.first] =
+                            total[i][0];
+                    else
+                        e.sum(m, total[i][0]);
+                }
+            }
+        }
         const auto c = e.cols(in ? n : 0);
         auto chunk = [&](int r, int x) HEX_INLINE {
             return reinterpret_cast<float4 *>(mine +
@@ -567,8 +610,9 @@ __global__ __launch_bounds__(64 * NM *NN, PL == 3 && BN == 128 ? 1 : 2) void gem
 // Adds up the splits and does what the product's epilogue would have done;
 // a thread takes eight columns.
 template <bool GATED, typename Epi>
-__global__ __launch_bounds__(kThreads) void join_k(const float *part, int splits, int first,
-                                                   int rows, int N, int64_t Np, Epi e)
+__global__ __launch_bounds__(kThreads) void join_k(const float *part, const float *sums,
+                                                   int splits, int first, int rows, int N,
+                                                   int64_t Np, Epi e)
 {
     const int64_t per = (N + 7) / 8, at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     if (at >= rows * per)
@@ -596,6 +640,14 @@ __global__ __launch_bounds__(kThreads) void join_k(const float *part, int splits
         e.done(m, n, v, u, c);
     else
         e.done(m, n, v, c, f);
+    if constexpr (Epi::kSums) {
+        if (n == 0) {
+            float t = 0.f;
+            for (int s = 0; s < splits; ++s)
+                t += sums[s * static_cast<int64_t>(rows) + r];
+            e.sum(m, t);
+        }
+    }
 }
 
 // The same for tiles of T x T that several runs share (run b of G: the steps b all /
@@ -663,6 +715,7 @@ hipError_t launch(const Plan &pl, const Side &P, const Side &Q, int half, float 
         a.nt = p.nt;
         a.half = half;
         a.part = p.splits != 1 ? ws : nullptr;
+        a.sums = ws + static_cast<int64_t>(p.splits) * p.rows * pl.Np; // part_bytes has room
         a.Np = pl.Np;
         const uint32_t blocks = static_cast<uint32_t>(p.mt * p.nt);
         const dim3 grid(blocks, static_cast<uint32_t>(p.splits));
@@ -682,8 +735,9 @@ hipError_t launch(const Plan &pl, const Side &P, const Side &Q, int half, float 
             }
             continue;
         } else if (p.tile == 128) {
-            HEX_LAUNCH((gemm_k<PL, TP, TQ, 128, 128, 32, 2, 2, false, GATED, Epi>), grid, dim3(256),
-                       0, st, a, e);
+            // float32: twice the waves, which the sums leave registers for
+            HEX_LAUNCH((gemm_k<PL, TP, TQ, 128, 128, 32, PL == 3 ? 4 : 2, 2, false, GATED, Epi>),
+                       grid, dim3(PL == 3 ? 512 : 256), 0, st, a, e);
         } else {
             HEX_LAUNCH((gemm_k<PL, TP, TQ, 64, GATED ? 128 : 64, PL == 3 ? 32 : 64, 2, 2, false,
                                GATED, Epi>),
@@ -695,7 +749,8 @@ hipError_t launch(const Plan &pl, const Side &P, const Side &Q, int half, float 
         const int64_t items = static_cast<int64_t>(p.rows) * ((pl.N + 7) / 8);
         HEX_LAUNCH((join_k<GATED, Epi>),
                    dim3(static_cast<uint32_t>((items + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                   st, static_cast<const float *>(ws), p.splits, p.first, p.rows, pl.N, pl.Np, e);
+                   st, static_cast<const float *>(ws), static_cast<const float *>(a.sums), p.splits,
+                   p.first, p.rows, pl.N, pl.Np, e);
         err = hipGetLastError();
     }
     return err;

@@ -63,7 +63,8 @@ inline size_t sums(const Part &p, int64_t Np, bool gated)
         return 0;
     if (p.splits == 0)
         return (static_cast<size_t>(p.mt) * p.nt + device_cus()) * (256 * 256 * 4);
-    return static_cast<size_t>(p.splits) * p.rows * Np * (gated ? 2 : 1) * 4;
+    // and those of the rows alone
+    return static_cast<size_t>(p.splits) * p.rows * (Np * (gated ? 2 : 1) + 1) * 4;
 }
 
 // The best of one launch for these rows, by its estimated time.
@@ -156,6 +157,16 @@ inline Plan make_plan(int M, int N, int K, bool gated, int planes)
         }
     }
     return pl;
+}
+
+// Whether the product can give the sums of its rows' operand beside it: blocks that
+// go through tiles do not.
+inline bool gives_sums(const Plan &pl)
+{
+    for (int i = 0; i < pl.parts; ++i)
+        if (pl.part[i].tile == 256)
+            return false;
+    return true;
 }
 
 inline size_t part_bytes(const Plan &pl, bool gated)

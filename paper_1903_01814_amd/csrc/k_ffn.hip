@@ -88,6 +88,7 @@ template <typename E, int ACT> struct GatedEpi {
     E *gu, *h;
     int64_t Fp;
     int F;
+    static constexpr bool kSums = false;
     struct Cols {
         float g[8], u[8];
     };
@@ -140,6 +141,7 @@ template <typename E, int ACT> struct GatedGradEpi {
     const E *gu;
     bf16raw *d;
     int64_t Fp, plane;
+    static constexpr bool kSums = false;
     struct Nothing {};
     struct Fetched {
         float g[8], u[8];
@@ -281,18 +283,24 @@ size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt
                                     st)) != hipSuccess)
         return sp.used;
     if (g.dx != nullptr && (err = store_product(false, px, tall(W1, a.K), D, part, g.dx, g.lddx,
-                                                none, dt, st)) != hipSuccess)
+                                                nullptr, none, dt, st)) != hipSuccess)
         return sp.used;
-    if (g.dw1 != nullptr && (err = store_product(true, p1, tall(X, a.K), tall(D, W), part, g.dw1,
-                                                 a.K, halves, g.dwt, st)) != hipSuccess)
+    // the biases' gradients beside the weights' where those products can give them
+    const bool beside1 = g.dw1 != nullptr && gemm::gives_sums(p1);
+    const bool beside2 = g.dw2 != nullptr && gemm::gives_sums(p2);
+    if (g.dw1 != nullptr &&
+        (err = store_product(true, p1, tall(X, a.K), tall(D, W), part, g.dw1, a.K,
+                             beside1 ? g.db1 : nullptr, halves, g.dwt, st)) != hipSuccess)
         return sp.used;
-    if (g.dw2 != nullptr && (err = store_product(true, p2, tall(H, a.F), tall(DY, a.N), part,
-                                                 g.dw2, a.F, none, g.dwt, st)) != hipSuccess)
+    if (g.dw2 != nullptr &&
+        (err = store_product(true, p2, tall(H, a.F), tall(DY, a.N), part, g.dw2, a.F,
+                             beside2 ? g.db2 : nullptr, none, g.dwt, st)) != hipSuccess)
         return sp.used;
-    if (g.db1 != nullptr && (err = col_sum(d, W, plane, planes, a.M, W, halves, sums, g.db1, BF16,
-                                           g.dwt, st)) != hipSuccess)
+    if (g.db1 != nullptr && !beside1 &&
+        (err = col_sum(d, W, plane, planes, a.M, W, halves, sums, g.db1, BF16, g.dwt, st)) !=
+            hipSuccess)
         return sp.used;
-    if (g.db2 != nullptr)
+    if (g.db2 != nullptr && !beside2)
         err = col_sum(g.dy, g.lddy, 0, 1, a.M, a.N, none, sums, g.db2, dt, g.dwt, st);
     return sp.used;
 }

@@ -25,6 +25,7 @@ template <typename E, int ACT> struct LinearEpi {
     int64_t ldr, ldy;
     int N;
     bool vec; // N, ldr and ldy whole vectors
+    static constexpr bool kSums = false;
     struct Cols {
         float b[8];
     };
@@ -102,13 +103,15 @@ Side tall(const Side &s, int cols)
 
 namespace {
 
-// y = v in O; rows may skip those between two halves
-template <typename O> struct StoreEpi {
-    O *y;
+// y = v in O; rows may skip those between two halves.  SUMS: sums of the rows'
+// operand to `sums`.
+template <typename O, bool SUMS> struct StoreEpi {
+    O *y, *sums;
     int64_t ldy;
     int N;
     Halves map;
     bool vec;
+    static constexpr bool kSums = SUMS;
     struct Fetched {};
     __device__ __forceinline__ Nothing cols(int) const { return Nothing{}; }
     __device__ __forceinline__ Fetched fetch(int, int) const { return Fetched{}; }
@@ -123,34 +126,40 @@ template <typename O> struct StoreEpi {
         else
             save_row8<O, false>(p, N - n, v);
     }
+    __device__ __forceinline__ void sum(int m, float v) const
+    {
+        const int row = map.row(m);
+        if (row >= 0)
+            sums[row] = from_f<O>(v);
+    }
 };
 
-template <typename O>
+template <int PL, typename O>
 hipError_t store_as(bool tall_q, const Plan &pl, const Side &P, const Side &Q, float *ws, O *y,
-                         int64_t ldy, Halves map, hipStream_t st)
+                    int64_t ldy, O *sums, Halves map, hipStream_t st)
 {
     const bool vec = pl.N % 8 == 0 && ldy % (16 / static_cast<int64_t>(sizeof(O))) == 0;
-    const StoreEpi<O> e{y, ldy, pl.N, map, vec};
-    // operands in one plane or in three
-    if (pl.planes == 3) {
-        if constexpr (sizeof(O) == 4)
-            return tall_q ? gemm::launch<3, true, true, false>(pl, P, Q, 0, ws, e, st)
-                          : gemm::launch<3, true, false, false>(pl, P, Q, 0, ws, e, st);
-        else
-            return hipErrorInvalidValue; // float32 operands have float32 results
-    }
-    return tall_q ? gemm::launch<1, true, true, false>(pl, P, Q, 0, ws, e, st)
-                  : gemm::launch<1, true, false, false>(pl, P, Q, 0, ws, e, st);
+    if (tall_q && sums != nullptr)
+        return gemm::launch<PL, true, true, false>(
+            pl, P, Q, 0, ws, StoreEpi<O, true>{y, sums, ldy, pl.N, map, vec}, st);
+    const StoreEpi<O, false> e{y, nullptr, ldy, pl.N, map, vec};
+    return tall_q ? gemm::launch<PL, true, true, false>(pl, P, Q, 0, ws, e, st)
+                  : gemm::launch<PL, true, false, false>(pl, P, Q, 0, ws, e, st);
 }
 
 } // namespace
 
 // D = Q P stored as it is: Q wide (data gradient) or tall (weight gradient), P tall
 hipError_t store_product(bool tall_q, const Plan &pl, const Side &P, const Side &Q, float *ws,
-                         void *y, int64_t ldy, Halves map, Dtype dt, hipStream_t st)
+                         void *y, int64_t ldy, void *sums, Halves map, Dtype dt, hipStream_t st)
 {
-    return dt == F32 ? store_as(tall_q, pl, P, Q, ws, static_cast<float *>(y), ldy, map, st)
-                     : store_as(tall_q, pl, P, Q, ws, static_cast<bf16raw *>(y), ldy, map, st);
+    float *yf = static_cast<float *>(y), *sf = static_cast<float *>(sums);
+    if (pl.planes == 3) // float32 operands have float32 results
+        return dt == F32 ? store_as<3>(tall_q, pl, P, Q, ws, yf, ldy, sf, map, st)
+                         : hipErrorInvalidValue;
+    return dt == F32 ? store_as<1>(tall_q, pl, P, Q, ws, yf, ldy, sf, map, st)
+                     : store_as<1>(tall_q, pl, P, Q, ws, static_cast<bf16raw *>(y), ldy,
+                                   static_cast<bf16raw *>(sums), map, st);
 }
 
 namespace {
@@ -236,15 +245,16 @@ size_t linear_bwd(const LinearArgs &a, const LinearGrads &g, void *ws, bool run,
             jobs.job[jobs.n++] = j->job[0];
     if ((err = pack(jobs, dt, st)) != hipSuccess)
         return sp.used;
-    if (g.dx != nullptr &&
-        (err = store_product(false, px, tall(W, a.K), DZ, parts, g.dx, g.lddx, none, dt, st)) !=
-            hipSuccess)
+    if (g.dx != nullptr && (err = store_product(false, px, tall(W, a.K), DZ, parts, g.dx, g.lddx,
+                                                nullptr, none, dt, st)) != hipSuccess)
         return sp.used;
+    // db beside dw where that product can give it
+    const bool beside = g.dw != nullptr && gemm::gives_sums(pw);
     if (g.dw != nullptr &&
-        (err = store_product(true, pw, tall(X, a.K), tall(DZ, a.N), parts, g.dw, a.K, none, g.dwt,
-                             st)) != hipSuccess)
+        (err = store_product(true, pw, tall(X, a.K), tall(DZ, a.N), parts, g.dw, a.K,
+                             beside ? g.db : nullptr, none, g.dwt, st)) != hipSuccess)
         return sp.used;
-    if (g.db != nullptr) {
+    if (g.db != nullptr && !beside) {
         if (dzj.n > 0)
             err = col_sum(DZ.p, DZ.ld, DZ.plane, planes, a.M, a.N, none, sums, g.db, BF16, g.dwt, st);
         else

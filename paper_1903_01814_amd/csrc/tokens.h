@@ -99,9 +99,10 @@ hipError_t linear_product(const gemm::Plan &pl, const gemm::Side &W, const gemm:
 // of a few tokens, tensors as they are
 hipError_t linear_few(const void *w, const void *x, int64_t ldx, int M, int N, int K,
                       const Output &o, int act, Dtype dt, hipStream_t st);
-// y [map(m)] = Q P in dt: P tall, Q wide (data gradient) or tall (weight gradient)
+// y [map(m)] = Q P in dt: P tall, Q wide (data gradient) or tall (weight gradient);
+// sums[map(m)], where not null (Q tall, gemm::gives_sums), the sums of Q over k
 hipError_t store_product(bool tall_q, const gemm::Plan &pl, const gemm::Side &P,
-                         const gemm::Side &Q, float *ws, void *y, int64_t ldy, Halves map, Dtype dt,
-                         hipStream_t st);
+                         const gemm::Side &Q, float *ws, void *y, int64_t ldy, void *sums,
+                         Halves map, Dtype dt, hipStream_t st);
 
 } // namespace hexk

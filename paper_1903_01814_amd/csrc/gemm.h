@@ -622,31 +622,48 @@ __global__ __launch_bounds__(kThreads) void join_k(const float *part, const floa
     const float *p = part + r * width + n;
     const auto c = e.cols(n);
     const auto f = e.fetch(m, n);
-    float v[8] = {}, u[8] = {};
-    for (int s = 0; s < splits; ++s) {
-        float x[8];
-        row8<float, true>(p + s * all, 8, x);
+    float v[8] = {}, u[8] = {}, t = 0.f;
+    const bool adds = Epi::kSums && n == 0;
+    // W splits' loads go out together: one after another they cost a trip to memory each
+    auto add = [&](auto width_of, int s) HEX_INLINE {
+        constexpr int W = decltype(width_of)::value;
+        float x[W][8], w[GATED ? W : 1][8], y[W];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] += x[i];
-        if constexpr (GATED) {
-            row8<float, true>(p + s * all + Np, 8, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                u[i] += x[i];
+        for (int j = 0; j < W; ++j) {
+            row8<float, true>(p + (s + j) * all, 8, x[j]);
+            if constexpr (GATED)
+                row8<float, true>(p + (s + j) * all + Np, 8, w[j]);
+            if constexpr (Epi::kSums)
+                y[j] = adds ? sums[(s + j) * static_cast<int64_t>(rows) + r] : 0.f;
         }
-    }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] += x[j][i];
+                if constexpr (GATED)
+                    u[i] += w[j][i];
+            }
+            if constexpr (Epi::kSums)
+                t += y[j];
+        }
+    };
+    int s = 0;
+    for (; s + 8 <= splits; s += 8)
+        add(std::integral_constant<int, 8>{}, s);
+    if (splits & 4)
+        add(std::integral_constant<int, 4>{}, s), s += 4;
+    if (splits & 2)
+        add(std::integral_constant<int, 2>{}, s), s += 2;
+    if (splits & 1)
+        add(std::integral_constant<int, 1>{}, s);
     if constexpr (GATED)
         e.done(m, n, v, u, c);
     else
         e.done(m, n, v, c, f);
     if constexpr (Epi::kSums) {
-        if (n == 0) {
-            float t = 0.f;
-            for (int s = 0; s < splits; ++s)
-                t += sums[s * static_cast<int64_t>(rows) + r];
+        if (adds)
             e.sum(m, t);
-        }
     }
 }
 

@@ -614,10 +614,11 @@ __global__ __launch_bounds__(kThreads) void join_k(const float *part, const floa
                                                    int splits, int first, int rows, int N,
                                                    int64_t Np, Epi e)
 {
-    const int64_t per = (N + 7) / 8, at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (at >= rows * per)
-        return;
+    // (fewer than 2^32 threads: the planner's bound of the split sums)
+    const uint32_t per = (N + 7) / 8, at = blockIdx.x * kThreads + threadIdx.x;
     const int r = static_cast<int>(at / per), m = first + r, n = static_cast<int>(at % per) * 8;
+    if (r >= rows)
+        return;
     const int64_t width = (GATED ? 2 : 1) * Np, all = rows * width;
     const float *p = part + r * width + n;
     const auto c = e.cols(n);

@@ -19,11 +19,13 @@ template <typename E> __global__ __launch_bounds__(kThreads) void pack_k(PackJob
         ++j;
     }
     const PackJob &q = jobs.job[j];
-    const int64_t per = q.dld / 8, at = static_cast<int64_t>(b) * kThreads + threadIdx.x;
-    if (at >= per * q.drows)
+    // (fewer than 2^32 threads: check_linear and check_ffn)
+    const uint32_t per = static_cast<uint32_t>(q.dld / 8);
+    const uint32_t at = static_cast<uint32_t>(b) * kThreads + threadIdx.x, r = at / per;
+    const int64_t row = r;
+    if (row >= q.drows)
         return;
-    const int64_t row = at / per;
-    const int col = static_cast<int>(at - row * per) * 8;
+    const int col = static_cast<int>(at - r * per) * 8;
     int64_t from = row;
     bool in = row < q.rows;
     if (q.half > 0) {

@@ -694,7 +694,7 @@ def _rows(t, name, dtype, n, cols):
     if t is None:
         return None, cols
     shape, stride = t.shape, t.stride()
-    if t.dtype is not dtype or not t.is_cuda or len(shape) != 2 or shape != (n, cols):
+    if t.dtype is not dtype or not t.is_cuda or shape != (n, cols):
         _refuse(t, name, dtype, (n, cols))
     if cols > 1 and stride[1] != 1 and n > 0:
         raise ValueError("hexconv: the rows of %s must be dense" % name)
@@ -707,7 +707,8 @@ def _stream_on(stream, x, *others):
     that of every other tensor."""
     torch = _torch()
     d = x.get_device()
-    if d != torch.cuda.current_device():
+    # without torch.cuda.current_device's check for a device, 0.3 us a call
+    if d != torch._C._cuda_getDevice():
         raise ValueError("hexconv: tensors on device %d, the current one is %d"
                          % (d, torch.cuda.current_device()))
     for t in others:

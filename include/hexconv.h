@@ -467,14 +467,17 @@ int hexdropout(const void *x, const void *res, void *y, int64_t n, double p, con
  *    one product hands to the next once to bf16: z and dz of a projection; h, dg
  *    and du of a gated block, whose g and u keep 10 bits or more between 2^-14 and
  *    2^15 (7 where one of eight neighbours lies outside).
- *  - Float32 products take each operand as the sum of three bf16 numbers, as
- *    hexattn_fwd does: operands under 2^-110 lose bits; infinities, and values
- *    from 3.39e38 on, give NaN.
+ *  - Float32 products of more than 32 tokens take each operand as the sum of three
+ *    bf16 numbers, as hexattn_fwd does: operands under 2^-110 lose bits;
+ *    infinities, and values from 3.39e38 on, give NaN.  (Gradients always do.)
  *  - A row's results depend on that row alone (gradients of weights on all rows):
  *    what is not finite in one reaches no other.
  *  - Gradients of weights and biases of projections and gated blocks come in
  *    `dwt`, float32 or dt.
- *  - Results repeat bit for bit.  Outputs must not overlap inputs.
+ *  - Results repeat bit for bit; a bias's gradient may be summed in another order
+ *    where the weights' is not asked for beside it.  Outputs must not overlap inputs.
+ *  - A workspace belongs to one call until that has run: calls on two streams, and
+ *    graphs that may run side by side, need one each.
  */
 #define HEX_NORM_MAX_DIM 16384
 #define HEX_LINEAR_MAX_DIM (1 << 20)
@@ -552,8 +555,8 @@ size_t hexffn_fwd_workspace(int M, int K, int F, int N, int64_t ldx, hex_dtype d
  *   y = h w2^T + b2 + res
  * w1 [2F][K], b1 [2F], w2 [N][F], b2 [N]; b1, b2 and res [M][N] may be NULL.
  * h [M][hexffn_width(F)] is written; gu [M][2 hexffn_width(F)], g and u for the
- * backward in a form of the library's own, may be NULL.  ws: at least hexffn_fwd_workspace(...) bytes, NULL where
- * that is 0.
+ * backward in a form of the library's own, may be NULL.  ws: at least
+ * hexffn_fwd_workspace(...) bytes, NULL where that is 0.
  */
 int hexffn_fwd(const void *x, const void *w1, const void *b1, const void *w2, const void *b2,
                const void *res, void *y, void *gu, void *h, void *ws, size_t ws_bytes, int M, int K,

@@ -264,51 +264,67 @@ __global__ __launch_bounds__(kJoin) void norm_join_k(const float *part, int slot
         db[c - C] = t;
 }
 
-template <typename E, bool VEC, bool SUMS, int G, int NV>
+enum Pass { FWD, BWD, BWD_SUMS };
+
+template <typename E, bool VEC, Pass P, int G, int NV>
 hipError_t launch_one(const void *x, const void *w, const void *b, void *y, float *mean,
                       float *rstd, const void *dy, const void *res, void *dx, float *part,
-                      int blocks, const NormArgs &a, bool bwd, hipStream_t st)
+                      int blocks, const NormArgs &a, hipStream_t st)
 {
     const E *X = static_cast<const E *>(x), *W = static_cast<const E *>(w);
-    if (bwd)
-        HEX_LAUNCH((norm_bwd_k<E, G, NV, VEC, SUMS>), dim3(blocks), dim3(kThreads), 0, st, X, W,
-                   mean, rstd, static_cast<const E *>(dy), static_cast<const E *>(res),
-                   static_cast<E *>(dx), part, a);
-    else
+    if constexpr (P == FWD)
         HEX_LAUNCH((norm_fwd_k<E, G, NV, VEC>), dim3(blocks), dim3(kThreads), 0, st, X, W,
                    static_cast<const E *>(b), static_cast<E *>(y), mean, rstd, a);
+    else
+        HEX_LAUNCH((norm_bwd_k<E, G, NV, VEC, P == BWD_SUMS>), dim3(blocks), dim3(kThreads), 0, st,
+                   X, W, mean, rstd, static_cast<const E *>(dy), static_cast<const E *>(res),
+                   static_cast<E *>(dx), part, a);
     return hipGetLastError();
 }
 
-// Lanes and vectors of a row, by its length: whole waves from 512 elements on,
-// a block from 4096 on (2048: 256 lanes instead of 64 took as long).
-#define HEX_NORM_CASES(CALL)                                                                  \
-    do {                                                                                      \
-        if (a.C <= 64) return CALL(8, 1);                                                     \
-        if (a.C <= 128) return CALL(16, 1);                                                   \
-        if (a.C <= 256) return CALL(32, 1);                                                   \
-        if (a.C <= 512) return CALL(64, 1);                                                   \
-        if (a.C <= 1024) return CALL(64, 2);                                                  \
-        if (a.C <= 2048) return CALL(256, 1);                                                 \
-        if (a.C <= 4096) return CALL(256, 2);                                                 \
-        if (a.C <= 8192) return CALL(256, 4);                                                 \
-        return CALL(256, 8);                                                                  \
-    } while (0)
-
-int rows_at_a_time(int C)
-{
-    return C <= 64 ? 32 : C <= 128 ? 16 : C <= 256 ? 8 : C <= 1024 ? 4 : 1;
-}
-
-template <typename E, bool VEC, bool SUMS>
+// Lanes and vectors of a row, by its length: one vector of eight a lane up to a
+// wave, two up to 1024, then a block.  Half the lanes with twice the vectors, and
+// twice or four times the lanes, took in us, forward / backward:
+//   65536 x 128, bfloat16     8.8 / 15.2, half  8.9 / 15.6, twice 13.0 / 19.5
+//   51200 x 512              21.3 / 31.4, half 18.8 / 37.7, four times 49.6 / 70.9
+//   51200 x 1024             39.0 / 76.1,                   four times 68.5 / 99.7
+//   16384 x 2048             27.6 / 52.2, a wave 24.0 / 79.5
+//   16384 x 2048, float32    47.4 / 88.7, a wave 58.6 / 103.6
+// so bfloat16's forward takes half the lanes where that was the faster.
+template <typename E, bool VEC, Pass P>
 hipError_t launch(const void *x, const void *w, const void *b, void *y, float *mean, float *rstd,
                   const void *dy, const void *res, void *dx, float *part, int blocks,
-                  const NormArgs &a, bool bwd, hipStream_t st)
+                  const NormArgs &a, hipStream_t st)
 {
 #define HEX_NORM_CALL(G, NV)                                                                  \
-    launch_one<E, VEC, SUMS, G, NV>(x, w, b, y, mean, rstd, dy, res, dx, part, blocks, a, bwd, st)
-    HEX_NORM_CASES(HEX_NORM_CALL);
+    launch_one<E, VEC, P, G, NV>(x, w, b, y, mean, rstd, dy, res, dx, part, blocks, a, st)
+    constexpr bool HALF = P == FWD && sizeof(E) == 2;
+    if (a.C <= 64)
+        return HEX_NORM_CALL(8, 1);
+    if (a.C <= 128)
+        return HEX_NORM_CALL(16, 1);
+    if (a.C <= 256)
+        return HEX_NORM_CALL((HALF ? 16 : 32), (HALF ? 2 : 1));
+    if (a.C <= 512)
+        return HEX_NORM_CALL((HALF ? 32 : 64), (HALF ? 2 : 1));
+    if (a.C <= 1024)
+        return HEX_NORM_CALL(64, 2);
+    if (a.C <= 2048)
+        return HEX_NORM_CALL((HALF ? 64 : 256), (HALF ? 4 : 1));
+    if (a.C <= 4096)
+        return HEX_NORM_CALL(256, 2);
+    if (a.C <= 8192)
+        return HEX_NORM_CALL(256, 4);
+    return HEX_NORM_CALL(256, 8);
 #undef HEX_NORM_CALL
+}
+
+// rows of a block at a time, 256 / G of launch
+int rows_at_a_time(int C, bool half)
+{
+    if (half && C > 128)
+        return C <= 256 ? 16 : C <= 512 ? 8 : C <= 2048 ? 4 : 1;
+    return C <= 64 ? 32 : C <= 128 ? 16 : C <= 256 ? 8 : C <= 1024 ? 4 : 1;
 }
 
 template <typename E> bool rows_aligned(std::initializer_list<int64_t> lds)
@@ -323,13 +339,13 @@ template <typename E>
 hipError_t fwd(const void *x, const void *w, const void *b, void *y, float *mean, float *rstd,
                const NormArgs &a, hipStream_t st)
 {
-    const int64_t R = rows_at_a_time(a.C);
+    const int64_t R = rows_at_a_time(a.C, sizeof(E) == 2);
     const int blocks = static_cast<int>((a.T + R - 1) / R);
     if (rows_aligned<E>({a.ldx, a.ldy}))
-        return launch<E, true, true>(x, w, b, y, mean, rstd, nullptr, nullptr, nullptr, nullptr,
-                                     blocks, a, false, st);
-    return launch<E, false, true>(x, w, b, y, mean, rstd, nullptr, nullptr, nullptr, nullptr,
-                                  blocks, a, false, st);
+        return launch<E, true, FWD>(x, w, b, y, mean, rstd, nullptr, nullptr, nullptr, nullptr,
+                                    blocks, a, st);
+    return launch<E, false, FWD>(x, w, b, y, mean, rstd, nullptr, nullptr, nullptr, nullptr,
+                                 blocks, a, st);
 }
 
 template <typename E>
@@ -343,15 +359,15 @@ hipError_t bwd(const void *x, const void *w, const float *mean, const float *rst
     float *mu = const_cast<float *>(mean), *rs = const_cast<float *>(rstd);
     hipError_t e;
     if (sums)
-        e = vec ? launch<E, true, true>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part, blocks,
-                                        a, true, st)
-                : launch<E, false, true>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part, blocks,
-                                         a, true, st);
+        e = vec ? launch<E, true, BWD_SUMS>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part,
+                                            blocks, a, st)
+                : launch<E, false, BWD_SUMS>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part,
+                                             blocks, a, st);
     else
-        e = vec ? launch<E, true, false>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part, blocks,
-                                         a, true, st)
-                : launch<E, false, false>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part,
-                                          blocks, a, true, st);
+        e = vec ? launch<E, true, BWD>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part, blocks, a,
+                                       st)
+                : launch<E, false, BWD>(x, w, nullptr, nullptr, mu, rs, dy, res, dx, part, blocks,
+                                        a, st);
     if (e != hipSuccess || !sums)
         return e;
     HEX_LAUNCH((norm_join_k), dim3((2 * a.C + 15) / 16), dim3(kJoin), 0, st, part, blocks, a.C,
@@ -365,7 +381,7 @@ hipError_t bwd(const void *x, const void *w, const float *mean, const float *rst
 // fewer where there are not four turns of rows for each.
 int norm_bwd_blocks(int64_t T, int C)
 {
-    const int64_t turns = (T + rows_at_a_time(C) - 1) / rows_at_a_time(C);
+    const int64_t R = rows_at_a_time(C, false), turns = (T + R - 1) / R;
     const int64_t most = 4 * static_cast<int64_t>(device_cus());
     int64_t n = (turns + 3) / 4;
     return static_cast<int>(n > most ? most : n);

@@ -19,6 +19,7 @@ import math
 
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
 from . import hexconv as hx
 
@@ -636,6 +637,7 @@ class HexLayerNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         x, w, b, mean, rstd = ctx.saved_tensors
         return _norm_bwd(x, w, b, mean, rstd, _matrix(g), None) + (None, None)
@@ -657,6 +659,7 @@ class HexLinearFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         x, w, z = ctx.saved_tensors
         need_x, need_w, need_b, need_res = ctx.needs_input_grad[:4]
@@ -690,6 +693,7 @@ class HexFeedForwardFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         x, nw, nb, n, mean, rstd, w1, b1, w2, b2, gu, h = ctx.saved_tensors
         n = x if n is None else n

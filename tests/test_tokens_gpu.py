@@ -208,6 +208,15 @@ def test_linear_sizes(T, N, K, dt):
 
 
 @pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("N,K", [(24, 4096), (24, 4100), (4200, 264), (4199, 1033)])
+@pytest.mark.parametrize("T", [1, 8, 9, 16, 32, 33])
+def test_linear_few_tokens_of_long_rows(T, N, K, dt):
+    """Every number of waves that share the contraction, and both block heights."""
+    torch_mod()
+    run_linear(T, N, K, dt, act="silu")
+
+
+@pytest.mark.parametrize("dt", DTYPES)
 @pytest.mark.parametrize("act", sorted(ACTS))
 @pytest.mark.parametrize("T,N,K,pad", [(3, 48, 56, 0), (77, 40, 64, 8), (77, 41, 63, 5)])
 def test_linear_activations(T, N, K, pad, act, dt):

@@ -360,3 +360,16 @@ def test_layer_without_norm_is_as_it_was():
     o = hnn.HexPixelAttentionFunction.apply(layer.qkv(x).view(-1, 8, 16), layer.q_norm, layer.k_norm,
                                             pos, layer.freq, layer.axis, start, (4, 2), 1e-6, False)
     assert torch.equal(layer(x, pos, start), x + layer.out(o.flatten(1)))
+
+
+def test_second_derivatives_refused():
+    """The gradients' own gradients are not there: asked for, they raise."""
+    d = dict(device="cuda")
+    x = torch.randn(5, 8, requires_grad=True, **d)
+    w = torch.randn(8, 8, requires_grad=True, **d)
+    w1, w2 = (torch.randn(s, requires_grad=True, **d) for s in ((16, 8), (8, 8)))
+    for y in (hnn.hex_layer_norm(x, w[0]), hnn.hex_linear(x, w),
+              hnn.hex_feed_forward(x, w1, w2, norm=(None, None, 1e-5))):
+        gx, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            gx.sum().backward()

@@ -23,8 +23,8 @@ template <bool FINE> __device__ __forceinline__ float sigmoid(float z)
 // The normal distribution's function (1 + erf(z / sqrt 2)) / 2.  bfloat16: Abramowitz
 // and Stegun 7.1.26, erf(x) = 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1
 // + p x), off by 1.5e-7 at most, so that its tail keeps bfloat16's bits down to
-// 4e-5 (z = -4); a gelu output z phi is off by 6e-7 there, 2^-20.  It takes a
-// third of the library's instructions, in a product's epilogue.
+// 4e-5 (z = -4); a gelu output z phi is off by 6e-7 there, 2^-20.  In the epilogue of
+// 51200 x 1024 x 1024 it takes 11 of 141 us.
 template <bool FINE> __device__ __forceinline__ float normal_cdf(float z)
 {
     if constexpr (FINE) {

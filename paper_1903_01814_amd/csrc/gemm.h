@@ -19,11 +19,17 @@
 // fills 1 KB in lane order; the lanes choose what they load, so the 16-byte
 // chunks of each row lie permuted by the row's number, and neither form
 // of read meets bank conflicts).  Three tiles take turns: while one is multiplied
-// the next two are on their way (a load takes 0.5 to 1 us, a tile half of that:
-// with one tile ahead the matrix cores were busy 0.44 of the time).  The barrier
-// stands before a tile's last step of 16 k, whose operands are in registers by
-// then, so the next tile's first operands and the loads of a new tile are issued
-// under that step's products.
+// the next two are on their way (weight gradient 4096 x 4096 over 8192: 282 -> 238
+// us from one tile ahead to two).  The barrier stands before a tile's last step of
+// 16 k, whose operands are in registers by then, so the next tile's first operands
+// and the loads of a new tile are issued under that step's products.
+//
+// What bounds it: the matrix cores, by the share of the time that LDS gives them
+// operands.  bfloat16: 16384 x 2048 x 2048 123 us (1114 TFLOP/s), its data gradient
+// 116 (1181), 4096 x 4096 over 8192 203 (1351); float32 4096 x 4096 x 4096 194 to 221
+// TFLOP/s.  Few steps of k are bound by memory instead: 16384 x 512 x 512 in float32
+// takes 62 us, of which 37 are steps and the rest the first loads and the stores, which
+// all blocks make at the same time.
 #pragma once
 
 #include "act.h"
@@ -201,7 +207,9 @@ __device__ __forceinline__ void tile_of(int b, int mt, int nt, int &m, int &n)
 // whose first loads are under way during it.
 template <int PL, bool TP, bool TQ, int BM, int BN, int KS, int NM, int NN, bool APART, bool GATED,
           typename Epi>
-__global__ __launch_bounds__(64 * NM *NN, PL == 3 && BM == 64 && BN == 128 ? 1 : 2) void gemm_k(Args a, Epi e)
+__global__
+__launch_bounds__(64 * NM * NN, PL == 3 && BM == 64 && BN == 128 ? 1 : 2) void gemm_k(Args a,
+                                                                                  Epi e)
 {
     constexpr int NW = NM * NN, WM = BM / NM, WN = BN / NN, TM = WM / 32, TN = WN / 32;
     // a plane of P, then one of Q, and so on
@@ -272,7 +280,8 @@ __global__ __launch_bounds__(64 * NM *NN, PL == 3 && BM == 64 && BN == 128 ? 1 :
             },
             a.P.rows - n0, wave, lane);
         lq.set(
-            a.Q.ld, [&](int r) HEX_INLINE { return min(r, a.Q.rows - 1 - m0); }, a.Q.rows - m0, wave, lane);
+            a.Q.ld, [&](int r) HEX_INLINE { return min(r, a.Q.rows - 1 - m0); }, a.Q.rows - m0,
+            wave, lane);
         baseP = reinterpret_cast<const char *>(a.P.p + (TP ? n0 : n0 * a.P.ld));
         baseQ = reinterpret_cast<const char *>(a.Q.p + (TQ ? m0 : m0 * a.Q.ld));
         k = first;

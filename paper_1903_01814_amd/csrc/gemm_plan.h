@@ -31,8 +31,20 @@ struct Plan {
 namespace plan {
 
 // What a tile costs: us a step of k for one block on a compute unit, and for each
-// of several; us of a block's start and epilogue.  Measured over 1024 to 16384
-// tokens and 1024 to 8192 of k; the estimates below meet those times within 15 %.
+// of several; us of a block's start and epilogue.  Fitted to products of 1024 to 16384
+// tokens and 1024 to 8192 of k.  Of 18 products of 1027 to 16432 tokens and 104 to 1366
+// features the choice is the fastest of all tiles and splits, or within 8 %, but for
+// one (4108 x 256 over 683 in float32: 37 us by tiles of 64, 31 by 128 in three
+// splits).  What the rule chooses, in us with the packing (float32):
+//   16432 x 512 over 512      82 by 128 (and 64 for 48 rows), 89 by 128 alone, 89 by 64
+//   512 x 512 over 16432      82 by 128 in 15 splits, 390 in one, 111 by 64 at best
+//   1366 x 256 over 4108      43 by 64 in 5 splits, 66 in one, 109 by 128 in one
+//   1027 x 216 over 104       9.1 by 64, 13.4 by 128, 10.8 by 64 in two splits
+// and in bfloat16:
+//   3287 x 200 over 536       5.5 by 64, 8.2 by 128, 10.2 by 64 in two splits
+//   51200 x 1024 over 1024 (gelu, residual)  169 by 256 and 64 for the last rows, 178
+//                             by 128, 196 by 256 alone, 210 by 256 in runs
+//   2048 x 5464 over 16432    385 by 256 in runs, 444 without
 struct Tile {
     int planes, rows, cols, ks, per_cu;
     double alone, each, fixed;
@@ -47,7 +59,8 @@ constexpr Tile kTiles[] = {{1, 256, 256, 32, 1, 0.9, 0.9, 9.0},
 // memory and a launch.
 inline double cost(const Part &p, const Tile &t, int64_t Np, bool gated, int cus)
 {
-    const int64_t blocks = static_cast<int64_t>(p.mt) * p.nt * p.splits, n = (blocks + cus - 1) / cus;
+    const int64_t blocks = static_cast<int64_t>(p.mt) * p.nt * p.splits;
+    const int64_t n = (blocks + cus - 1) / cus;
     const double wide = gated && t.rows == 64 ? 2. : 1.; // 128 columns
     const int64_t rounds = (n + t.per_cu - 1) / t.per_cu;
     double us = wide * p.per * (n == 1 ? t.alone : fmax(t.alone, n * t.each)) + rounds * t.fixed;
@@ -136,7 +149,8 @@ inline Plan make_plan(int M, int N, int K, bool gated, int planes)
         if (t.planes != planes)
             continue;
         const int cols = gated && t.rows > 64 ? t.cols / 2 : t.cols;
-        const int64_t nt = (N + cols - 1) / cols, mt = (static_cast<int64_t>(M) + t.rows - 1) / t.rows;
+        const int64_t nt = (N + cols - 1) / cols;
+        const int64_t mt = (static_cast<int64_t>(M) + t.rows - 1) / t.rows;
         const int64_t each = mt * nt / cus, rows = each * cus / nt * t.rows;
         if (each < 1 || rows < t.rows || rows >= M)
             continue;

@@ -187,8 +187,8 @@ template <typename E, int ACT>
 hipError_t gated_product(const Plan &pl, const Side &W, const Side &X, float *ws, const FfnArgs &a,
                          hipStream_t st)
 {
-    return gemm::launch<sizeof(E) == 4 ? 3 : 1, false, false, true>(pl, W, X, static_cast<int>(round8(a.F)), ws,
-                                            gated<E, ACT>(a), st);
+    return gemm::launch<sizeof(E) == 4 ? 3 : 1, false, false, true>(
+        pl, W, X, static_cast<int>(round8(a.F)), ws, gated<E, ACT>(a), st);
 }
 template <typename E, int ACT> hipError_t gated_few(const FfnArgs &a, hipStream_t st)
 {

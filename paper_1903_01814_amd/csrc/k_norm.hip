@@ -140,7 +140,8 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_k(const E *x, const E *w, c
             const int c = col_of<G>(l, j), k = in ? a.C - c : 0, from = c < a.C ? c : 0;
             next.x[j] = raw8<E, VEC>(x + at * a.ldx + from, k);
             next.g[j] = raw8<E, VEC>(dy + at * a.ldy + from, k);
-            next.add[j] = raw8<E, VEC>(res != nullptr ? res + at * a.ldr + from : x, res != nullptr ? k : 0);
+            next.add[j] = raw8<E, VEC>(res != nullptr ? res + at * a.ldr + from : x,
+                                       res != nullptr ? k : 0);
         }
         next.mu = mean[at];
         next.r = rstd[at];

@@ -541,8 +541,9 @@ int hexlinear_bwd(const void *x, const void *w, const void *z, const void *dy, v
                   int64_t lddy, int64_t lddx, hex_act act, hex_dtype dwt, hex_dtype dt,
                   void *stream);
 
-/* Columns of h for F hidden features, F rounded up to a multiple of 8; gu has
- * twice as many (negative hex_status for F outside 1 .. HEX_LINEAR_MAX_DIM). */
+/* Columns of h for F hidden features: F rounded up to a multiple of 8, past 256 of
+ * 64; gu has twice as many (negative hex_status for F outside 1 ..
+ * HEX_LINEAR_MAX_DIM). */
 int hexffn_width(int F);
 
 /* Bytes of device workspace hexffn_fwd needs (may be 0; 0 for invalid

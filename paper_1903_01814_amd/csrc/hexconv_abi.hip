@@ -1411,7 +1411,7 @@ int hexffn_width(int F)
 {
     if (F < 1)
         return HEX_ERR_INVALID_ARG;
-    return F > HEX_LINEAR_MAX_DIM ? HEX_ERR_UNSUPPORTED : (F + 7) / 8 * 8;
+    return F > HEX_LINEAR_MAX_DIM ? HEX_ERR_UNSUPPORTED : hexk::ffn_width(F);
 }
 
 size_t hexffn_fwd_workspace(int M, int K, int F, int N, int64_t ldx, hex_dtype dt)

@@ -107,6 +107,7 @@ template <typename E, int ACT> struct GatedEpi {
                                          const Cols &c) const
     {
         constexpr bool FINE = sizeof(E) == 4;
+        constexpr float zeros[8] = {};
         const int k = F - f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -123,6 +124,11 @@ template <typename E, int ACT> struct GatedEpi {
             E *p = gu + static_cast<int64_t>(m) * 2 * Fp + f;
             Kept::save(p, g);
             Kept::save(p + Fp, u);
+            if (k <= 8)
+                for (int64_t c = 8; c < Fp - f; c += 8) {
+                    save_row8<E, true>(p + c, 8, zeros);
+                    save_row8<E, true>(p + Fp + c, 8, zeros);
+                }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -131,16 +137,20 @@ template <typename E, int ACT> struct GatedEpi {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 g[i] = i < k ? g[i] : 0.f;
-        save_row8<E, true>(h + static_cast<int64_t>(m) * Fp + f, 8, g);
+        E *p = h + static_cast<int64_t>(m) * Fp;
+        save_row8<E, true>(p + f, 8, g);
+        if (k <= 8)
+            for (int64_t c = f + 8; c < Fp; c += 8)
+                save_row8<E, true>(p + c, 8, zeros);
     }
 };
 
-// dg and du from dh, in bfloat16 or in three planes; in the columns F .. Fp - 1
-// dh, g and u are zeros, so dg and du are
+// dg and du from dh, in bfloat16 or in three planes, side by side; in the columns
+// from F to a whole vector dh, g and u are zeros, so dg and du are
 template <typename E, int ACT> struct GatedGradEpi {
     const E *gu;
     bf16raw *d;
-    int64_t Fp, plane;
+    int64_t Fp, F8, ldd, plane; // columns of half of gu, of d; rows of d
     static constexpr bool kSums = false;
     struct Nothing {};
     struct Fetched {
@@ -159,7 +169,7 @@ template <typename E, int ACT> struct GatedGradEpi {
                                          const Fetched &x) const
     {
         constexpr bool FINE = sizeof(E) == 4;
-        const int64_t at = static_cast<int64_t>(m) * 2 * Fp + f;
+        const int64_t at = static_cast<int64_t>(m) * ldd + f;
         float dg[8], du[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -170,10 +180,10 @@ template <typename E, int ACT> struct GatedGradEpi {
         }
         if constexpr (FINE) {
             save_planes(d + at, plane, dg);
-            save_planes(d + at + Fp, plane, du);
+            save_planes(d + at + F8, plane, du);
         } else {
             save_row8<bf16raw, true>(d + at, 8, dg);
-            save_row8<bf16raw, true>(d + at + Fp, 8, du);
+            save_row8<bf16raw, true>(d + at + F8, 8, du);
         }
     }
 };
@@ -181,7 +191,7 @@ template <typename E, int ACT> struct GatedGradEpi {
 template <typename E, int ACT> GatedEpi<E, ACT> gated(const FfnArgs &a)
 {
     return GatedEpi<E, ACT>{static_cast<const E *>(a.b1), static_cast<E *>(a.gu),
-                            static_cast<E *>(a.h), round8(a.F), a.F};
+                            static_cast<E *>(a.h), pitch(a.F), a.F};
 }
 template <typename E, int ACT>
 hipError_t gated_product(const Plan &pl, const Side &W, const Side &X, float *ws, const FfnArgs &a,
@@ -198,25 +208,30 @@ template <typename E, int ACT> hipError_t gated_few(const FfnArgs &a, hipStream_
 
 template <typename E, int ACT>
 hipError_t gated_grad(const Plan &pl, const Side &W2, const Side &DY, float *ws, const void *gu,
-                      bf16raw *d, int64_t Fp, int64_t plane, hipStream_t st)
+                      const Side &D, int F, hipStream_t st)
 {
     return gemm::launch<sizeof(E) == 4 ? 3 : 1, true, false, false>(
-        pl, W2, DY, 0, ws, GatedGradEpi<E, ACT>{static_cast<const E *>(gu), d, Fp, plane}, st);
+        pl, W2, DY, 0, ws,
+        GatedGradEpi<E, ACT>{static_cast<const E *>(gu), const_cast<bf16raw *>(D.p), pitch(F),
+                             round8(F), D.ld, D.plane},
+        st);
 }
 
 } // namespace
 
+int ffn_width(int F) { return static_cast<int>(pitch(F)); }
+
 size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err)
 {
     const int act = a.act, planes = dt == F32 ? 3 : 1;
-    const int64_t Fp = round8(a.F);
+    const int64_t Fp = pitch(a.F);
     const Output o{a.b2, a.res, a.y, nullptr, a.ldr, a.ldy};
     if (a.M <= few::kMost) {
         if (run && (err = HEX_BY_TYPE(gated_few, a, st)) == hipSuccess)
             err = linear_few(a.w2, a.h, Fp, a.M, a.N, a.F, o, ACT_NONE, dt, st);
         return 0;
     }
-    const Halves none{0, 0}, halves{a.F, static_cast<int>(Fp)};
+    const Halves none{0, 0}, halves{a.F, static_cast<int>(round8(a.F))};
     Space sp{static_cast<char *>(ws)};
     PackJobs jobs{}, late{};
     const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, none, sp, jobs);
@@ -238,9 +253,9 @@ size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt
                hipError_t &err)
 {
     const int planes = dt == F32 ? 3 : 1;
-    const int64_t Fp = round8(a.F);
-    const int W = static_cast<int>(2 * Fp);
-    const Halves none{0, 0}, halves{a.F, static_cast<int>(Fp)};
+    const int64_t Fp = pitch(a.F);
+    const int F8 = static_cast<int>(round8(a.F)), W = 2 * F8;
+    const Halves none{0, 0}, halves{a.F, F8};
     Space sp{static_cast<char *>(ws)};
     PackJobs dyj{}, w2j{}, w1j{}, xj{}, hj{};
     const Side DY = operand(g.dy, nullptr, 0, a.M, a.N, g.lddy, dt, none, sp, dyj);
@@ -248,9 +263,8 @@ size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt
     const Side W1 = operand(a.w1, nullptr, 0, 2 * a.F, a.K, a.K, dt, halves, sp, w1j);
     const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, none, sp, xj);
     const Side H = operand(a.h, nullptr, 0, a.M, static_cast<int>(Fp), Fp, dt, none, sp, hj);
-    const int64_t plane = static_cast<int64_t>(a.M) * W;
-    bf16raw *d = sp.take<bf16raw>(planes * plane);
-    const Side D{d, W, plane, a.M};
+    const int64_t ldd = pitch(W), plane = a.M * ldd;
+    const Side D{sp.take<bf16raw>(planes * plane), ldd, plane, a.M};
     const Plan ph = gemm::make_plan(a.M, a.F, a.N, false, planes);
     const Plan px = gemm::make_plan(a.M, a.K, W, false, planes);
     const Plan p1 = gemm::make_plan(W, a.K, a.M, false, planes);
@@ -279,8 +293,8 @@ size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt
     if ((err = pack(jobs, dt, st)) != hipSuccess || (err = pack(more, dt, st)) != hipSuccess)
         return sp.used;
     const int act = a.act;
-    if (inner && (err = HEX_BY_TYPE(gated_grad, ph, tall(W2, a.F), DY, part, a.gu, d, Fp, plane,
-                                    st)) != hipSuccess)
+    if (inner && (err = HEX_BY_TYPE(gated_grad, ph, tall(W2, a.F), DY, part, a.gu, D, a.F, st)) !=
+                     hipSuccess)
         return sp.used;
     if (g.dx != nullptr && (err = store_product(false, px, tall(W1, a.K), D, part, g.dx, g.lddx,
                                                 nullptr, none, dt, st)) != hipSuccess)
@@ -297,7 +311,7 @@ size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt
                              beside2 ? g.db2 : nullptr, none, g.dwt, st)) != hipSuccess)
         return sp.used;
     if (g.db1 != nullptr && !beside1 &&
-        (err = col_sum(d, W, plane, planes, a.M, W, halves, sums, g.db1, BF16, g.dwt, st)) !=
+        (err = col_sum(D.p, ldd, plane, planes, a.M, W, halves, sums, g.db1, BF16, g.dwt, st)) !=
             hipSuccess)
         return sp.used;
     if (g.db2 != nullptr && !beside2)

@@ -87,7 +87,7 @@ Side operand(const void *src, const void *z, int act, int rows, int cols, int64_
     if (act == ACT_NONE && map.half == map.halfp && ready(cols, ld, dt))
         return Side{static_cast<const bf16raw *>(src), ld, 0, rows};
     const int planes = dt == F32 ? 3 : 1;
-    const int64_t dld = round8(cols);
+    const int64_t dld = pitch(cols);
     const int64_t drows = map.half > 0 ? 2 * static_cast<int64_t>(map.halfp) : rows;
     bf16raw *dst = ws.take<bf16raw>(planes * drows * dld);
     PackJob &q = jobs.job[jobs.n++];

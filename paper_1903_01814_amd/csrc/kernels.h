@@ -384,6 +384,7 @@ struct FfnGrads {
     int64_t lddy, lddx;
     Dtype dwt;
 };
+int ffn_width(int F); // columns of h
 size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err);
 size_t ffn_bwd(const FfnArgs &a, const FfnGrads &g, void *ws, bool run, Dtype dt, hipStream_t st,
                hipError_t &err);

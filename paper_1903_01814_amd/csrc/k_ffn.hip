@@ -221,6 +221,11 @@ hipError_t gated_grad(const Plan &pl, const Side &W2, const Side &DY, float *ws,
 
 int ffn_width(int F) { return static_cast<int>(pitch(F)); }
 
+// From so many tokens on w2 is copied to rows that begin on cache lines, as h's do:
+// the forward of 4096 tokens, 1024 and 2736 features 98 us without and 102 with it, of
+// 16384, 512 and 1368 104 and 103, of 16432, 2048 and 5464 1060 and 1025.
+constexpr int kCopy = 8192;
+
 size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err)
 {
     const int act = a.act, planes = dt == F32 ? 3 : 1;
@@ -236,7 +241,8 @@ size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, h
     PackJobs jobs{}, late{};
     const Side X = operand(a.x, nullptr, 0, a.M, a.K, a.ldx, dt, none, sp, jobs);
     const Side W1 = operand(a.w1, nullptr, 0, 2 * a.F, a.K, a.K, dt, halves, sp, jobs);
-    const Side W2 = operand(a.w2, nullptr, 0, a.N, a.F, a.F, dt, none, sp, jobs);
+    const bool copy = a.M >= kCopy && a.F != pitch(a.F);
+    const Side W2 = operand(a.w2, nullptr, 0, a.N, a.F, a.F, dt, none, sp, jobs, copy);
     const Side H = operand(a.h, nullptr, 0, a.M, static_cast<int>(Fp), Fp, dt, none, sp, late);
     const Plan p1 = gemm::make_plan(a.M, a.F, a.K, true, planes);
     const Plan p2 = gemm::make_plan(a.M, a.N, a.F, false, planes);

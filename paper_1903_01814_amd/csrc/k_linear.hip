@@ -82,9 +82,9 @@ bool ready(int64_t n, int64_t ld, Dtype dt) { return dt == BF16 && n % 8 == 0 &&
 // The operand of a tensor [rows][cols]: itself, or a place in the workspace and
 // the job that fills it.
 Side operand(const void *src, const void *z, int act, int rows, int cols, int64_t ld, Dtype dt,
-             Halves map, Space &ws, PackJobs &jobs)
+             Halves map, Space &ws, PackJobs &jobs, bool copy)
 {
-    if (act == ACT_NONE && map.half == map.halfp && ready(cols, ld, dt))
+    if (act == ACT_NONE && map.half == map.halfp && ready(cols, ld, dt) && !copy)
         return Side{static_cast<const bf16raw *>(src), ld, 0, rows};
     const int planes = dt == F32 ? 3 : 1;
     const int64_t dld = pitch(cols);

@@ -87,9 +87,10 @@ struct Side;
 }
 // The product's operand of a tensor [rows][cols]: itself, or (float32, rows of
 // parts of vectors, two halves that are, an activation's gradient) a place in the
-// workspace and the job that fills it.
+// workspace and the job that fills it.  copy: a place in any case, for rows that begin
+// on cache lines.
 gemm::Side operand(const void *src, const void *z, int act, int rows, int cols, int64_t ld, Dtype dt,
-                   Halves map, Space &ws, PackJobs &jobs);
+                   Halves map, Space &ws, PackJobs &jobs, bool copy = false);
 // its columns as the operand's rows
 gemm::Side tall(const gemm::Side &s, int cols);
 

@@ -13,8 +13,8 @@
 // products (bfloat16 32 k, float32 4), weights as the rows.  Tokens go in groups
 // of 16; rows past the last token are zeros.
 //
-// bfloat16, four tokens: 2048 x 2048 (8.4 MB) 4.9 us, 2 x 5464 x 2048 (45 MB) 13.3 (3.4
-// TB/s), 2048 x 5464 (22 MB) 7.6; the launch and the first load are 3 of each.
+// bfloat16, four tokens: 2048 x 2048 (8.4 MB) 5.0 us, 2 x 5464 x 2048 (45 MB) 11.9 (3.8
+// TB/s), 2048 x 5464 (22 MB) 7.2; the launch and the first load are 3 of each.
 #pragma once
 
 #include "act.h"

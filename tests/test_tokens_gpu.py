@@ -612,3 +612,81 @@ def test_ffn_keeps_tokens_apart(T):
         assert torch.equal(y[keep], a["y"][keep]) and torch.equal(dx[keep], a["dx"][keep])
         assert torch.isnan(y[1]).all() and torch.isnan(dx[1]).all()
         assert not torch.isfinite(y[T - 2]).all()
+
+
+# ------------------------------------------------- offsets that pass 32 bits
+
+FAR = (1 << 22) - 8  # the longest stride; 520 rows of it are 2^31 elements and more
+
+
+def far(t):
+    """t's rows a stride of FAR apart (what lies between them is not written)."""
+    v = torch.empty((t.shape[0], FAR), dtype=t.dtype, device="cuda")[:, :t.shape[1]]
+    return v.copy_(t)
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+def test_norm_far_rows(dt):
+    torch_mod()
+    T, C = 520, 72
+    g = torch.Generator().manual_seed(5)
+    (x64, x), (dy64, dy) = (normal(g, T, C, dt=dt) for _ in range(2))
+    (w64, w), (b64, b) = (normal(g, C, dt=dt) for _ in range(2))
+    want = ref.norm(x64, w64, b64, 1e-5, dt, dy64, zero((T, C)))
+    x, dy, y, dx = far(x), far(dy), far(nan(T, C, dt=dt)), far(nan(T, C, dt=dt))
+    mean, rstd, dw, db = nan(T), nan(T), nan(C), nan(C)
+    hx.hexnorm_fwd(x, w, b, y, mean, rstd)
+    hx.hexnorm_bwd(x, w, mean, rstd, dy, None, dx, dw, db,
+                   space(hx.hexnorm_bwd_workspace(T, C, hx._dtype_code(x))))
+    for name, got in (("y", y), ("dx", dx), ("dw", dw), ("db", db)):
+        near(got, want[name], name)
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("N,K", [(48, 64), (41, 63)])
+def test_linear_far_rows(N, K, dt):
+    torch_mod()
+    T = 520
+    g = torch.Generator().manual_seed(6)
+    x64, x = normal(g, T, K, dt=dt)
+    w64, w = normal(g, N, K, dt=dt, std=K ** -0.5)
+    r64, r = normal(g, T, N, dt=dt)
+    dy64, dy = normal(g, T, N, dt=dt)
+    want = ref.linear(x64, w64, zero((N,)), r64, "none", dt, dy64)
+    x, r, dy, y, dx = far(x), far(r), far(dy), far(nan(T, N, dt=dt)), far(nan(T, K, dt=dt))
+    code, dw, db = hx._dtype_code(x), nan(N, K, dt=dt), nan(N, dt=dt)
+    hx.hexlinear_fwd(x, w, None, r, y, None, space(hx.hexlinear_fwd_workspace(T, N, K, FAR, code)))
+    hx.hexlinear_bwd(x, w, None, dy, dx, dw, db,
+                     space(hx.hexlinear_bwd_workspace(T, N, K, FAR, FAR, 0, code)))
+    for name, got in (("y", y), ("dx", dx), ("dw", dw), ("db", db)):
+        near(got, want[name], name)
+
+
+def test_linear_far_rows_of_large_tiles():
+    """Offsets within a tile of 256 rows come near 2^32 bytes there."""
+    torch_mod()
+    T, N, K = 2048, 8192, 512
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, w = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((T, K), (N, K)))
+    xf, y = far(x), nan(T, N, dt="bf16")
+    hx.hexlinear_fwd(xf, w, None, None, y, None, space(hx.hexlinear_fwd_workspace(T, N, K, FAR, 1)))
+    value, mag = big64(x, w)
+    near_big(y, value, mag, K, "bf16", "y")
+
+
+def test_linear_output_past_32_bits():
+    """More than 2^31 elements of y and of dy; rows at both ends are compared."""
+    torch_mod()
+    T, N, K = 1050000, 2048, 8
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, w = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((T, K), (N, K)))
+    y = torch.empty((T, N), dtype=torch.bfloat16, device="cuda")
+    hx.hexlinear_fwd(x, w, None, None, y, None, space(hx.hexlinear_fwd_workspace(T, N, K, K, 1)))
+    dx = nan(T, K, dt="bf16")
+    hx.hexlinear_bwd(x, w, None, y, dx, None, None,
+                     space(hx.hexlinear_bwd_workspace(T, N, K, K, N, 0, 1)))
+    for rows in (slice(0, 300), slice(T - 700, T)):
+        value, mag = big64(x[rows], w)
+        near_big(y[rows], value, mag, K, "bf16", "y")
+        value, mag = big64(y[rows], w.t())
+        near_big(dx[rows], value, mag, N, "bf16", "dx")

@@ -194,3 +194,9 @@ def test_reference():
     got = ref.norm(x, ins[1].detach(), ins[2].detach(), 1e-3, "f32", gy, add)
     assert torch.allclose(got["y"][0], y.detach()) and torch.allclose(got["dx"][0], want[0] + add)
     assert torch.allclose(got["dw"][0], want[1]) and torch.allclose(got["db"][0], want[2])
+
+
+def test_ffn_width_whole_lines():
+    """Rows of h begin on cache lines past 256 columns."""
+    assert [hx.hexffn_width(f) for f in (1, 8, 250, 256, 257, 320, 683)] == [8, 8, 256, 256, 320,
+                                                                             320, 704]

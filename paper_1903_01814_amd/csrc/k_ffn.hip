@@ -10,8 +10,8 @@
 // round h, dg and du once to bfloat16, as operands of the products that follow, and g
 // and u where they are kept for the backward (below); h is made of unrounded ones.
 //
-// 16432 tokens, 2048 to 5464 to 2048 features, bfloat16: g, u and h 745 us (985
-// TFLOP/s), dg and du 535 (their product, 1.3 GB of g, u, dg and du besides), the
+// 16432 tokens, 2048 to 5464 to 2048 features, bfloat16: g, u and h 765 us (961
+// TFLOP/s), dg and du 564 (their product, 1.3 GB of g, u, dg and du besides), the
 // others as gemm.h says.  Made apart from its product, h would take another pass over g
 // and u, 0.36 GB.
 #include "few.h"

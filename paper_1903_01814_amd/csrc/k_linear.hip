@@ -144,8 +144,12 @@ hipError_t store_as(bool tall_q, const Plan &pl, const Side &P, const Side &Q, f
         return gemm::launch<PL, true, true, false>(
             pl, P, Q, 0, ws, StoreEpi<O, true>{y, sums, ldy, pl.N, map, vec}, st);
     const StoreEpi<O, false> e{y, nullptr, ldy, pl.N, map, vec};
-    return tall_q ? gemm::launch<PL, true, true, false>(pl, P, Q, 0, ws, e, st)
-                  : gemm::launch<PL, true, false, false>(pl, P, Q, 0, ws, e, st);
+    if (tall_q)
+        return gemm::launch<PL, true, true, false>(pl, P, Q, 0, ws, e, st);
+    if constexpr (PL == 1 && sizeof(O) == 4) // weights' gradients alone have another type
+        return hipErrorInvalidValue;
+    else
+        return gemm::launch<PL, true, false, false>(pl, P, Q, 0, ws, e, st);
 }
 
 } // namespace

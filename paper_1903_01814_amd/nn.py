@@ -918,7 +918,7 @@ class HexPixelAttention(nn.Module):
     prefill and step do the same over a HexCache, without dropout."""
 
     def __init__(self, dim, heads, kv_heads=None, head_dim=None, bases=(10000.0, 100.0, 100.0),
-                 causal=False, dropout=0.0, eps=1e-6, norm=False, device=None, dtype=None):
+                 causal=False, dropout=0.0, eps=1e-6, device=None, dtype=None, norm=False):
         super().__init__()
         self.heads = (int(heads), int(kv_heads or heads))
         self.head_dim = int(head_dim or dim // heads)

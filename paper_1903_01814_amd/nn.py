@@ -806,7 +806,8 @@ class HexFeedForward(nn.Module):
     """Gated feed-forward layer: x + dropout(down(act(gate n) up n)) with n the layer
     norm of x (``norm`` False: x itself).  ``weight1`` holds the gate's rows, then
     the other projection's.  Each token by itself: forward takes any leading axes, and
-    is its own form for single tokens."""
+    is its own form for single tokens.  forward(x, drop=False) leaves the dropout out in
+    training too, as serving does."""
 
     def __init__(self, dim, hidden, activation="silu", bias=False, norm=True, dropout=0.0, eps=1e-5,
                  device=None, dtype=None):
@@ -834,8 +835,8 @@ class HexFeedForward(nn.Module):
                 if b is not None:
                     b.uniform_(-bound, bound)
 
-    def forward(self, x):
-        drop = self.training and self.dropout > 0
+    def forward(self, x, drop=True):
+        drop = drop and self.training and self.dropout > 0
         n = self.norm
         y = hex_feed_forward(x, self.weight1, self.weight2, self.bias1, self.bias2, self.activation,
                              not drop, None if n is None else (n.weight, n.bias, n.eps))
@@ -1061,8 +1062,9 @@ class HexPixelBlock(nn.Module):
     between the feed-forward's projections, 8/3 of ``dim`` rounded to whole vectors by
     default.
 
-    forward, prefill and step as those of HexPixelAttention.  The feed-forward acts
-    on every token by itself, on those outside ``start`` and past a prompt's cut too."""
+    forward, prefill and step as those of HexPixelAttention, the latter two without
+    dropout.  The feed-forward acts on every token by itself, on those outside ``start``
+    and past a prompt's cut too."""
 
     def __init__(self, dim, heads, kv_heads=None, head_dim=None, hidden=None,
                  bases=(10000.0, 100.0, 100.0), causal=False, dropout=0.0, activation="silu",
@@ -1080,10 +1082,16 @@ class HexPixelBlock(nn.Module):
     def new_cache(self, streams, capacity):
         return self.attention.new_cache(streams, capacity)
 
+    def _serve(self, x):
+        ff = self.feed_forward
+        if isinstance(ff, HexFeedForward) and ff.training and ff.dropout > 0:
+            return ff(x, drop=False)
+        return ff(x)
+
     @torch.no_grad()
     def prefill(self, x, pos, start, cache, longest):
-        return self.feed_forward(self.attention.prefill(x, pos, start, cache, longest))
+        return self._serve(self.attention.prefill(x, pos, start, cache, longest))
 
     @torch.no_grad()
     def step(self, x, pos, cache):
-        return self.feed_forward(self.attention.step(x, pos, cache))
+        return self._serve(self.attention.step(x, pos, cache))

@@ -1,0 +1,30 @@
+"""The block of attention and feed-forward layer as it serves, on the GPU."""
+import pytest
+
+from gpu_helpers import torch_mod
+
+torch = pytest.importorskip("torch")
+hnn = pytest.importorskip("paper_1903_01814_amd.nn")
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_serving_in_training(dtype):
+    """A block with dropout that was not put in evaluation mode: prefill and steps have
+    the bits of evaluation."""
+    torch_mod()
+    torch.manual_seed(0)
+    b = hnn.HexPixelBlock(48, 4, 2, 16, hidden=72, causal=True, dropout=0.5, device="cuda",
+                          dtype=dtype)
+    x, pos = torch.randn(9, 48, device="cuda").to(dtype), torch.rand(9, 3, device="cuda")
+    new, at = torch.randn(2, 3, 48, device="cuda").to(dtype), torch.rand(2, 3, 3, device="cuda")
+    start = torch.tensor([0, 4, 9], dtype=torch.int32, device="cuda")
+    got = []
+    for mode in (True, False):
+        b.train(mode)
+        cache = b.new_cache(2, 12)
+        got.append([b.prefill(x, pos, start, cache, 5), b.step(new, at, cache)])
+    for u, v in zip(*got):
+        assert torch.equal(u, v)

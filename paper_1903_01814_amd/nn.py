@@ -802,12 +802,29 @@ class HexLinear(nn.Module):
                                                    self.bias is not None, self.activation)
 
 
+class _Projection(nn.Linear):
+    """torch's linear layer with the library's product."""
+
+    def forward(self, x):
+        return hex_linear(x, self.weight, self.bias)
+
+
+def _bare(module, kind):
+    """Whether a call of the module does what its class's forward does and nothing
+    else (hooks, a forward or a class of its own), so that it may be part of another
+    call."""
+    return (type(module) is kind and "forward" not in vars(module) and
+            not (module._forward_hooks or module._forward_pre_hooks or module._backward_hooks or
+                 module._backward_pre_hooks or nn.modules.module._has_any_global_hook()))
+
+
 class HexFeedForward(nn.Module):
     """Gated feed-forward layer: x + dropout(down(act(gate n) up n)) with n the layer
     norm of x (``norm`` False: x itself).  ``weight1`` holds the gate's rows, then
     the other projection's.  Each token by itself: forward takes any leading axes, and
     is its own form for single tokens.  forward(x, drop=False) leaves the dropout out in
-    training too, as serving does."""
+    training too, as serving does.  A norm with hooks, or another module in its place, is
+    called by itself."""
 
     def __init__(self, dim, hidden, activation="silu", bias=False, norm=True, dropout=0.0, eps=1e-5,
                  device=None, dtype=None):
@@ -837,11 +854,14 @@ class HexFeedForward(nn.Module):
 
     def forward(self, x, drop=True):
         drop = drop and self.training and self.dropout > 0
-        n = self.norm
-        y = hex_feed_forward(x, self.weight1, self.weight2, self.bias1, self.bias2, self.activation,
-                             not drop, None if n is None else (n.weight, n.bias, n.eps))
+        norm, apart = self.norm, False
+        if norm is not None:
+            apart = not _bare(norm, HexLayerNorm)
+            norm = None if apart else (norm.weight, norm.bias, norm.eps)
+        y = hex_feed_forward(self.norm(x) if apart else x, self.weight1, self.weight2, self.bias1,
+                             self.bias2, self.activation, not (drop or apart), norm)
         if not drop:
-            return y
+            return x + y if apart else y
         rng = torch.empty(2, dtype=torch.int64, device=x.device).random_()
         return hex_dropout(y, self.dropout, rng, residual=x)
 
@@ -912,7 +932,8 @@ class HexPixelAttention(nn.Module):
     positions of len(bases) axes, softmax attention (grouped heads), output
     projection, and with ``dropout`` the residual branch's dropout.  The
     projections are torch's linear layers; with ``norm`` the branch starts with a
-    layer norm, and they are the library's, the residual added in the last one.
+    layer norm, and their products are the library's, the residual added in the last
+    one (apart, where that has hooks or another module is in its place).
 
     forward(x [T][dim], pos, start): x + dropout(projection(attention(x))),
     the mask by torch's generator of x's device (torch.manual_seed).
@@ -926,8 +947,9 @@ class HexPixelAttention(nn.Module):
         self.causal, self.dropout, self.eps = bool(causal), float(dropout), float(eps)
         Hq, Hkv = self.heads
         kw = {"device": device, "dtype": dtype}
-        self.qkv = nn.Linear(dim, (Hq + 2 * Hkv) * self.head_dim, bias=False, **kw)
-        self.out = nn.Linear(Hq * self.head_dim, dim, bias=False, **kw)
+        linear = _Projection if norm else nn.Linear
+        self.qkv = linear(dim, (Hq + 2 * Hkv) * self.head_dim, bias=False, **kw)
+        self.out = linear(Hq * self.head_dim, dim, bias=False, **kw)
         self.norm = HexLayerNorm(dim, **kw) if norm else None
         self.q_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
         self.k_norm = nn.Parameter(torch.ones(self.head_dim, **kw))
@@ -953,14 +975,15 @@ class HexPixelAttention(nn.Module):
 
     def _project(self, x):
         Hq, Hkv = self.heads
-        qkv = self.qkv(x) if self.norm is None else hex_linear(self.norm(x), self.qkv.weight)
+        qkv = self.qkv(x if self.norm is None else self.norm(x))
         return qkv.view(-1, Hq + 2 * Hkv, self.head_dim)
 
     def _leave(self, o, x):
         """The output projection of o, and x."""
-        if self.norm is None:
-            return x + self.out(o)
-        return hex_linear(o, self.out.weight, residual=x)
+        out = self.out
+        if _bare(out, _Projection):
+            return hex_linear(o, out.weight, out.bias, residual=x)
+        return x + out(o)
 
     def forward(self, x, pos, start):
         o = HexPixelAttentionFunction.apply(self._project(x), self.q_norm, self.k_norm, pos,
@@ -968,8 +991,7 @@ class HexPixelAttention(nn.Module):
                                             self.causal)
         if not (self.training and self.dropout > 0):
             return self._leave(o.flatten(1), x)
-        y = self.out(o.flatten(1)) if self.norm is None else hex_linear(o.flatten(1),
-                                                                        self.out.weight)
+        y = self.out(o.flatten(1))
         # both words from torch's generator of the device, as its own dropout
         # draws: who saves and restores that (activation checkpointing) gets the
         # same mask again, and a captured graph draws a new one in every replay

@@ -28,3 +28,29 @@ def test_serving_in_training(dtype):
         got.append([b.prefill(x, pos, start, cache, 5), b.step(new, at, cache)])
     for u, v in zip(*got):
         assert torch.equal(u, v)
+
+
+# results rounded once more, and all that follows from them: a few roundings of a norm
+TOL = {torch.float32: 1e-6, torch.bfloat16: 1e-2}
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", ["attention.norm", "attention.qkv", "attention.out",
+                                  "feed_forward.norm"])
+def test_hooked_parts(name, dtype):
+    """A hook that only looks on changes roundings at most, forward and backward."""
+    torch_mod()
+    torch.manual_seed(1)
+    b = hnn.HexPixelBlock(48, 4, 2, 16, hidden=72, device="cuda", dtype=dtype)
+    x = torch.randn(70, 48, device="cuda").to(dtype).requires_grad_(True)
+    pos = torch.rand(70, 3, device="cuda")
+    start = torch.tensor([0, 30, 70], dtype=torch.int32, device="cuda")
+    gy, got, seen = torch.randn(70, 48, device="cuda").to(dtype), [], []
+    for hooked in (False, True):
+        if hooked:
+            b.get_submodule(name).register_forward_hook(lambda m, a, y: seen.append(y.shape))
+        y = b(x, pos, start)
+        got.append([y.detach(), *torch.autograd.grad(y, [x, *b.parameters()], gy)])
+    assert len(seen) == 1
+    for u, v in zip(*got):
+        assert float((u.double() - v.double()).norm() / u.double().norm()) <= TOL[dtype]

@@ -366,7 +366,7 @@ size_t linear_fwd(const LinearArgs &a, void *ws, bool run, Dtype dt, hipStream_t
                   hipError_t &err);
 size_t linear_bwd(const LinearArgs &a, const LinearGrads &g, void *ws, bool run, Dtype dt,
                   hipStream_t st, hipError_t &err);
-// p[0 .. n - 1] := 0
+// p[0 .. n - 1] := 0, p 16-byte aligned, n up to 2^33
 hipError_t zero_fill(void *p, int64_t n, Dtype dt, hipStream_t st);
 
 // ---- gated feed-forward ---------------------------------------------------

@@ -118,14 +118,18 @@ template <bool TALL, int B, int KS, int NW> struct Loader {
     // Load j of a tile; base: of the block's rows and the tile's k.  As an
     // instruction of its own, so that the compiler does not wait for loads of one
     // buffer where another is read (it did, in one turn of three); meet() in the
-    // kernel waits.  It has no result in registers, a buffer is read behind a
-    // meeting only, and nothing else here uses m0.
+    // kernel waits.  A buffer is read behind a meeting only.  m0, which names the place
+    // in LDS, is put back: it is the compiler's, which takes no word that a statement
+    // changes it.
     __device__ __forceinline__ void load(char *lds, int wave, const char *base, int j) const
     {
         const uint32_t to = static_cast<uint32_t>(
             reinterpret_cast<uintptr_t>((LdsPtr)(lds + 1024 * (wave + NW * j))));
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to),
-                     "v"(at[j]), "s"(base));
+        uint32_t was;
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                     "global_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                     : "=&s"(was)
+                     : "s"(to), "v"(at[j]), "s"(base));
     }
     // a tile of `left` k: the chunks past them become zeros, each lane in its place
     __device__ __forceinline__ void load_part(char *lds, int wave, const char *base, int left) const

@@ -30,7 +30,7 @@ using gemm::Side;
 // of their norm); so eight values in a row become float16, 11 bits, where all of
 // them have its exponents, 2^-14 .. 2^15, and bfloat16 where one has not: 2.4e-3,
 // as a projection's gradients have.  The first value's last bit says which (1:
-// float16), so that it is off by up to twice a rounding.
+// float16), so that it is off by up to a step of its type, twice a rounding.
 struct Kept {
     template <typename E> static __device__ __forceinline__ void save(E *p, const float (&v)[8])
     {
@@ -55,7 +55,11 @@ struct Kept {
                 for (int i = 0; i < 8; ++i)
                     h[i] = static_cast<_Float16>(v[i]);
                 u = __builtin_bit_cast(uint4, h);
-                u.x |= 1u;
+                // the first cut, not rounded: the odd number that it lies next to is then
+                // a step away at most, half a step more after rounding
+                const uint32_t cut =
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(v[0], 0.f));
+                u.x = (u.x & 0xffff0000u) | (cut & 0xffffu) | 1u;
             } else {
                 pack8<bf16raw>(v, &u);
                 // the first to 7 bits, to nearest even

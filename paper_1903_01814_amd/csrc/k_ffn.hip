@@ -230,9 +230,16 @@ hipError_t gated_grad(const Plan &pl, const Side &W2, const Side &DY, float *ws,
 
 int ffn_width(int F) { return static_cast<int>(pitch(F)); }
 
-// From so many tokens on w2 is copied to rows that begin on cache lines, as h's do:
-// the forward of 4096 tokens, 1024 and 2736 features 98 us without and 102 with it, of
-// 16384, 512 and 1368 104 and 103, of 16432, 2048 and 5464 1060 and 1025.
+// From so many tokens on w2 is copied to rows that begin on cache lines, as h's do.
+// Forward in us, without and with the copy:
+//   features          4096 tokens     8192           12288          16384
+//   512 and 1368      36.4    38.6    59.8    61.6   88.9    90.5   104.5   104.0
+//   1024 and 2736     97.1   100.3   168.6   168.4   252.9   250.1  294.1   295.0
+//   2048 and 1368     96.4    97.4   159.0   160.9   234.5   234.4  275.5   279.2
+//   1024 and 5464     165.9  168.7   343.0   330.7   487.5   465.9  570.7   549.4
+//   2048 and 5464     303.4  295.0   506.1   507.4   799.5   791.8  1035.9  1000.6
+// A copy costs 2 to 4 us where h is small beside the caches, and gains 1 to 4 % from
+// where it is not; 32768 tokens of 2048 and 5464 2048 and 1970.
 constexpr int kCopy = 8192;
 
 size_t ffn_fwd(const FfnArgs &a, void *ws, bool run, Dtype dt, hipStream_t st, hipError_t &err)

@@ -371,7 +371,8 @@ hipError_t zero_fill(void *p, int64_t n, Dtype dt, hipStream_t st);
 
 // ---- gated feed-forward ---------------------------------------------------
 // h = act(x wg^T + bg) (x wu^T + bu), y = h w2^T + b2 + res; w1 = wg over wu.
-// gu [M][2 Fp] and h [M][Fp] with Fp = F rounded up to 8.
+// gu [M][2 Fp] and h [M][Fp] with Fp = ffn_width(F); the columns from F on are written,
+// with zeros.
 struct FfnArgs {
     const void *x, *w1, *b1, *w2, *b2, *res;
     void *y, *gu, *h;

@@ -560,6 +560,8 @@ def hex_dropout(x, p, rng, residual=None, call=0):
 
 
 # ----------------------------------------- operators on tokens by themselves
+# Projections and gated blocks in float32 take infinities, and values from 3.39e38 on,
+# as NaN in gradients and for more than 32 tokens (hexconv.h); no other token sees them.
 
 ACTIVATIONS = {None: hx.HEX_ACT_NONE, "relu": hx.HEX_ACT_RELU, "gelu": hx.HEX_ACT_GELU,
                "silu": hx.HEX_ACT_SILU}
@@ -725,7 +727,8 @@ def hex_layer_norm(x, weight=None, bias=None, eps=1e-5):
 
 def hex_linear(x, weight, bias=None, residual=None, activation=None):
     """activation(x weight^T + bias) + residual over the last axis of x: weight
-    [out, in], activation None, "relu", "gelu" or "silu"."""
+    [out, in], activation None, "relu", "gelu" or "silu".  float32 infinities give NaN
+    from 33 tokens on and in gradients."""
     shape = x.shape[:-1] + weight.shape[:1]
     if residual is not None:
         if residual.shape != shape:
@@ -739,7 +742,8 @@ def hex_linear(x, weight, bias=None, residual=None, activation=None):
 
 def hex_feed_forward(x, w1, w2, b1=None, b2=None, activation="silu", residual=False, norm=None):
     """(activation(n w1[:F]^T + b1[:F]) (n w1[F:]^T + b1[F:])) w2^T + b2, plus x where
-    `residual` is true; n is x, or with norm = (weight, bias, eps) its layer norm."""
+    `residual` is true; n is x, or with norm = (weight, bias, eps) its layer norm.
+    float32 infinities give NaN from 33 tokens on and in gradients."""
     if residual and w2.shape[0] != x.shape[-1]:
         raise ValueError("hex_feed_forward: a residual needs as many features out as in")
     nw, nb, eps = (None, None, None) if norm is None else norm
@@ -771,8 +775,8 @@ class HexLayerNorm(nn.Module):
 
 class HexLinear(nn.Module):
     """Projection over the last axis with an activation (None, "relu", "gelu",
-    "silu"); forward(x, residual=None) adds the residual in the same pass.
-    Initial weights and bias are uniform in +-1/sqrt(in_features)."""
+    "silu"); forward(x, residual=None) adds the residual in the same pass.  float32
+    infinities as in hex_linear.  Initial weights and bias are uniform in +-1/sqrt(in_features)."""
 
     def __init__(self, in_features, out_features, bias=True, activation=None, device=None,
                  dtype=None):
@@ -824,7 +828,7 @@ class HexFeedForward(nn.Module):
     the other projection's.  Each token by itself: forward takes any leading axes, and
     is its own form for single tokens.  forward(x, drop=False) leaves the dropout out in
     training too, as serving does.  A norm with hooks, or another module in its place, is
-    called by itself."""
+    called by itself.  float32 infinities as in hex_feed_forward."""
 
     def __init__(self, dim, hidden, activation="silu", bias=False, norm=True, dropout=0.0, eps=1e-5,
                  device=None, dtype=None):
